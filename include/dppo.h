@@ -62,6 +62,9 @@ enum { DPPO_BINARY_TV = 0, DPPO_BINARY_KL = 1, DPPO_TOPK_TV = 2, DPPO_TOPK_KL = 
        DPPO_GIVEN_D = 6 };
 /* Element types of the logits / dlogits tensors. */
 enum { DPPO_F32 = 0, DPPO_BF16 = 1 };
+/* 8-bit floating-point formats (dppo_fp8_quantize, dppo_gemm_tn_fp8): 4 exponent and 3 mantissa bits without infinities
+ * (largest value 448), or 5 and 2 (57344). */
+enum { DPPO_E4M3 = 0, DPPO_E5M2 = 1 };
 /* opts->dlogits_dtype */
 enum { DPPO_DLOGITS_SAME = 0, DPPO_DLOGITS_F32 = 1 };
 /* opts->kernel.  RING: the bulk-copy (TMA) streaming kernel; it takes logits / dlogits whose bases are 16-byte aligned
@@ -97,7 +100,8 @@ enum {
   DPPO_STATUS_BAD_SAMPLED_ID = 1, /* sampled_ids[t] outside [0, V)          */
   DPPO_STATUS_BAD_TOPK_ID = 2,    /* a mu_topk_ids entry outside [0, V)     */
   DPPO_STATUS_NONFINITE_ROW = 4,  /* lse of a row is NaN or infinite         */
-  DPPO_STATUS_WAIT_LIMIT = 8      /* a bounded on-chip wait gave up          */
+  DPPO_STATUS_WAIT_LIMIT = 8,     /* a bounded on-chip wait gave up          */
+  DPPO_STATUS_BAD_SAMPLING = 16   /* dppo_sample: a setting of a row outside its range */
 };
 
 /* Options; all-zero means defaults. */
@@ -317,6 +321,84 @@ int dppo_exact_divergence(const void* logits, const void* mu_logits, int64_t T, 
                           int64_t logits_row_stride, int64_t mu_row_stride, int dtype,
                           const uint8_t* token_mask, float* tv, float* kl, float* entropy,
                           int32_t* status, const dppo_opts* opts, void* cuda_stream);
+
+/*
+ * Draws one token per row of logits and records what the loss entry points read about it: the rollout side of the step
+ * (Sec. 3: a_t ~ mu(. | s_t); Sec. 4.4: the ids and probabilities of mu's K most probable tokens).
+ *
+ * mu is the distribution the token is drawn from.  With z the row, tau its temperature and w_j = exp((z_j - max z) / tau),
+ * order the tokens by logit, largest first, equal logits by id, lowest first.  Kept are
+ *   the first top_k tokens (top_k <= 0 or >= V: all),
+ *   of those the shortest prefix whose mass is at least top_p times theirs, never less than one token (top_p >= 1: all),
+ *   of those the tokens with w_j >= min_p (min_p = 0: all);
+ * mu(j) = w_j / (sum of the kept w) for kept j, 0 otherwise.  tau = 0 is greedy: the largest logit, mu = 1.  The token drawn is
+ * the lowest id a with  sum_{j <= a} mu(j) > uniform.  Logits of -inf (and tokens whose weight is below 2^-1000) are never
+ * drawn and never kept.
+ *
+ *  logits         [T, V] row-major, row stride in elements (>= V; rows may start at any element), DPPO_F32 or DPPO_BF16;
+ *                 V < 2^31.
+ *  uniform        [T] double in [0, 1): one random number per row (8-byte aligned).  Doubles, because an fp32 uniform's steps
+ *                 of 2^-24 are coarser than the probabilities in the tail of a large vocabulary.
+ *  temperature    [T] fp32 >= 0, finite; NULL = 1 for all rows.        top_k   [T] int32; NULL = off.
+ *  top_p          [T] fp32 >= 0; NULL = off.                           min_p   [T] fp32 in [0, 1]; NULL = off.
+ *  token_mask     [T] bytes or NULL; rows with a zero byte are not read and give zeros.
+ *  K              width of the record, 0 <= K <= min(V, DPPO_SAMPLE_MAX_TOPK); 0 = none.
+ *  sampled_ids    [T] out.         mu_logp  [T] out: log mu(a).
+ *  mu_topk_ids    [T, K] out: the first K tokens of the order above (-inf logits last, by id).
+ *  mu_topk_p      [T, K] out: their mu (0 for tokens that are not kept).  Both may be NULL when K == 0.
+ *  status         device word: DPPO_STATUS_NONFINITE_ROW (a NaN or +inf logit, or nothing but -inf), DPPO_STATUS_BAD_SAMPLING
+ *                 (a setting or the uniform number outside its range); such rows give zeros.
+ * Needs no workspace; one kernel launch.  The same inputs give the same bits.
+ */
+#define DPPO_SAMPLE_MAX_TOPK 1024
+int dppo_sample(const void* logits, int64_t T, int64_t V, int64_t logits_row_stride, int logits_dtype,
+                const double* uniform, const float* temperature, const int32_t* top_k, const float* top_p,
+                const float* min_p, const uint8_t* token_mask, int K,
+                int32_t* sampled_ids, float* mu_logp, int32_t* mu_topk_ids, float* mu_topk_p,
+                int32_t* status, void* cuda_stream);
+
+/*
+ * Rounds a matrix to 8-bit floating point with one fp32 scale per block, as stored and / or transposed, reading it once:
+ * the operands of dppo_gemm_tn_fp8.
+ *
+ *  x           [rows, cols] row-major, row stride in elements (>= cols, any alignment), x_dtype DPPO_F32 or DPPO_BF16.
+ *  fp8_format  DPPO_E4M3 or DPPO_E5M2; B = its largest finite value.
+ *  block_rows  1: one scale per 1 x 128 elements along a row of the result; 128: one per 128 x 128 elements.  Blocks at the
+ *              edges are smaller.
+ *  q           [rows, cols] out, one byte per element, row stride q_row_stride >= cols (bytes behind a row are left alone), or
+ *              NULL.  q = x / scale rounded to nearest even, scale = max(amax, 2^-100) / B with amax the block's largest
+ *              magnitude.
+ *  q_scale     out: scale of the block of row (block) i and columns 128 k .. 128 k + 127 at q_scale[i * row_stride + k * k_stride];
+ *              the strides may have either order but must not make two scales share a place.
+ *  qt          [cols, rows] out: the same for the transposed matrix (blocks run along x's columns), or NULL.  With
+ *              block_rows = 128 its bytes and scales are those of q, transposed.  At least one of q and qt is given.
+ *  status      device word: DPPO_STATUS_NONFINITE_ROW if a block holds a NaN or an infinity; its scale and all its bytes are NaN.
+ */
+int dppo_fp8_quantize(const void* x, int64_t rows, int64_t cols, int64_t x_row_stride, int x_dtype, int fp8_format,
+                      int block_rows, void* q, int64_t q_row_stride, float* q_scale, int64_t q_scale_row_stride,
+                      int64_t q_scale_k_stride, void* qt, int64_t qt_row_stride, float* qt_scale,
+                      int64_t qt_scale_row_stride, int64_t qt_scale_k_stride, int32_t* status, void* cuda_stream);
+
+/*
+ * C[M, N] = A[M, K] . B[N, K]^T for 8-bit floating-point matrices with a scale per block of 128 along K:
+ *   C[m, n] = sum_kb a_scale[m, kb] b_scale[n, kb] sum_{k in block kb} A[m, k] B[n, k].
+ * Tensor cores (tcgen05, fp32 accumulation) form the inner sums in tensor memory; each is scaled and added up in fp32
+ * registers.
+ *
+ *  A, B        row-major with K contiguous, row strides lda, ldb in bytes (>= K, multiples of 16; 16-byte aligned bases), formats
+ *              DPPO_E4M3 or DPPO_E5M2 each.  Bytes behind column K are not read as data.
+ *  a_block_rows, b_block_rows  1 or 128: rows of A (of B) that share a scale.
+ *  a_scale     scale of row (block) i and K block k at a_scale[i * a_scale_row_stride + k * a_scale_k_stride]; b_scale alike.
+ *              With row stride 1 the kernel reads them in whole lines.
+ *  C           [M, N], c_dtype DPPO_F32 or DPPO_BF16 (rounded once, from the fp32 sum), row stride ldc elements (>= N).
+ *  K = 0 gives C = 0.  status: device word, DPPO_STATUS_WAIT_LIMIT (may be NULL).  opts: wait_limit_us, test_inject.
+ */
+int dppo_gemm_tn_fp8(const void* A, int64_t lda, int a_format, int a_block_rows, const float* a_scale,
+                     int64_t a_scale_row_stride, int64_t a_scale_k_stride,
+                     const void* B, int64_t ldb, int b_format, int b_block_rows, const float* b_scale,
+                     int64_t b_scale_row_stride, int64_t b_scale_k_stride,
+                     int M, int N, int K, void* C, int c_dtype, int64_t ldc,
+                     int32_t* status, const dppo_opts* opts, void* cuda_stream);
 
 /* Name of an error code (static string, never NULL). */
 const char* dppo_error_string(int code);

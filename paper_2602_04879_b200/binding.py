@@ -18,7 +18,9 @@ F32, BF16 = 0, 1
 DLOGITS_SAME, DLOGITS_F32 = 0, 1
 KERNEL_AUTO, KERNEL_GENERIC, KERNEL_RING = 0, 1, 2
 INJECT_NO_COPIES = 1
-STATUS_BAD_SAMPLED_ID, STATUS_BAD_TOPK_ID, STATUS_NONFINITE_ROW, STATUS_WAIT_LIMIT = 1, 2, 4, 8
+STATUS_BAD_SAMPLED_ID, STATUS_BAD_TOPK_ID, STATUS_NONFINITE_ROW, STATUS_WAIT_LIMIT, STATUS_BAD_SAMPLING = 1, 2, 4, 8, 16
+E4M3, E5M2 = 0, 1
+FP8_FORMATS = {torch.float8_e4m3fn: E4M3, torch.float8_e5m2: E5M2}
 VARIANTS = {"binary_tv": BINARY_TV, "binary_kl": BINARY_KL, "topk_tv": TOPK_TV, "topk_kl": TOPK_KL, "ppo_clip": PPO_CLIP, "minimal_mask": MINIMAL_MASK, "given_d": GIVEN_D}
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libdppo.so")
@@ -90,6 +92,16 @@ def lib():
         L.dppo_gemm_nn_bf16.argtypes = L.dppo_gemm_tn_bf16.argtypes
         L.dppo_loss_fwd_bwd_static_ws.restype = c_int
         L.dppo_loss_fwd_bwd_static_ws.argtypes = L.dppo_loss_fwd_bwd.argtypes[:22] + [c_void_p]
+        L.dppo_sample.restype = c_int
+        L.dppo_sample.argtypes = [c_void_p, c_int64, c_int64, c_int64, c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                  c_void_p, c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
+        L.dppo_fp8_quantize.restype = c_int
+        L.dppo_fp8_quantize.argtypes = [c_void_p, c_int64, c_int64, c_int64, c_int, c_int, c_int, c_void_p, c_int64, c_void_p, c_int64, c_int64,
+                                        c_void_p, c_int64, c_void_p, c_int64, c_int64, c_void_p, c_void_p]
+        L.dppo_gemm_tn_fp8.restype = c_int
+        L.dppo_gemm_tn_fp8.argtypes = [c_void_p, c_int64, c_int, c_int, c_void_p, c_int64, c_int64,
+                                       c_void_p, c_int64, c_int, c_int, c_void_p, c_int64, c_int64,
+                                       c_int, c_int, c_int, c_void_p, c_int, c_int64, c_void_p, POINTER(DppoOpts), c_void_p]
         _lib = L
     return _lib
 
@@ -356,3 +368,106 @@ def dppo_loss_fwd_bwd_host(logits, sampled_ids, mu_logp, advantages, token_mask=
     if rc != 0:
         raise DppoError(rc, "dppo_loss_fwd_bwd_host")
     return dict(loss=float(loss.value), divergence=D, mask=M, dlogits=dl, status=int(status.value))
+
+
+SAMPLE_MAX_TOPK = 1024
+
+
+def dppo_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, token_mask=None, K=0, out=None, status=None,
+                stream=None):
+    """Calls ``dppo_sample`` on CUDA tensors: one token per row of ``logits`` [T,V] (fp32 or bf16, any row stride) from the
+    uniform numbers ``uniform`` [T] float64.  ``temperature``, ``top_p``, ``min_p`` [T] fp32 and ``top_k`` [T] int32 may each
+    be None (off).  Returns dict(sampled_ids[T] int32, mu_logp[T], mu_topk_ids[T,K], mu_topk_p[T,K] (None for K = 0),
+    status[1]), which ``dppo_loss_fwd_bwd`` takes as they are; ``out``: a dict of those tensors to write into.  Nothing is
+    synchronised."""
+    assert logits.is_cuda and logits.dim() == 2 and (logits.shape[1] <= 1 or logits.stride(1) == 1)
+    T, V = logits.shape
+    dev = logits.device
+    for name, t, dt in (("uniform", uniform, torch.float64), ("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                        ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32), ("token_mask", token_mask, torch.uint8)):
+        assert t is None or (t.device == dev and t.dtype == dt and t.shape == (T,) and t.is_contiguous()), name
+    if out is None:
+        out = dict(sampled_ids=torch.empty(T, dtype=torch.int32, device=dev), mu_logp=torch.empty(T, dtype=torch.float32, device=dev),
+                   mu_topk_ids=torch.empty((T, K), dtype=torch.int32, device=dev) if K > 0 else None,
+                   mu_topk_p=torch.empty((T, K), dtype=torch.float32, device=dev) if K > 0 else None)
+    else:
+        for name, dt, shape in (("sampled_ids", torch.int32, (T,)), ("mu_logp", torch.float32, (T,)), ("mu_topk_ids", torch.int32, (T, K)),
+                                ("mu_topk_p", torch.float32, (T, K))):
+            t = out.get(name)
+            assert (t is None and len(shape) == 2 and K == 0) or (t.device == dev and t.dtype == dt and t.shape == shape and t.is_contiguous()), name
+    if status is None:
+        status = torch.zeros(1, dtype=torch.int32, device=dev)
+    st = stream if stream is not None else torch.cuda.current_stream(dev)
+    with torch.cuda.device(dev):
+        rc = lib().dppo_sample(_ptr(logits), T, V, logits.stride(0) if T > 1 else V, _dtype_code(logits), _ptr(uniform), _ptr(temperature),
+                               _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(token_mask), int(K), _ptr(out["sampled_ids"]), _ptr(out["mu_logp"]),
+                               _ptr(out.get("mu_topk_ids")), _ptr(out.get("mu_topk_p")), _ptr(status), c_void_p(st.cuda_stream))
+    if rc != 0:
+        raise DppoError(rc, "dppo_sample")
+    return dict(sampled_ids=out["sampled_ids"], mu_logp=out["mu_logp"], mu_topk_ids=out.get("mu_topk_ids"), mu_topk_p=out.get("mu_topk_p"),
+                status=status)
+
+
+def _fp8_pair(rows, cols, block_rows, dtype, dev):
+    """An 8-bit matrix whose rows start on 16-byte boundaries and its scales [row blocks, column blocks], stored block column after
+    block column: what dppo_gemm_tn_fp8 reads fastest."""
+    q = torch.empty((rows, -(-cols // 16) * 16), dtype=dtype, device=dev)[:, :cols]
+    scale = torch.empty((-(-cols // 128), -(-rows // block_rows)), dtype=torch.float32, device=dev).t()
+    return q, scale
+
+
+def dppo_fp8_quantize(x, dtype=torch.float8_e4m3fn, block_rows=1, rowwise=True, transposed=False, status=None, stream=None):
+    """Calls ``dppo_fp8_quantize`` on a CUDA matrix x [rows,cols] (fp32 or bf16, any row stride).  ``dtype``: torch.float8_e4m3fn or
+    torch.float8_e5m2; ``block_rows`` 1 or 128.  Returns dict(q, scale, qt, qt_scale, status): q [rows,cols] and its scales
+    [row blocks, column blocks] with ``rowwise``, qt [cols,rows] and its scales with ``transposed`` (None otherwise); the rows of
+    q and qt start on 16-byte boundaries, as ``dppo_gemm_tn_fp8`` wants them.  Nothing is synchronised."""
+    assert x.is_cuda and x.dim() == 2 and (x.shape[1] <= 1 or x.stride(1) == 1) and dtype in FP8_FORMATS and (rowwise or transposed)
+    rows, cols = x.shape
+    dev = x.device
+    q = scale = qt = qt_scale = None
+    block = 128 if int(block_rows) == 128 else 1
+    if rowwise:
+        q, scale = _fp8_pair(rows, cols, block, dtype, dev)
+    if transposed:
+        qt, qt_scale = _fp8_pair(cols, rows, block, dtype, dev)
+    if status is None:
+        status = torch.zeros(1, dtype=torch.int32, device=dev)
+    st = stream if stream is not None else torch.cuda.current_stream(dev)
+
+    def strides(m, s):
+        return (m.stride(0), _ptr(s), s.stride(0), s.stride(1)) if m is not None else (0, None, 0, 0)
+    with torch.cuda.device(dev):
+        rc = lib().dppo_fp8_quantize(_ptr(x), rows, cols, x.stride(0) if rows > 1 else cols, _dtype_code(x), FP8_FORMATS[dtype], int(block_rows),
+                                     _ptr(q), *strides(q, scale), _ptr(qt), *strides(qt, qt_scale), _ptr(status), c_void_p(st.cuda_stream))
+    if rc != 0:
+        raise DppoError(rc, "dppo_fp8_quantize")
+    return dict(q=q, scale=scale, qt=qt, qt_scale=qt_scale, status=status)
+
+
+def dppo_gemm_tn_fp8(A, a_scale, B, b_scale, a_block_rows=1, b_block_rows=128, out_dtype=torch.float32, C=None, status=None, stream=None,
+                     wait_limit_us=0, test_inject=0):
+    """C[M,N] = A[M,K] . B[N,K]^T for 8-bit CUDA matrices (torch.float8_e4m3fn / torch.float8_e5m2, last dimension contiguous, rows on
+    16-byte boundaries) with fp32 scales [row blocks, ceil(K/128)] of any strides.  ``a_block_rows`` / ``b_block_rows``: rows that
+    share a scale, 1 or 128.  Returns (C, status), C fp32 or bf16; nothing is synchronised."""
+    assert A.is_cuda and B.is_cuda and A.dtype in FP8_FORMATS and B.dtype in FP8_FORMATS and A.dim() == 2 and B.dim() == 2
+    M, K = A.shape
+    N = B.shape[0]
+    assert B.shape[1] == K and B.device == A.device and (K <= 1 or (A.stride(1) == 1 and B.stride(1) == 1))
+    for name, s, rows, blk in (("a_scale", a_scale, M, a_block_rows), ("b_scale", b_scale, N, b_block_rows)):
+        assert s.device == A.device and s.dtype == torch.float32 and s.shape == (-(-rows // (128 if int(blk) == 128 else 1)), -(-K // 128)), name
+    if C is None:
+        C = torch.empty((M, N), dtype=out_dtype, device=A.device)
+    assert C.device == A.device and C.shape == (M, N) and (N <= 1 or C.stride(1) == 1)
+    if status is None:
+        status = torch.zeros(1, dtype=torch.int32, device=A.device)
+    st = stream if stream is not None else torch.cuda.current_stream(A.device)
+    up16 = -(-K // 16) * 16                               # a single row has no pitch of its own
+    with torch.cuda.device(A.device):
+        rc = lib().dppo_gemm_tn_fp8(_ptr(A), A.stride(0) if M > 1 else up16, FP8_FORMATS[A.dtype], int(a_block_rows), _ptr(a_scale),
+                                    a_scale.stride(0), a_scale.stride(1), _ptr(B), B.stride(0) if N > 1 else up16, FP8_FORMATS[B.dtype],
+                                    int(b_block_rows), _ptr(b_scale), b_scale.stride(0), b_scale.stride(1), M, N, K, _ptr(C), _dtype_code(C),
+                                    C.stride(0) if M > 1 else N, _ptr(status),
+                                    ctypes.byref(_opts(wait_limit_us=wait_limit_us, test_inject=test_inject)), c_void_p(st.cuda_stream))
+    if rc != 0:
+        raise DppoError(rc, "dppo_gemm_tn_fp8")
+    return C, status

@@ -1,0 +1,274 @@
+"""Drawing tokens from rows of logits against the float64 restatement (needs a B200).
+
+Tolerances.  The sums are 64-bit and the exponentials good to 1.3e-12 relative, so the running sums are off by less than 1e-11
+of the whole mass: ids are compared wherever no decision of the exact computation is closer than that to flipping.  mu_logp and
+the record's probabilities are rounded to fp32 once: 2^-24 relative, plus 1e-11 for what goes before."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2602_04879_b200 as dppo
+from paper_2602_04879_b200 import binding
+from oracle import rollout_oracle as R
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+EDGE = 1e-11
+
+
+def _rows(T, V, dtype, seed, sigma=3.0, peak=8.0):
+    g = torch.Generator().manual_seed(seed)
+    z = sigma * torch.randn((T, V), generator=g)
+    z[torch.arange(T), torch.randint(0, V, (T,), generator=g)] += peak * torch.rand(T, generator=g)
+    return z.to(dtype)
+
+
+def _uniform(T, seed):
+    return torch.rand(T, generator=torch.Generator().manual_seed(seed + 77), dtype=torch.float64)
+
+
+def _settings(T, seed, kinds):
+    g = torch.Generator().manual_seed(seed + 5)
+    s = {}
+    if "t" in kinds:
+        s["temperature"] = 0.3 + 1.2 * torch.rand(T, generator=g)
+        s["temperature"][::7] = 0.0
+    if "k" in kinds:
+        s["top_k"] = torch.randint(-1, 60, (T,), generator=g, dtype=torch.int32)
+    if "K" in kinds:
+        s["top_k"] = torch.randint(1000, 3000, (T,), generator=g, dtype=torch.int32)
+    if "p" in kinds:
+        s["top_p"] = 0.3 + 0.75 * torch.rand(T, generator=g)
+    if "P" in kinds:
+        s["top_p"] = 0.9 + 0.0999 * torch.rand(T, generator=g)
+    if "m" in kinds:
+        s["min_p"] = 0.2 * torch.rand(T, generator=g) ** 3
+    return s
+
+
+def _on_gpu(z, u, K, s, mask=None, **kw):
+    return dppo.dppo_sample(z if z.is_cuda else z.to(DEV), u.to(DEV), K=K, token_mask=None if mask is None else mask.to(DEV),
+                            **{n: v.to(DEV) for n, v in s.items()}, **kw)
+
+
+def _check(out, z, u, K, s, mask=None, rows=None, status=0):
+    torch.cuda.synchronize()
+    assert int(out["status"].item()) == status
+    zh = z.float().cpu().numpy()
+    ids, logp = out["sampled_ids"].cpu().numpy(), out["mu_logp"].cpu().numpy()
+    tid = out["mu_topk_ids"].cpu().numpy() if K else None
+    tp = out["mu_topk_p"].cpu().numpy() if K else None
+    compared = 0
+    for t in rows if rows is not None else range(zh.shape[0]):
+        one = {n: v[t].item() for n, v in s.items()}
+        ora = R.sample_row(zh[t], u[t].item(), K=K, **one) if mask is None or mask[t] else None
+        if ora is None:
+            assert ids[t] == 0 and logp[t] == 0 and (not K or (not tid[t].any() and not tp[t].any())), t
+            continue
+        assert 0 <= ids[t] < zh.shape[1]
+        if K:
+            assert np.array_equal(tid[t], ora["top_ids"]), (t, tid[t], ora["top_ids"])
+        if ora["margin"] < EDGE:
+            continue
+        compared += 1
+        assert ids[t] == ora["id"], (t, ids[t], ora["id"], ora["margin"], one)
+        assert abs(logp[t] - ora["logp"]) <= 2.0 ** -24 * abs(ora["logp"]) + EDGE, (t, logp[t], ora["logp"])
+        if K:
+            assert np.all(np.abs(tp[t] - ora["top_p"]) <= 2.0 ** -24 * ora["top_p"] + EDGE), t
+    return compared
+
+
+@pytest.mark.parametrize("kinds", ["", "t", "k", "p", "m", "tkpm", "tPm", "P", "K", "tKp", "Km"])
+@pytest.mark.parametrize("T,V,dtype,K", [(40, 4096, torch.float32, 20), (33, 50257, torch.bfloat16, 64), (9, 151936, torch.bfloat16, 0),
+                                         (150, 1001, torch.float32, 5)])
+def test_sampling_matches_the_definition(T, V, dtype, K, kinds):
+    z, u, s = _rows(T, V, dtype, seed=V + T), _uniform(T, V), _settings(T, V, kinds)
+    assert _check(_on_gpu(z, u, K, s), z, u, K, s) >= T - 1
+
+
+@pytest.mark.parametrize("V", [1, 2, 3, 7, 8, 9, 31, 255, 256, 257, 1024, 8191, 20481])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_odd_sizes_and_full_width_records(V, dtype):
+    T, K = 12, min(V, 1024)
+    z, u, s = _rows(T, V, dtype, seed=V), _uniform(T, V), _settings(T, V, "tpm")
+    assert _check(_on_gpu(z, u, K, s), z, u, K, s) >= T - 1
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("offset", [0, 1, 3, 8])
+def test_rows_of_a_wider_tensor_at_any_offset(dtype, offset):
+    """Row strides above V, rows that start at any element; what lies beside the rows is NaN and must not be looked at."""
+    T, V = 10, 3001
+    wide = torch.full((T, V + 37), float("nan"), dtype=dtype)
+    z = _rows(T, V, dtype, seed=offset)
+    wide[:, offset:offset + V] = z
+    w, u, s = wide.to(DEV)[:, offset:offset + V], _uniform(T, 3), _settings(T, 3, "tp")
+    assert w.stride(0) == V + 37
+    assert _check(_on_gpu(w, u, 16, s), z, u, 16, s) >= T - 1
+
+
+def test_a_row_does_not_depend_on_how_many_share_the_call():
+    """1 to 100 rows a call: eight, four, two or one SM per row; the same ids, and values equal up to the order of 64-bit additions."""
+    z, u, s = _rows(100, 151936, torch.bfloat16, seed=4), _uniform(100, 4), _settings(100, 4, "tP")
+    whole = _on_gpu(z, u, 20, s)
+    for T in (1, 18, 19, 37, 74, 75):
+        part = _on_gpu(z[:T], u[:T], 20, {n: v[:T] for n, v in s.items()})
+        assert torch.equal(part["sampled_ids"], whole["sampled_ids"][:T]) and torch.equal(part["mu_topk_ids"], whole["mu_topk_ids"][:T])
+        assert torch.allclose(part["mu_logp"], whole["mu_logp"][:T], rtol=2.0 ** -23, atol=1e-11)
+        again = _on_gpu(z[:T], u[:T], 20, {n: v[:T] for n, v in s.items()})
+        assert all(torch.equal(part[n], again[n]) for n in part)
+
+
+NEG = float("-inf")
+
+
+def _special_rows(dtype, V=6000):
+    """Rows that a mask, a tie or an order makes awkward, each with what is special about it."""
+    g = torch.Generator().manual_seed(11)
+    base = 2.0 * torch.randn(V, generator=g)
+    rows = []
+
+    def add(z):
+        rows.append(z.to(dtype))
+    add(torch.where(torch.arange(V) == 4321, base, NEG))                       # one token left
+    add(torch.where(torch.arange(V) % 500 == 3, base, NEG))                    # fewer tokens left than the record holds
+    low = torch.finfo(dtype).min
+    add(torch.where(torch.arange(V) % 700 == 1, base, torch.full((V,), low)))  # masked with the type's lowest value
+    add(torch.full((V,), low))                                                 # nothing but that: uniform
+    add(torch.full((V,), 0.25))                                                # all equal: more ties than the list holds
+    add(torch.where(torch.arange(V) < 5000, torch.full((V,), 3.0), base - 9))  # five thousand ties at the top
+    add(torch.sort(base).values)                                               # ascending, descending: the largest in few groups
+    add(torch.sort(base, descending=True).values)
+    add(torch.zeros(V) * torch.where(torch.arange(V) % 2 == 0, 1.0, -1.0))     # +0 and -0 are equal
+    add(base * 1e4)                                                            # weights far below the smallest double
+    add(base * 1e-4)
+    add(torch.where(torch.arange(V) == 7, torch.full((V,), 3e38), base))
+    add(torch.where(torch.arange(V) % 3 == 0, base, NEG))
+    return torch.stack(rows)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("setting", [{}, {"top_k": 3}, {"top_k": 40}, {"top_k": 1024}, {"top_k": 1500}, {"top_k": 4500}, {"top_p": 0.5}, {"top_p": 0.999},
+                                     {"min_p": 0.3}, {"min_p": 1.0}, {"top_k": 2000, "top_p": 0.7}, {"temperature": 0.01}, {"temperature": 0.0},
+                                     {"temperature": 50.0, "top_p": 0.9, "min_p": 1e-3}, {"top_p": 0.0}])
+def test_masked_tied_and_ordered_rows(dtype, setting):
+    z = _special_rows(dtype)
+    T, K = z.shape[0], 30
+    for seed in (1, 2):
+        u = _uniform(T, seed)
+        s = {n: torch.full((T,), v, dtype=torch.int32 if n == "top_k" else torch.float32) for n, v in setting.items()}
+        _check(_on_gpu(z, u, K, s), z, u, K, s)
+
+
+def test_ends_of_the_unit_interval():
+    z = _rows(8, 5000, torch.float32, seed=2)
+    z[0, :100] = NEG
+    z[1, -100:] = NEG
+    first = torch.zeros(8, dtype=torch.float64)
+    out = _on_gpu(z, first, 0, {})
+    assert out["sampled_ids"].tolist() == [100] + [0] * 7
+    s = {"top_k": torch.full((8,), 50, dtype=torch.int32)}
+    out = _on_gpu(z, first, 0, s)
+    assert out["sampled_ids"].tolist() == [int(torch.topk(r, 50).indices.min()) for r in z]
+    last = torch.full((8,), 1.0 - 2.0 ** -53, dtype=torch.float64)
+    out = _on_gpu(z, last, 0, s)
+    assert out["sampled_ids"].tolist() == [int(torch.topk(r, 50).indices.max()) for r in z]
+    out = _on_gpu(z, last, 0, {})
+    assert all(np.isfinite(z[t, i].item()) for t, i in enumerate(out["sampled_ids"].tolist()))
+
+
+def test_dropped_rows_and_status_bits():
+    z = _rows(8, 3000, torch.float32, seed=9)
+    u = _uniform(8, 9)
+    z[1, 77] = float("nan")
+    z[2, 2999] = float("inf")
+    z[3] = NEG
+    z[4, 5] = -float("nan")
+    mask = torch.tensor([1, 1, 1, 1, 1, 0, 1, 1], dtype=torch.uint8)
+    out = _on_gpu(z, u, 4, {}, mask)
+    _check(out, z, u, 4, {}, mask, status=binding.STATUS_NONFINITE_ROW)
+    # a masked row may hold anything: it is not read
+    z[5] = float("nan")
+    only = torch.tensor([1, 0, 0, 0, 0, 0, 1, 1], dtype=torch.uint8)
+    _check(_on_gpu(z, u, 4, {}, only), z, u, 4, {}, only)
+    good = _rows(6, 500, torch.float32, seed=1)
+    bad = {"temperature": [-1.0, float("nan"), float("inf")], "top_p": [-0.1, float("nan")], "min_p": [-0.1, 1.5, float("nan")]}
+    for name, values in bad.items():
+        for v in values:
+            s = {name: torch.tensor([0.5, 0.5, v, 0.5, 0.5, 0.5])}
+            out = _on_gpu(good, u[:6], 4, s)
+            torch.cuda.synchronize()
+            assert int(out["status"].item()) == binding.STATUS_BAD_SAMPLING
+            assert out["sampled_ids"][2] == 0 and out["mu_logp"][2] == 0 and not out["mu_topk_p"][2].any()
+            s[name][2] = 0.5
+            _check(_on_gpu(good, u[:6], 4, s), good, u[:6], 4, s)
+    for v in (1.0, -1e-300, float("nan")):
+        uu = u[:6].clone()
+        uu[3] = v
+        out = _on_gpu(good, uu, 0, {})
+        torch.cuda.synchronize()
+        assert int(out["status"].item()) == binding.STATUS_BAD_SAMPLING and out["sampled_ids"][3] == 0
+
+
+def test_empty_batch_and_outputs_of_the_caller():
+    out = _on_gpu(torch.empty((0, 100)), torch.empty(0, dtype=torch.float64), 5, {})
+    assert out["sampled_ids"].shape == (0,) and out["mu_topk_ids"].shape == (0, 5)
+    z, u = _rows(3, 400, torch.float32, seed=3), _uniform(3, 3)
+    # the outputs are views into larger buffers whose other entries stay as they were
+    ids = torch.full((5,), -7, dtype=torch.int32, device=DEV)
+    lp = torch.full((5,), -7.0, device=DEV)
+    ti = torch.full((5, 6), -7, dtype=torch.int32, device=DEV)
+    tp = torch.full((5, 6), -7.0, device=DEV)
+    out = _on_gpu(z, u, 6, {}, out=dict(sampled_ids=ids[1:4], mu_logp=lp[1:4], mu_topk_ids=ti[1:4], mu_topk_p=tp[1:4]))
+    _check(out, z, u, 6, {})
+    assert all(b[0].eq(-7).all() and b[4].eq(-7).all() for b in (ids, lp, ti, tp))
+
+
+def test_long_rows_beyond_the_usual_vocabulary():
+    for V, dtype in ((1 << 20, torch.bfloat16), ((1 << 21) + 3, torch.float32)):
+        z, u = _rows(2, V, dtype, seed=5), _uniform(2, 5)
+        for kinds in ("", "P", "k"):
+            s = _settings(2, 6, kinds)
+            _check(_on_gpu(z, u, 10, s), z, u, 10, s)
+
+
+def test_graph_replay_other_streams_and_concurrent_calls():
+    z, u, s = _rows(30, 50257, torch.bfloat16, seed=8).to(DEV), _uniform(30, 8).to(DEV), _settings(30, 8, "tkp")
+    s = {n: v.to(DEV) for n, v in s.items()}
+    ref = dppo.dppo_sample(z, u, K=8, **s)
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = dppo.dppo_sample(z, u, K=8, status=st, **s)
+    for _ in range(2):
+        g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(out[n], ref[n]) for n in ("sampled_ids", "mu_logp", "mu_topk_ids", "mu_topk_p"))
+    u2 = _uniform(30, 9)
+    u.copy_(u2)
+    g.replay()
+    torch.cuda.synchronize()
+    _check(out, z.cpu(), u2, 8, {n: v.cpu() for n, v in s.items()})
+    ref = {n: v.clone() for n, v in out.items()}
+    side = [torch.cuda.Stream() for _ in range(2)]
+    outs = []
+    for q in side:
+        q.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(q):
+            outs += [dppo.dppo_sample(z, u, K=8, **s) for _ in range(5)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(o[n], ref[n]) for o in outs for n in ("sampled_ids", "mu_logp", "mu_topk_ids", "mu_topk_p"))
+
+
+@pytest.mark.parametrize("K", [20])
+def test_the_record_feeds_the_loss(K):
+    """Sampled, then evaluated under the same logits: ratio 1, no divergence beyond fp32, nothing masked, for every variant that
+    reads the record."""
+    z, u, adv = _rows(64, 32000, torch.bfloat16, seed=1).to(DEV), _uniform(64, 1).to(DEV), torch.ones(64, device=DEV)
+    o = dppo.dppo_sample(z, u, K=K)
+    for variant in (dppo.BINARY_TV, dppo.BINARY_KL, dppo.TOPK_TV, dppo.TOPK_KL):
+        r = dppo.dppo_loss_fwd_bwd(z, o["sampled_ids"], o["mu_logp"], adv, None, variant, K, 1e-4, o["mu_topk_ids"], o["mu_topk_p"], want_stats=True)
+        torch.cuda.synchronize()
+        assert int(r["status"].item()) == 0 and bool(r["mask"].all()) and float(r["divergence"].abs().max()) <= 1e-5
+        assert abs(float(r["loss"].item()) + 1.0) <= 1e-5                      # -mean(r A) with r = 1, A = 1
