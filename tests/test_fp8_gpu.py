@@ -195,6 +195,19 @@ def test_product_with_more_tiles_than_sms_and_strided_everything():
         assert bool((wc[:M, N:] == -3).all()) and bool((wc[M] == -3).all())
 
 
+@pytest.mark.parametrize("cta_group", [1, 2])
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (61, 1000, 700), (257, 700, 300), (600, 513, 2048), (2000, 20000, 130)])
+@pytest.mark.parametrize("b_br", [1, 128])
+def test_product_on_single_sms_and_on_pairs(cta_group, M, N, K, b_br):
+    A, sa = _operand(M, K, "e4m3", 1, seed=M)
+    B, sb = _operand(N, K, "e4m3", b_br, seed=N)
+    for out in (torch.float32, torch.bfloat16):
+        C, status = dppo.dppo_gemm_tn_fp8(A, sa, B, sb, 1, b_br, out, cta_group=cta_group)
+        torch.cuda.synchronize()
+        assert int(status.item()) == 0
+        _check_product(C, A, sa, 1, B, sb, b_br)
+
+
 def test_product_over_an_empty_sum_and_of_nothing():
     sa, sb = torch.empty((5, 0), device=DEV), torch.empty((1, 0), device=DEV)
     A, B = (torch.empty((n, 0), dtype=torch.float8_e4m3fn, device=DEV) for n in (5, 7))
@@ -216,13 +229,14 @@ def test_nan_blocks_reach_only_their_rows():
     assert bool(C[131].isnan().all()) and int(C.isnan().sum()) == 260
 
 
-def test_product_gives_up_and_the_next_call_is_fine():
+@pytest.mark.parametrize("cta_group", [1, 2])
+def test_product_gives_up_and_the_next_call_is_fine(cta_group):
     A, sa = _operand(300, 500, "e4m3", 1, seed=3)
     B, sb = _operand(520, 500, "e4m3", 128, seed=4)
-    C, status = dppo.dppo_gemm_tn_fp8(A, sa, B, sb, wait_limit_us=20000, test_inject=binding.INJECT_NO_COPIES)
+    C, status = dppo.dppo_gemm_tn_fp8(A, sa, B, sb, cta_group=cta_group, wait_limit_us=20000, test_inject=binding.INJECT_NO_COPIES)
     torch.cuda.synchronize()
     assert int(status.item()) & binding.STATUS_WAIT_LIMIT
-    C, status = dppo.dppo_gemm_tn_fp8(A, sa, B, sb, wait_limit_us=20000)
+    C, status = dppo.dppo_gemm_tn_fp8(A, sa, B, sb, cta_group=cta_group, wait_limit_us=20000)
     torch.cuda.synchronize()
     assert int(status.item()) == 0
     _check_product(C, A, sa, 1, B, sb, 128)
