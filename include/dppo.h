@@ -391,8 +391,7 @@ int dppo_fp8_quantize(const void* x, int64_t rows, int64_t cols, int64_t x_row_s
  *  a_scale     scale of row (block) i and K block k at a_scale[i * a_scale_row_stride + k * a_scale_k_stride]; b_scale alike.
  *              With row stride 1 the kernel reads them in whole lines.
  *  C           [M, N], c_dtype DPPO_F32 or DPPO_BF16 (rounded once, from the fp32 sum), row stride ldc elements (>= N).
- *  K = 0 gives C = 0.  status: device word, DPPO_STATUS_WAIT_LIMIT (may be NULL).  opts: wait_limit_us, test_inject,
- *  gemm_cta_group (2: tiles of 256 x 256 on pairs of SMs, 1: 128 x 128 on single ones, 0: by the shape).
+ *  K = 0 gives C = 0.  status: device word, DPPO_STATUS_WAIT_LIMIT (may be NULL).  opts: wait_limit_us, test_inject.
  */
 int dppo_gemm_tn_fp8(const void* A, int64_t lda, int a_format, int a_block_rows, const float* a_scale,
                      int64_t a_scale_row_stride, int64_t a_scale_k_stride,

@@ -446,10 +446,10 @@ def dppo_fp8_quantize(x, dtype=torch.float8_e4m3fn, block_rows=1, rowwise=True, 
 
 
 def dppo_gemm_tn_fp8(A, a_scale, B, b_scale, a_block_rows=1, b_block_rows=128, out_dtype=torch.float32, C=None, status=None, stream=None,
-                     cta_group=0, wait_limit_us=0, test_inject=0):
+                     wait_limit_us=0, test_inject=0):
     """C[M,N] = A[M,K] . B[N,K]^T for 8-bit CUDA matrices (torch.float8_e4m3fn / torch.float8_e5m2, last dimension contiguous, rows on
     16-byte boundaries) with fp32 scales [row blocks, ceil(K/128)] of any strides.  ``a_block_rows`` / ``b_block_rows``: rows that
-    share a scale, 1 or 128.  ``cta_group``: gemm_cta_group of dppo_opts.  Returns (C, status), C fp32 or bf16; nothing is synchronised."""
+    share a scale, 1 or 128.  Returns (C, status), C fp32 or bf16; nothing is synchronised."""
     assert A.is_cuda and B.is_cuda and A.dtype in FP8_FORMATS and B.dtype in FP8_FORMATS and A.dim() == 2 and B.dim() == 2
     M, K = A.shape
     N = B.shape[0]
@@ -468,8 +468,7 @@ def dppo_gemm_tn_fp8(A, a_scale, B, b_scale, a_block_rows=1, b_block_rows=128, o
                                     a_scale.stride(0), a_scale.stride(1), _ptr(B), B.stride(0) if N > 1 else up16, FP8_FORMATS[B.dtype],
                                     int(b_block_rows), _ptr(b_scale), b_scale.stride(0), b_scale.stride(1), M, N, K, _ptr(C), _dtype_code(C),
                                     C.stride(0) if M > 1 else N, _ptr(status),
-                                    ctypes.byref(_opts(cta_group=cta_group, wait_limit_us=wait_limit_us, test_inject=test_inject)),
-                                    c_void_p(st.cuda_stream))
+                                    ctypes.byref(_opts(wait_limit_us=wait_limit_us, test_inject=test_inject)), c_void_p(st.cuda_stream))
     if rc != 0:
         raise DppoError(rc, "dppo_gemm_tn_fp8")
     return C, status

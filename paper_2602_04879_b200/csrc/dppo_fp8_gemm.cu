@@ -7,23 +7,24 @@
 // promotion warps read each P_kb back (tcgen05.ld), scale it and add it to fp32 sums in their registers, while the tensor cores
 // work on the next block in the other half of tensor memory.
 //
-// Persistent CTAs, one per SM:
-//   warp 0       TMA producer: boxes of 128 bytes along K, 128-byte swizzle, 4 stages; with each stage the scales of the tile's rows
-//                (and of its columns, if each has its own) for that K block, into a ring of 8
+// Persistent CTAs, one per SM, tiles of 128 x w (w = 256 or 128, chosen per call):
+//   warp 0       producer: TMA boxes of 128 bytes along K, 128-byte swizzle, 3 stages; with each stage the scales of the tile's rows and
+//                columns for that K block by 4-byte asynchronous copies (any strides) into a ring of 8
 //   warp 1       allocates tensor memory (two P_kb buffers) and issues the MMAs
 //   warps 2, 3   stand between the mbarriers and the promotion warps: warp 3 waits for a finished P_kb and lets them go, warp 2 hears
 //                that they have read it and frees the buffer.  Promotion warps see only named barriers, which cost them a few
 //                cycles where polling, and arriving on, an mbarrier cost a few hundred
-//   warps 4-11   promotion: a warp owns 32 rows (its quarter of the tensor-memory lanes) and half of the tile's columns, its
-//                fp32 sums in registers (setmaxnreg moves registers from warps 0-3 to these); finished tiles leave through shared
-//                memory and bulk tensor stores
-// CG = 2: pairs of CTAs (a cluster of two SMs, tcgen05 cta_group::2) on tiles of 256 x 192, each CTA staging its 128 rows of A
-// and half of the tile's rows of B and promoting its own 128 x 192 sums (96 per thread: a promotion warp then has registers for
-// all of its columns of a P_kb at once, reads them in one go and frees the buffer before it adds them up).  CG = 1: single CTAs on tiles of 128 x 128.
-// Every wait is bounded.
+//   warps 4-11   promotion: a warp owns 32 rows (its quarter of the tensor-memory lanes) and 128 of the columns, its fp32 sums in
+//                registers (setmaxnreg moves registers from warps 0-3 to these); finished tiles leave through shared memory and
+//                bulk tensor stores
+// With few tiles and a long K a cluster of S CTAs shares a tile: each sums S-th part of the K blocks, leaves its sums in its shared
+// memory, and all add up a part of the rows each, CTA after CTA (a fixed order), through distributed shared memory.
+// Every wait is bounded (dppo_pipe.cuh).
 //
-// What bounds it is the hand-over of the P_kb buffers (MMA done -> sums read -> buffer free), two of which are in flight: scales have no
-// barrier of their own (the MMA waited for them along with the operands), and the arrival that frees a buffer is relaxed.
+// What bounds it is the hand-over of the P_kb buffers (MMA done -> sums read -> buffer free), two of which are in flight, and the
+// fp32 additions themselves (256 of the 512 cycles that the MMAs of a block take at their nominal rate).  Scales have no barrier of
+// their own: the MMA waits for them along with the operands.
+#include <cooperative_groups.h>
 #include <mutex>
 
 #include "dppo_common.cuh"
@@ -34,34 +35,28 @@ namespace {
 
 namespace f8 {
 
-constexpr int BM = 128, BK = 128;
+constexpr int BM = 128, BN = 256, BK = 128;                // BN: the widest tile
+constexpr int COLS = 128;                                  // columns of a promotion warp
 constexpr int THREADS = 384, PROMO_WARPS = 8;
-constexpr int SRING = 8;
+constexpr int STAGES = 3, SRING = 8, SCALES = BM + BN;
+constexpr int A_BYTES = BM * BK, STAGE_BYTES = (BM + BN) * BK;
+constexpr int OUT_BYTES = PROMO_WARPS * 8192;              // two blocks of 32 rows x 128 bytes per promotion warp
+constexpr int PART_PITCH = BN + 4;                         // floats; a CTA's sums of a shared tile, in the stages' memory
+constexpr int MAX_SPLIT = 8;
+constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + OUT_BYTES + SRING * SCALES * 4 + 512 + 1024;
+static_assert(BM * PART_PITCH * 4 <= STAGES * STAGE_BYTES, "partial tile");
 // 384 threads x 168 registers at launch = 64512 = 128 x 72 + 256 x 216
 constexpr int REGS_LOW = 72, REGS_HIGH = 216;
 static_assert(128 * REGS_LOW + 32 * PROMO_WARPS * REGS_HIGH <= THREADS * 168, "register split");
 
-template <int CG> struct Cfg {
-  static constexpr int TILE_M = BM * CG, BN = 256;
-  static constexpr int B_ROWS = BN / CG;                    // rows of B that one CTA stages
-  static constexpr int COLS = 128;                          // columns of a promotion warp
-  static constexpr int A_BYTES = BM * BK, B_BYTES = B_ROWS * BK, STAGE_BYTES = A_BYTES + B_BYTES;
-  static constexpr int STAGES = CG == 2 ? 5 : 3;
-  static constexpr int OUT_BYTES = PROMO_WARPS * 4096;      // 32 rows x 32 columns per promotion warp (two such blocks for bf16)
-  static constexpr int SCALES = BM + BN;
-  static constexpr int TMEM_BUF = 256, TMEM_COLS = 2 * TMEM_BUF;      // columns between / of the two buffers (a power of two)
-  static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + OUT_BYTES + SRING * SCALES * 4 + 512 + 1024;
-};
-
 struct Params {
-  int M, N, K;
-  int a_shift;                       // log2 of the rows of A that share a scale (0 or 7)
+  int M, N, bn, split;               // bn: columns of a tile; split: CTAs that share a tile
+  int a_shift;                       // log2 of the rows of A that share a scale (0 or 7; B: the template argument)
   const float* sa;
   int64_t sa_row, sa_k;
   const float* sb;
   int64_t sb_row, sb_k;
   int kblocks;
-  int a_tma, b_tma;                  // the scales of the rows of A / B come with the operands (map_sa / map_sb)
   void* C;
   int64_t ldc;
   int c_bf16, c_vec, tma_store;      // c_vec: 16-byte stores allowed; tma_store: map_c describes C
@@ -71,36 +66,50 @@ struct Params {
   int inject;
 };
 
-template <int CG>
 __device__ __forceinline__ void mma_f8(uint32_t tmem_c, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
-  if (CG == 2)
-    asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n"
-        ::"r"(tmem_c), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
-  else
-    asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n"
-        ::"r"(tmem_c), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
-}
-template <int CG> __device__ __forceinline__ void commit(uint32_t bar) {
-  if (CG == 2) gemm::mma_commit_pair(bar); else gemm::mma_commit(bar);
-}
-// N columns of this warp's lanes, all on their way before the first is waited for
-template <int N> __device__ __forceinline__ void read_columns(uint32_t taddr, uint32_t* r);
-template <> __device__ __forceinline__ void read_columns<64>(uint32_t taddr, uint32_t* r) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%64];\n"
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%65];\n"
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n"
+      ::"r"(tmem_c), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// 64 columns of this warp's 32 lanes: r[j] is column j of the thread's row
+__device__ __forceinline__ void read_rows(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
+      "%24,%25,%26,%27,%28,%29,%30,%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,"
+      "%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];\n"
       "tcgen05.wait::ld.sync.aligned;\n"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
-        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
-        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
-        "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]),
-        "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]), "=r"(r[50]),
-        "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]),
-        "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
-      : "r"(taddr + 0), "r"(taddr + 32)
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
+        "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
+        "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
+        "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
+        "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+      : "r"(taddr)
       : "memory");
+}
+// 64 columns of 16 lanes in the layout of a matrix-instruction accumulator: r[4 g], r[4 g + 1] are columns 8 g + 2 (lane % 4), + 1 of row
+// lane / 4, r[4 g + 2], r[4 g + 3] those of row lane / 4 + 8
+__device__ __forceinline__ void read_fragment(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
+      "%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
+      "tcgen05.wait::ld.sync.aligned;\n"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+// 4-byte asynchronous copy of base[at]; zero when not `valid`
+__device__ __forceinline__ void cp_async4(uint32_t dst, const float* base, int64_t at, bool valid) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(valid ? base + at : base), "r"(valid ? 4 : 0) : "memory");
+}
+// this thread's arrival on the barrier once its copies so far have landed
+__device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ uint32_t elect_one() {
   uint32_t p;
@@ -122,170 +131,169 @@ __device__ __forceinline__ void empty_sync(uint32_t b) {
 __device__ __forceinline__ void empty_arrive(uint32_t b) {
   if (b) asm volatile("barrier.cta.arrive 6, %0;" ::"n"(BAR_THREADS) : "memory"); else asm volatile("barrier.cta.arrive 5, %0;" ::"n"(BAR_THREADS) : "memory");
 }
-// Arrivals that order none of this thread's memory accesses: what they hand over is a tensor-memory buffer that has been read
-// (tcgen05.fence orders that), not shared memory.  A release would wait for the thread's loads of the coming scales, and at cluster
-// scope for much more: the tensor cores waited 1000 and 2000 cycles a block for it.
-__device__ __forceinline__ void arrive_relaxed(uint32_t bar) {
-  asm volatile("mbarrier.arrive.relaxed.cta.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void arrive_relaxed_cluster(uint32_t cluster_bar) {
-  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
-}
 __device__ __forceinline__ void st128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
+__device__ __forceinline__ void st64(uint32_t addr, float2 v) {
+  asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(addr), "f"(v.x), "f"(v.y) : "memory");
+}
+__device__ __forceinline__ void st32(uint32_t addr, uint32_t v) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
 __device__ __forceinline__ uint32_t bf16x2(float2 v) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(v.x, v.y);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// acc[0, 16) += s * r (* the column's scale): 32 columns of one row, packed fp32 pairs
-template <bool B_ROW_SCALES>
-__device__ __forceinline__ void promote32(float2* acc, const uint32_t* r, float s, const float* sb) {
+// acc += s * r: 64 columns of one row, packed fp32 pairs
+__device__ __forceinline__ void promote_rows(float2* acc, const uint32_t* r, float s) {
   const float2 s2 = make_float2(s, s);
 #pragma unroll
-  for (int j = 0; j < 32; j += 4) {
-    float2 u = make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1])), v = make_float2(__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3]));
-    if (B_ROW_SCALES) {
-      const float4 w = *reinterpret_cast<const float4*>(sb + j);
-      u = __fmul2_rn(u, make_float2(w.x, w.y));
-      v = __fmul2_rn(v, make_float2(w.z, w.w));
-    }
-    acc[j / 2] = __ffma2_rn(u, s2, acc[j / 2]);
-    acc[j / 2 + 1] = __ffma2_rn(v, s2, acc[j / 2 + 1]);
+  for (int j = 0; j < 32; ++j) acc[j] = __ffma2_rn(make_float2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1])), s2, acc[j]);
+}
+// acc += s0, s1 (the two rows) * sb (the columns') * r: a fragment of 16 rows x 64 columns.  The thread needs only every fourth pair
+// of the column scales: read by one row per thread, each warp would fetch all 128 of them for every block, and the shared
+// memory's 128 bytes a cycle would be what bounds the kernel.
+__device__ __forceinline__ void promote_fragment(float2* acc, const uint32_t* r, float s0, float s1, const float* sb) {
+  const float2 a0 = make_float2(s0, s0), a1 = make_float2(s1, s1);
+#pragma unroll
+  for (int g = 0; g < 8; ++g) {
+    const float2 w = *reinterpret_cast<const float2*>(sb + 8 * g);
+    const float2 u = __fmul2_rn(make_float2(__uint_as_float(r[4 * g]), __uint_as_float(r[4 * g + 1])), w);
+    const float2 v = __fmul2_rn(make_float2(__uint_as_float(r[4 * g + 2]), __uint_as_float(r[4 * g + 3])), w);
+    acc[2 * g] = __ffma2_rn(u, a0, acc[2 * g]);
+    acc[2 * g + 1] = __ffma2_rn(v, a1, acc[2 * g + 1]);
   }
 }
 
-template <int CG, bool B_ROW_SCALES>       // B_ROW_SCALES: b_block_rows = 1
+template <bool B_ROW_SCALES>       // b_block_rows = 1
 __global__ void __launch_bounds__(THREADS, 1) gemm_tn_fp8_kernel(const __grid_constant__ CUtensorMap map_a,
                                                                  const __grid_constant__ CUtensorMap map_b,
-                                                                 const __grid_constant__ CUtensorMap map_c,
-                                                                 const __grid_constant__ CUtensorMap map_sa,
-                                                                 const __grid_constant__ CUtensorMap map_sb, Params p) {
-  using C = Cfg<CG>;
-  constexpr int STAGES = C::STAGES, STAGE_BYTES = C::STAGE_BYTES, BN = C::BN, COLS = C::COLS;
+                                                                 const __grid_constant__ CUtensorMap map_c, Params p) {
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   unsigned char* out_stage = smem + STAGES * STAGE_BYTES;
-  float* sring = reinterpret_cast<float*>(out_stage + C::OUT_BYTES);
-  unsigned long long* bars = reinterpret_cast<unsigned long long*>(sring + SRING * C::SCALES);
-  const uint32_t full0 = smem_u32(bars), done0 = smem_u32(bars + STAGES);
-  const uint32_t tempty0 = smem_u32(bars + 2 * STAGES);
+  float* sring = reinterpret_cast<float*>(out_stage + OUT_BYTES);
+  unsigned long long* bars = reinterpret_cast<unsigned long long*>(sring + SRING * SCALES);
+  const uint32_t full0 = smem_u32(bars), done0 = smem_u32(bars + STAGES), tempty0 = smem_u32(bars + 2 * STAGES);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 2);
   const WaitCtl wc{reinterpret_cast<volatile int*>(tmem_slot + 1), p.wait_ns};
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t rank = (CG == 2) ? cluster_ctarank() : 0u;       // 0: leader of the pair
-  const int group = (int)blockIdx.x / CG, ngroups = (int)gridDim.x / CG;
+  const int rank = p.split > 1 ? (int)cluster_ctarank() : 0;
+  const int group = (int)blockIdx.x / p.split, ngroups = (int)gridDim.x / p.split;
 
   if (tid == 0) {
-    for (int i = 0; i < STAGES; ++i) { mbar_init(full0 + 8 * i, 1); mbar_init(done0 + 8 * i, 1); }
-    for (int i = 0; i < 2; ++i) mbar_init(tempty0 + 8 * i, CG);
+    for (int i = 0; i < STAGES; ++i) { mbar_init(full0 + 8 * i, 1 + 32); mbar_init(done0 + 8 * i, 1); }
+    for (int i = 0; i < 2; ++i) mbar_init(tempty0 + 8 * i, 1);
     *wc.flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   if (warp == 1) {
-    if (CG == 2) {
-      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(C::TMEM_COLS) : "memory");
-      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-    } else {
-      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(C::TMEM_COLS) : "memory");
-      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(2 * BN) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
-  if (CG == 2) cluster_sync_all();      // the peer's barriers exist before anything is sent to them
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem_base = *tmem_slot;
 
-  const int tiles_m = (p.M + C::TILE_M - 1) / C::TILE_M, tiles_n = (p.N + BN - 1) / BN;
-  const int64_t ntiles = (int64_t)tiles_m * tiles_n;
-  const int kblocks = p.kblocks;
+  const int bn = p.bn, tiles_m = (p.M + BM - 1) / BM, tiles_n = (p.N + bn - 1) / bn;
+  const int ntiles = tiles_m * tiles_n;
+  const int per = (p.kblocks + p.split - 1) / p.split, kb_first = min(p.kblocks, rank * per);
+  const int kblocks = min(p.kblocks, kb_first + per) - kb_first;      // this CTA's K blocks of each tile
   const uint32_t smem_base = smem_u32(smem);
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_LOW));
     if (warp == 0) {
-      // ---------------------------------------------------------------- TMA producer (of this CTA's operand slices)
-      if (lane == 0 && !(p.inject & DPPO_INJECT_NO_COPIES)) {
-        constexpr uint32_t kSlot = C::SCALES * 4;
-        const uint32_t bytes = STAGE_BYTES + (p.a_tma ? BM * 4 : 0) + (B_ROW_SCALES && p.b_tma ? BN * 4 : 0), ring = smem_u32(sring);
+      // ---------------------------------------------------------------- producer
+      if (!(p.inject & DPPO_INJECT_NO_COPIES)) {
+        const uint32_t bytes = A_BYTES + bn * BK, ring = smem_u32(sring);
         int s = 0;
         uint32_t ph = 0, it = 0;
         bool ok = true;
-        for (int64_t tile = group; tile < ntiles && ok; tile += ngroups) {
-          const int m0 = (int)(tile % tiles_m) * C::TILE_M + (int)rank * BM, n0 = (int)(tile / tiles_m) * BN;
-          for (int kb = 0; kb < kblocks; ++kb, ++it) {
-            if (!mbar_wait(done0 + 8 * s, ph ^ 1u, wc)) { ok = false; break; }
-            const uint32_t a_dst = smem_base + s * STAGE_BYTES, b_dst = a_dst + C::A_BYTES;
-            // The slot's last scales were those of 8 K blocks ago.  A stage is free once the MMAs of 4 blocks ago are done, and
-            // those began after every promotion warp had read the block 2 before them: nobody reads the slot any more.
-            const uint32_t sc_dst = ring + (it % SRING) * kSlot;
-            if (CG == 2) {       // both CTAs' bytes are counted on the leader's barrier
-              const uint32_t bar = map_to_cta(full0 + 8 * s, 0);
-              if (rank == 0) mbar_arrive_expect_tx(full0 + 8 * s, 2 * bytes);
-              gemm::tma_load_2d_pair(a_dst, &map_a, kb * BK, m0, bar);
-              gemm::tma_load_2d_pair(b_dst, &map_b, kb * BK, n0 + (int)rank * C::B_ROWS, bar);
-              if (p.a_tma) gemm::tma_load_2d_pair(sc_dst, &map_sa, m0, kb, bar);
-              if (B_ROW_SCALES && p.b_tma) gemm::tma_load_2d_pair(sc_dst + BM * 4, &map_sb, n0, kb, bar);
-            } else {
-              mbar_arrive_expect_tx(full0 + 8 * s, bytes);
-              gemm::tma_load_2d(a_dst, &map_a, kb * BK, m0, full0 + 8 * s);
-              gemm::tma_load_2d(b_dst, &map_b, kb * BK, n0, full0 + 8 * s);
-              if (p.a_tma) gemm::tma_load_2d(sc_dst, &map_sa, m0, kb, full0 + 8 * s);
-              if (B_ROW_SCALES && p.b_tma) gemm::tma_load_2d(sc_dst + BM * 4, &map_sb, n0, kb, full0 + 8 * s);
+        for (int tile = group; tile < ntiles && ok; tile += ngroups) {
+          const int m0 = (tile % tiles_m) * BM, n0 = (tile / tiles_m) * bn;
+          const float* sa = p.sa + (int64_t)(m0 >> p.a_shift) * p.sa_row + kb_first * p.sa_k;
+          const float* sb = p.sb + (int64_t)(B_ROW_SCALES ? n0 : n0 >> 7) * p.sb_row + kb_first * p.sb_k;
+          for (int kb = kb_first; kb < kb_first + kblocks; ++kb, ++it) {
+            if (!mbar_wait_warp(done0 + 8 * s, ph ^ 1u, wc)) { ok = false; break; }
+            const uint32_t a_dst = smem_base + s * STAGE_BYTES, bar = full0 + 8 * s;
+            if (lane == 0) {
+              mbar_arrive_expect_tx(bar, bytes);
+              gemm::tma_load_2d(a_dst, &map_a, kb * BK, m0, bar);
+              gemm::tma_load_2d(a_dst + A_BYTES, &map_b, kb * BK, n0, bar);
             }
+            // The slot's last scales were those of 8 K blocks ago.  A stage is free once the MMAs of 3 blocks ago are done, and
+            // those began after every promotion warp had read the block 2 before them: nobody reads the slot any more.
+            const uint32_t sc = ring + (it % SRING) * (SCALES * 4);
+            if (!p.a_shift) {
+#pragma unroll
+              for (int j = 0; j < BM; j += 32) cp_async4(sc + 4 * (j + lane), sa, (int64_t)(j + lane) * p.sa_row, m0 + j + lane < p.M);
+            } else if (lane == 0) {
+              cp_async4(sc, sa, 0, true);
+            }
+            if (B_ROW_SCALES) {
+#pragma unroll
+              for (int j = 0; j < BN; j += 32) cp_async4(sc + 4 * (BM + j + lane), sb, (int64_t)(j + lane) * p.sb_row, n0 + j + lane < p.N);
+            } else if (lane < 2) {
+              cp_async4(sc + 4 * (BM + lane), sb, lane * p.sb_row, n0 + lane * 128 < p.N);
+            }
+            cp_async_arrive(bar);
+            sa += p.sa_k;
+            sb += p.sb_k;
             if (++s == STAGES) { s = 0; ph ^= 1u; }
           }
         }
       }
     } else if (warp == 1) {
-      // ---------------------------------------------------------------- MMA issuer (in a pair: the leader's only)
+      // ---------------------------------------------------------------- MMA issuer
       // (the whole warp runs the loop, so that descriptors and addresses are warp-uniform values for the compiler, and one elected
       // lane issues: with a single lane in the loop each MMA took three times as long to issue)
-      if (rank == 0) {
-        const uint32_t idesc = p.formats | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(C::TILE_M >> 4) << 24);
-        const uint64_t adesc0 = gemm::make_desc_k_sw128(smem_base), bdesc0 = gemm::make_desc_k_sw128(smem_base + C::A_BYTES);
-        int s = 0;
-        uint32_t ph = 0, it = 0;
-        bool ok = true;
-        for (int64_t tile = group; tile < ntiles && ok; tile += ngroups) {
-          for (int kb = 0; kb < kblocks; ++kb, ++it) {
-            const uint32_t b = it & 1u, use = it >> 1;
-            ok = mbar_wait(tempty0 + 8 * b, (use & 1u) ^ 1u, wc) && mbar_wait(full0 + 8 * s, ph, wc);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint64_t adesc = adesc0 + (uint64_t)(s * (STAGE_BYTES >> 4)), bdesc = bdesc0 + (uint64_t)(s * (STAGE_BYTES >> 4));
-            if (elect_one()) {
+      const uint32_t idesc = p.formats | ((uint32_t)(bn >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
+      const uint64_t adesc0 = gemm::make_desc_k_sw128(smem_base), bdesc0 = gemm::make_desc_k_sw128(smem_base + A_BYTES);
+      int s = 0;
+      uint32_t ph = 0, it = 0;
+      bool ok = true;
+      for (int tile = group; tile < ntiles && ok; tile += ngroups) {
+        for (int kb = 0; kb < kblocks; ++kb, ++it) {
+          const uint32_t b = it & 1u, use = it >> 1;
+          ok = mbar_wait(tempty0 + 8 * b, (use & 1u) ^ 1u, wc) && mbar_wait(full0 + 8 * s, ph, wc);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint64_t adesc = adesc0 + (uint64_t)(s * (STAGE_BYTES >> 4)), bdesc = bdesc0 + (uint64_t)(s * (STAGE_BYTES >> 4));
+          if (elect_one()) {
 #pragma unroll
-              for (int k = 0; k < BK / 32; ++k)      // 32 elements = 32 bytes along K inside the swizzle atom
-                mma_f8<CG>(tmem_base + b * C::TMEM_BUF, adesc + (uint64_t)(k * 2), bdesc + (uint64_t)(k * 2), idesc, k != 0);
-              commit<CG>(done0 + 8 * s);             // the stage may be filled again, and P_kb is complete
-            }
-            __syncwarp();
-            if (++s == STAGES) { s = 0; ph ^= 1u; }
+            for (int k = 0; k < BK / 32; ++k)        // 32 elements = 32 bytes along K inside the swizzle atom
+              mma_f8(tmem_base + b * BN, adesc + (uint64_t)(k * 2), bdesc + (uint64_t)(k * 2), idesc, k != 0);
+            gemm::mma_commit(done0 + 8 * s);         // the stage may be filled again, and P_kb is complete
           }
+          __syncwarp();
+          if (++s == STAGES) { s = 0; ph ^= 1u; }
         }
       }
     } else {
-      // ---------------------------------------------------------------- helpers.  They serve every K block even after a wait ran
-      // out (mbar_wait then returns at once), so that no one is left at a named barrier.
-      const uint32_t tempty = CG == 2 ? map_to_cta(tempty0, 0) : tempty0;
+      // ---------------------------------------------------------------- helpers.  They serve every K block even after a wait ran out
+      // (then without waiting for the tensor cores), so that no one is left at a named barrier.  Warp 3 may not arrive for a
+      // block before the buffer's previous block has been read, or its arrival would count for that one.  A finished block
+      // implies that; after an abort it waits for the buffer itself, which the promotion warps and warp 2 free without fail:
+      // they only ever wait for warp 3.
       int s = 0;
       uint32_t it = 0, ph = 0;
-      for (int64_t tile = group; tile < ntiles; tile += ngroups) {
+      for (int tile = group; tile < ntiles; tile += ngroups) {
         for (int kb = 0; kb < kblocks; ++kb, ++it) {
           const uint32_t b = it & 1u;
           if (warp == 3) {
-            if (!wc.aborted()) mbar_wait(done0 + 8 * s, ph, wc);
+            if (wc.aborted() || !mbar_wait(done0 + 8 * s, ph, wc)) {
+#pragma unroll 1
+              for (int i = 0; i < (1 << 24) && !mbar_try_wait(tempty0 + 8 * b, ((it >> 1) & 1u) ^ 1u); ++i) {}
+            }
             __syncwarp();
             if (++s == STAGES) { s = 0; ph ^= 1u; }
             full_arrive(b);
           } else {
             empty_sync(b);
-            if (lane == 0) { if (CG == 2) arrive_relaxed_cluster(tempty + 8 * b); else arrive_relaxed(tempty + 8 * b); }
+            if (lane == 0) mbar_arrive(tempty0 + 8 * b);
           }
         }
       }
@@ -294,102 +302,149 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tn_fp8_kernel(const __grid_co
     // ------------------------------------------------------------------ promotion
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_HIGH));
     const int q = warp & 3, part = (warp - 4) >> 2;
-    const uint32_t wbuf = smem_u32(out_stage) + (uint32_t)(warp - 4) * 4096u;
-    const bool a_direct = !p.a_shift && !p.a_tma, b_direct = B_ROW_SCALES && !p.b_tma;
-    uint32_t it = 0, out_it = 0;
-    for (int64_t tile = group; tile < ntiles; tile += ngroups) {
-      const int m0 = (int)(tile % tiles_m) * C::TILE_M + (int)rank * BM + q * 32, n0 = (int)(tile / tiles_m) * BN + part * COLS;
-      const bool live = m0 < p.M && n0 < p.N;        // this warp's part of the tile meets C (what it adds up otherwise is not stored)
+    const uint32_t wbuf = smem_u32(out_stage) + (uint32_t)(warp - 4) * 8192u;
+    uint32_t it = 0;
+    for (int tile = group; tile < ntiles; tile += ngroups) {
+      const int m0 = (tile % tiles_m) * BM + q * 32, n0 = (tile / tiles_m) * bn + part * COLS;
+      const int n_end = min(p.N, n0 - part * COLS + bn);             // the tile's columns end here
+      const bool live = m0 < p.M && n0 < n_end;      // this warp's part of the tile meets C (what it adds up otherwise is not stored)
       float2 acc[COLS / 2];
 #pragma unroll
       for (int j = 0; j < COLS / 2; ++j) acc[j] = make_float2(0.f, 0.f);
-      // scales that all rows (columns) of this warp share: lane i keeps the one of K block kb0 + i
-      for (int kb0 = 0; kb0 < kblocks; kb0 += 32) {
-        float shared_s = 1.f;
-        if (live && kb0 + lane < kblocks) {
-          if (p.a_shift) shared_s = p.sa[(int64_t)(m0 >> 7) * p.sa_row + (kb0 + lane) * p.sa_k];
-          if (!B_ROW_SCALES) shared_s *= p.sb[(int64_t)(n0 >> 7) * p.sb_row + (kb0 + lane) * p.sb_k];
-        }
-        const int kn = min(32, kblocks - kb0);
-        float s = __shfl_sync(0xffffffffu, shared_s, 0);
 #pragma unroll 1
-        for (int i = 0; i < kn; ++i, ++it) {
-          const uint32_t b = it & 1u;
-          float* sc = sring + (it % SRING) * C::SCALES;
-          float* sbv = sc + BM + part * COLS;
-          full_sync(b);
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const float sa = p.a_tma ? sc[q * 32 + lane] : 1.f;
-          const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + b * C::TMEM_BUF + part * COLS;
-          uint32_t r[64];
-          read_columns<64>(taddr, r);
-          s *= sa;
-          if (a_direct && m0 + lane < p.M) s *= p.sa[(int64_t)(m0 + lane) * p.sa_row + (kb0 + i) * p.sa_k];
-          if (b_direct) {                            // column scales of a layout that no tensor map describes: one by one, a part each
-            for (int j = q * 32 + lane; j < COLS; j += 128) sbv[j] = n0 + j < p.N ? p.sb[(int64_t)(n0 + j) * p.sb_row + (kb0 + i) * p.sb_k] : 0.f;
-            bar_sync(7 + part, 128);
-          }
-          promote32<B_ROW_SCALES>(acc, r, s, sbv);
-          promote32<B_ROW_SCALES>(acc + 16, r + 32, s, sbv + 32);
-          read_columns<64>(taddr + 64, r);
+      for (int kb = 0; kb < kblocks; ++kb, ++it) {
+        const uint32_t b = it & 1u, taddr = tmem_base + ((uint32_t)(q * 32) << 16) + b * BN + part * COLS;
+        const float* sc = sring + (it % SRING) * SCALES;
+        uint32_t r[64];
+        full_sync(b);
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (B_ROW_SCALES) {
+          const float* sv = sc + BM + part * COLS + 2 * (lane & 3);
+          const float* sr = sc + (p.a_shift ? 0 : q * 32 + (lane >> 2));
+          const int r8 = p.a_shift ? 0 : 8;
+          const float s0 = sr[0], s1 = sr[r8];
+          read_fragment(taddr, r);
+          promote_fragment(acc, r, s0, s1, sv);
+          read_fragment(taddr + 64, r);
+          promote_fragment(acc + 16, r, s0, s1, sv + 64);
+          const float s2 = sr[2 * r8], s3 = sr[3 * r8];
+          read_fragment(taddr + (16u << 16), r);
+          promote_fragment(acc + 32, r, s2, s3, sv);
+          read_fragment(taddr + 64 + (16u << 16), r);
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           empty_arrive(b);                           // buffer read
-          const float s_next = __shfl_sync(0xffffffffu, shared_s, (i + 1) & 31);
-          promote32<B_ROW_SCALES>(acc + 32, r, s, sbv + 64);
-          promote32<B_ROW_SCALES>(acc + 48, r + 32, s, sbv + 96);
-          s = s_next;
-          if (b_direct) bar_sync(7 + part, 128);     // before the slot's scales are written again
+          promote_fragment(acc + 48, r, s2, s3, sv + 64);
+        } else {
+          const float sa = sc[p.a_shift ? 0 : q * 32 + lane], sb = sc[BM + part];
+          read_rows(taddr, r);
+          const float x = sa * sb;
+          promote_rows(acc, r, x);
+          read_rows(taddr + 64, r);
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          empty_arrive(b);                           // buffer read
+          promote_rows(acc + 32, r, x);
         }
       }
-      if (!live) continue;
-      const int row = m0 + lane;
-      if (p.tma_store) {
-        // 32 rows x 32 columns at a time through the warp's block(s), 16-byte pieces placed by the 128-byte (fp32) or
-        // 64-byte (bf16) swizzle
+      // pair j of the thread's sums: which row of the warp's 32 and which column of its 128 (a pair is two adjacent columns)
+      auto pair_row = [&](int j) { return B_ROW_SCALES ? (j >> 5) * 16 + (j & 1) * 8 + (lane >> 2) : lane; };
+      auto pair_col = [&](int j) { return B_ROW_SCALES ? ((j & 31) >> 1) * 8 + 2 * (lane & 3) : 2 * j; };
+      if (p.split > 1) {
+        // the tile's only owner of these K blocks: its sums go where the operands were (all of them have been used)
+        float* part_sums = reinterpret_cast<float*>(smem) + (q * 32) * PART_PITCH + part * COLS;
 #pragma unroll
-        for (int c = 0; c < COLS / 32; ++c) {
-          if (n0 + c * 32 >= p.N) break;
-          const uint32_t buf = wbuf + (p.c_bf16 ? (out_it & 1u) * 2048u : 0u);
-          const float2* v = acc + c * 16;
-          if (lane == 0) { if (p.c_bf16) gemm::bulk_wait_read<1>(); else gemm::bulk_wait_read<0>(); }
+        for (int j = 0; j < COLS / 2; ++j) *reinterpret_cast<float2*>(part_sums + pair_row(j) * PART_PITCH + pair_col(j)) = acc[j];
+      } else if (!live) {
+        continue;
+      } else if (p.tma_store) {
+        // Blocks of 32 rows x 128 bytes (32 fp32 or 64 bf16 columns), 16-byte pieces placed by the 128-byte swizzle, two of them in
+        // the warp's 8 KB at a time: one wait for the stores before, one proxy fence.  (Rows of 64 bytes took the copy engine,
+        // which the operand loads need too, twice as long.)
+        const int ncol = p.c_bf16 ? 64 : 32;
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {                // bf16: all four quarters of the columns at once; fp32: two and two
+          if (g == 1 && p.c_bf16) break;
+          if (lane == 0) gemm::bulk_wait_read<0>();
           __syncwarp();
           if (p.c_bf16) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              st128(buf + (uint32_t)lane * 64u + (uint32_t)((j ^ ((lane >> 1) & 3)) * 16), bf16x2(v[4 * j]), bf16x2(v[4 * j + 1]), bf16x2(v[4 * j + 2]), bf16x2(v[4 * j + 3]));
+            for (int j = 0; j < COLS / 2; j += B_ROW_SCALES ? 1 : 4) {
+              const int row = pair_row(j), col = pair_col(j), unit = (col & 63) >> 3;
+              const uint32_t at = wbuf + (uint32_t)((col >> 6) * 4096 + row * 128 + ((unit ^ (row & 7)) << 4));
+              if (B_ROW_SCALES) st32(at + (col & 7) * 2, bf16x2(acc[j]));
+              else st128(at, bf16x2(acc[j]), bf16x2(acc[j + 1]), bf16x2(acc[j + 2]), bf16x2(acc[j + 3]));
+            }
           } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-              st128(buf + (uint32_t)lane * 128u + (uint32_t)((j ^ (lane & 7)) * 16), __float_as_uint(v[2 * j].x), __float_as_uint(v[2 * j].y),
-                    __float_as_uint(v[2 * j + 1].x), __float_as_uint(v[2 * j + 1].y));
+            for (int j = 0; j < COLS / 2; j += B_ROW_SCALES ? 1 : 2) {
+              // (columns 64 g to 64 g + 63)
+              if ((B_ROW_SCALES ? (j & 31) >> 4 : j >> 5) != g) continue;
+              const int row = pair_row(j), col = pair_col(j), unit = (col & 31) >> 2;
+              const uint32_t at = wbuf + (uint32_t)(((col >> 5) & 1) * 4096 + row * 128 + ((unit ^ (row & 7)) << 4));
+              if (B_ROW_SCALES) st64(at + (col & 3) * 4, acc[j]);
+              else st128(at, __float_as_uint(acc[j].x), __float_as_uint(acc[j].y), __float_as_uint(acc[j + 1].x), __float_as_uint(acc[j + 1].y));
+            }
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
-          if (lane == 0) { gemm::tma_store_2d(&map_c, buf, n0 + c * 32, m0); gemm::bulk_commit(); }
-          ++out_it;
-        }
-      } else if (row < p.M) {
-        if (p.c_bf16) {
-          __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.C) + (int64_t)row * p.ldc + n0;
-#pragma unroll
-          for (int j = 0; j < COLS; j += 2) {
-            if (n0 + j < p.N) dst[j] = __float2bfloat16_rn(acc[j / 2].x);
-            if (n0 + j + 1 < p.N) dst[j + 1] = __float2bfloat16_rn(acc[j / 2].y);
+          if (lane == 0) {
+            for (int c = 0; c < 2; ++c) {
+              const int col = n0 + (2 * g + c) * ncol;
+              if (col < n_end) gemm::tma_store_2d(&map_c, wbuf + c * 4096u, col, m0);
+            }
+            gemm::bulk_commit();
           }
-        } else {
-          float* dst = reinterpret_cast<float*>(p.C) + (int64_t)row * p.ldc + n0;
+        }
+      } else {
 #pragma unroll
-          for (int j = 0; j < COLS; j += 2) {
-            if (n0 + j < p.N) dst[j] = acc[j / 2].x;
-            if (n0 + j + 1 < p.N) dst[j + 1] = acc[j / 2].y;
+        for (int j = 0; j < COLS / 2; ++j) {
+          const int row = m0 + pair_row(j), col = n0 + pair_col(j);
+          if (row < p.M) {
+            const int64_t at = (int64_t)row * p.ldc + col;
+            if (p.c_bf16) {
+              __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.C) + at;
+              if (col < n_end) dst[0] = __float2bfloat16_rn(acc[j].x);
+              if (col + 1 < n_end) dst[1] = __float2bfloat16_rn(acc[j].y);
+            } else {
+              float* dst = reinterpret_cast<float*>(p.C) + at;
+              if (col < n_end) dst[0] = acc[j].x;
+              if (col + 1 < n_end) dst[1] = acc[j].y;
+            }
           }
         }
       }
     }
-    if (lane == 0 && out_it > 0) gemm::bulk_wait_all<0>();
+    if (lane == 0) gemm::bulk_wait_all<0>();         // the stores still read this CTA's memory
   }
 
   __syncwarp();
+  if (p.split > 1) {
+    // each CTA of the cluster adds up a part of the tile's rows
+    cooperative_groups::cluster_group cl = cooperative_groups::this_cluster();
+    cl.sync();
+    const int m0 = (group % tiles_m) * BM, n0 = (group / tiles_m) * bn, n_end = min(p.N, n0 + bn);
+    const int rows = BM / p.split;
+    for (int i = tid; i < rows * (BN / 4); i += THREADS) {
+      const int r = rank * rows + i / (BN / 4), c = (i % (BN / 4)) * 4, row = m0 + r, col = n0 + c;
+      if (row >= p.M || col >= n_end) continue;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int o = 0; o < p.split; ++o) {
+        const float4 w = *reinterpret_cast<const float4*>(cl.map_shared_rank(reinterpret_cast<float*>(smem), o) + r * PART_PITCH + c);
+        v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+      }
+      const float e[4] = {v.x, v.y, v.z, v.w};
+      const int64_t at = (int64_t)row * p.ldc + col;
+      if (p.c_bf16) {
+        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.C) + at;
+        if (p.c_vec && col + 4 <= n_end) *reinterpret_cast<uint2*>(dst) = make_uint2(bf16x2(make_float2(v.x, v.y)), bf16x2(make_float2(v.z, v.w)));
+        else for (int k = 0; k < 4; ++k) if (col + k < n_end) dst[k] = __float2bfloat16_rn(e[k]);
+      } else {
+        float* dst = reinterpret_cast<float*>(p.C) + at;
+        if (p.c_vec && col + 4 <= n_end) *reinterpret_cast<float4*>(dst) = v;
+        else for (int k = 0; k < 4; ++k) if (col + k < n_end) dst[k] = e[k];
+      }
+    }
+    cl.sync();                          // nobody leaves while its sums are read
+  }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   // after a wait ran out: time for loads and tensor-core work still under way
@@ -397,11 +452,9 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tn_fp8_kernel(const __grid_co
     if (tid == 0 && p.status) atomicOr(p.status, DPPO_STATUS_WAIT_LIMIT);
     drain_after_abort();
   }
-  if (CG == 2) cluster_sync_all();      // a pair leaves together
   if (warp == 1) {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    if (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(C::TMEM_COLS) : "memory");
-    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(C::TMEM_COLS) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(2 * BN) : "memory");
   }
 }
 
@@ -433,46 +486,43 @@ bool make_map(CUtensorMap* map, CUtensorMapDataType type, int es, const void* ba
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Scales [rows, kblocks] with adjacent rows, boxes of `box` rows of one K block; false if the layout does not allow a map
-bool make_scale_map(CUtensorMap* map, const float* base, int64_t rows, int64_t row_stride, int64_t kblocks, int64_t k_stride, int box) {
-  EncodeFn enc = get_encode();
-  if (!enc || row_stride != 1 || k_stride % 4 != 0 || k_stride < rows || ((uintptr_t)base % 16) != 0) return false;
-  cuuint64_t dims[2] = {(cuuint64_t)rows, (cuuint64_t)kblocks};
-  cuuint64_t strides[1] = {(cuuint64_t)k_stride * 4};
-  cuuint32_t boxes[2] = {(cuuint32_t)box, 1u};
-  cuuint32_t estr[2] = {1u, 1u};
-  return enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<float*>(base), dims, strides, boxes, estr,
-             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-template <int CG, bool B_ROW_SCALES>
-cudaError_t launch(Params p, const void* A, int64_t lda, const void* B, int64_t ldb, int sms, cudaStream_t st) {
-  using C = Cfg<CG>;
-  CUtensorMap ma, mb, mc, msa, msb;
-  if (!make_map(&ma, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, A, p.M, p.K, lda, 128, BM)) return cudaErrorInvalidValue;
-  if (!make_map(&mb, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, B, p.N, p.K, ldb, 128, C::B_ROWS)) return cudaErrorInvalidValue;
-  mc = msa = msb = ma;
-  p.a_tma = !p.a_shift && make_scale_map(&msa, p.sa, p.M, p.sa_row, p.kblocks, p.sa_k, BM);
-  p.b_tma = B_ROW_SCALES && make_scale_map(&msb, p.sb, p.N, p.sb_row, p.kblocks, p.sb_k, C::BN);
+template <bool B_ROW_SCALES>
+cudaError_t launch(Params p, const void* A, int64_t lda, const void* B, int64_t ldb, int K, int sms, cudaStream_t st) {
+  // Tile width (whole blocks of 128 columns) and split: the time of a K block of a tile hardly depends on the width (the hand-over's
+  // latency), so a block is counted as 256 + width, a shared tile's exchange as two blocks, and the cheapest choice is taken.
+  const int64_t tm = (p.M + BM - 1) / BM;
+  int64_t best = INT64_MAX;
+  for (int w = BN; w >= 128; w -= 128) {
+    const int64_t tiles = tm * ((p.N + w - 1) / w);
+    if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
+    for (int S = 1; S <= MAX_SPLIT; S *= 2) {
+      // (clusters of 8 do not fit the SMs of every GPC without a rest: 112 of 148 SMs can be counted on)
+      if (S > 1 && (tiles * S > (S == 8 ? sms * 3 / 4 : sms) || p.kblocks < 2 * S)) break;
+      const int64_t cost = ((tiles * S + sms - 1) / sms) * ((p.kblocks + S - 1) / S + (S > 1 ? 2 : 0)) * (256 + w);
+      if (cost < best) { best = cost; p.bn = w; p.split = S; }
+    }
+  }
+  CUtensorMap ma, mb, mc;
+  if (!make_map(&ma, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, A, p.M, K, lda, 128, BM)) return cudaErrorInvalidValue;
+  if (!make_map(&mb, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, B, p.N, K, ldb, 128, p.bn)) return cudaErrorInvalidValue;
+  mc = ma;
   p.tma_store = p.c_vec && make_map(&mc, p.c_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, p.c_bf16 ? 2 : 4, p.C, p.M, p.N,
-                                    p.ldc, 32, 32);
-  auto kernel = gemm_tn_fp8_kernel<CG, B_ROW_SCALES>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES);
+                                    p.ldc, p.c_bf16 ? 64 : 32, 32);
+  auto kernel = gemm_tn_fp8_kernel<B_ROW_SCALES>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
   if (e != cudaSuccess) return e;
-  const int64_t ntiles = (int64_t)((p.M + C::TILE_M - 1) / C::TILE_M) * ((p.N + C::BN - 1) / C::BN);
-  const int slots = sms / CG;
+  const int64_t ctas = tm * ((p.N + p.bn - 1) / p.bn) * p.split;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((ntiles < slots ? ntiles : slots) * CG));
+  cfg.gridDim = dim3((unsigned)(ctas < sms ? ctas : sms));           // a shared tile never has to wait for another: ctas <= sms then
   cfg.blockDim = dim3(THREADS);
-  cfg.dynamicSmemBytes = C::SMEM_BYTES;
+  cfg.dynamicSmemBytes = SMEM_BYTES;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = CG; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[0].val.clusterDim.x = (unsigned)p.split; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = (CG > 1) ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, kernel, ma, mb, mc, msa, msb, p);
+  cfg.numAttrs = p.split > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, ma, mb, mc, p);
 }
 
 }  // namespace f8
@@ -493,7 +543,7 @@ extern "C" int dppo_gemm_tn_fp8(const void* A, int64_t lda, int a_format, int a_
   if ((a_block_rows != 1 && a_block_rows != 128) || (b_block_rows != 1 && b_block_rows != 128)) return DPPO_ERR_UNSUPPORTED;
   dppo_opts o = {};
   if (opts) o = *opts;
-  if (o.gemm_cta_group < 0 || o.gemm_cta_group > 2 || o.wait_limit_us < 0) return DPPO_ERR_UNSUPPORTED;
+  if (o.wait_limit_us < 0) return DPPO_ERR_UNSUPPORTED;
   if (M == 0 || N == 0) return DPPO_OK;
   if (!C || (K > 0 && (!A || !B || !a_scale || !b_scale))) return DPPO_ERR_NULL;
   if (ldc < N || (K > 0 && (lda < K || ldb < K))) return DPPO_ERR_STRIDE;
@@ -506,7 +556,7 @@ extern "C" int dppo_gemm_tn_fp8(const void* A, int64_t lda, int a_format, int a_
   if (K == 0)                                            // an empty sum
     return cudaMemset2DAsync(C, (size_t)ldc * es, 0, (size_t)N * es, (size_t)M, st) == cudaSuccess ? DPPO_OK : DPPO_ERR_CUDA;
   f8::Params p = {};
-  p.M = M; p.N = N; p.K = K;
+  p.M = M; p.N = N;
   p.a_shift = a_block_rows == 128 ? 7 : 0;
   p.sa = a_scale; p.sa_row = a_scale_row_stride; p.sa_k = a_scale_k_stride;
   p.sb = b_scale; p.sb_row = b_scale_row_stride; p.sb_k = b_scale_k_stride;
@@ -519,10 +569,6 @@ extern "C" int dppo_gemm_tn_fp8(const void* A, int64_t lda, int a_format, int a_
   int dev = 0, sms = 0;
   cudaGetDevice(&dev);
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  const int64_t pair_tiles = (int64_t)((M + 255) / 256) * ((N + 255) / 256);
-  const bool pairs = o.gemm_cta_group == 2 || (o.gemm_cta_group == 0 && M > 128 && pair_tiles >= sms / 4);
-  cudaError_t e;
-  if (pairs) e = b_block_rows == 1 ? f8::launch<2, true>(p, A, lda, B, ldb, sms, st) : f8::launch<2, false>(p, A, lda, B, ldb, sms, st);
-  else e = b_block_rows == 1 ? f8::launch<1, true>(p, A, lda, B, ldb, sms, st) : f8::launch<1, false>(p, A, lda, B, ldb, sms, st);
+  const cudaError_t e = b_block_rows == 1 ? f8::launch<true>(p, A, lda, B, ldb, K, sms, st) : f8::launch<false>(p, A, lda, B, ldb, K, sms, st);
   return e == cudaSuccess ? DPPO_OK : DPPO_ERR_CUDA;
 }

@@ -195,17 +195,23 @@ def test_product_with_more_tiles_than_sms_and_strided_everything():
         assert bool((wc[:M, N:] == -3).all()) and bool((wc[M] == -3).all())
 
 
-@pytest.mark.parametrize("cta_group", [1, 2])
-@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (61, 1000, 700), (257, 700, 300), (600, 513, 2048), (2000, 20000, 130)])
+@pytest.mark.parametrize("M,N,K", [(1, 256, 20000), (64, 1024, 8192), (70, 300, 4100), (200, 100, 9000), (500, 1000, 1500), (61, 30000, 300), (129, 37000, 256)])
 @pytest.mark.parametrize("b_br", [1, 128])
-def test_product_on_single_sms_and_on_pairs(cta_group, M, N, K, b_br):
+def test_product_of_few_tiles_and_of_ragged_rounds(M, N, K, b_br):
+    """Clusters of two to eight CTAs that share a tile along K, and tiles narrower than 256 columns (their columns cross the 128-blocks
+    of the scales)."""
     A, sa = _operand(M, K, "e4m3", 1, seed=M)
     B, sb = _operand(N, K, "e4m3", b_br, seed=N)
     for out in (torch.float32, torch.bfloat16):
-        C, status = dppo.dppo_gemm_tn_fp8(A, sa, B, sb, 1, b_br, out, cta_group=cta_group)
+        C, status = dppo.dppo_gemm_tn_fp8(A, sa, B, sb, 1, b_br, out)
         torch.cuda.synchronize()
         assert int(status.item()) == 0
         _check_product(C, A, sa, 1, B, sb, b_br)
+        assert torch.equal(dppo.dppo_gemm_tn_fp8(A, sa, B, sb, 1, b_br, out)[0], C)
+    wide = torch.full((M + 1, N + 3), -3.0, device=DEV)
+    C, status = dppo.dppo_gemm_tn_fp8(A, sa, B, sb, 1, b_br, C=wide[:M, :N])
+    _check_product(C, A, sa, 1, B, sb, b_br)
+    assert bool((wide[:, N:] == -3).all()) and bool((wide[M] == -3).all())
 
 
 def test_product_over_an_empty_sum_and_of_nothing():
@@ -229,14 +235,15 @@ def test_nan_blocks_reach_only_their_rows():
     assert bool(C[131].isnan().all()) and int(C.isnan().sum()) == 260
 
 
-@pytest.mark.parametrize("cta_group", [1, 2])
-def test_product_gives_up_and_the_next_call_is_fine(cta_group):
-    A, sa = _operand(300, 500, "e4m3", 1, seed=3)
-    B, sb = _operand(520, 500, "e4m3", 128, seed=4)
-    C, status = dppo.dppo_gemm_tn_fp8(A, sa, B, sb, cta_group=cta_group, wait_limit_us=20000, test_inject=binding.INJECT_NO_COPIES)
+@pytest.mark.parametrize("M,K", [(300, 500), (100, 5000)])
+def test_product_gives_up_and_the_next_call_is_fine(M, K):
+    """A CTA per tile, and a cluster that shares its tiles (all of it meets at its barriers and leaves)."""
+    A, sa = _operand(M, K, "e4m3", 1, seed=3)
+    B, sb = _operand(520, K, "e4m3", 128, seed=4)
+    C, status = dppo.dppo_gemm_tn_fp8(A, sa, B, sb, wait_limit_us=20000, test_inject=binding.INJECT_NO_COPIES)
     torch.cuda.synchronize()
     assert int(status.item()) & binding.STATUS_WAIT_LIMIT
-    C, status = dppo.dppo_gemm_tn_fp8(A, sa, B, sb, cta_group=cta_group, wait_limit_us=20000)
+    C, status = dppo.dppo_gemm_tn_fp8(A, sa, B, sb, wait_limit_us=20000)
     torch.cuda.synchronize()
     assert int(status.item()) == 0
     _check_product(C, A, sa, 1, B, sb, 128)
