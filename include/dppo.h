@@ -117,7 +117,7 @@ typedef struct dppo_opts {
   float eps_low;       /* DPPO_PPO_CLIP only: lower clip range; <= 0: same as delta                      */
   int lm_head_layout;  /* dppo_fused_lmhead_fwd_bwd only: DPPO_LM_HEAD_DV (0) = W and dW are [d, V] row-major;
                           DPPO_LM_HEAD_VD (1) = both are [V, d] row-major (how a linear layer stores its weight)  */
-  int gemm_cta_group;  /* tensor-core GEMMs (fused variant, dppo_gemm_*): 0 or 2 = 256 x 256 tiles on pairs of SMs
+  int gemm_cta_group;  /* bf16 tensor-core GEMMs (fused variant, dppo_gemm_*_bf16): 0 or 2 = 256 x 256 tiles on pairs of SMs
                           (tcgen05 cta_group::2, each SM stages half of the B tile); 1 = 128 x 256 tiles on single SMs.
                           The results of the two modes agree up to the order of the fp32 additions in the tensor cores */
   int fused_rows_per_block;  /* dppo_fused_lmhead_fwd_bwd only: R > 0 finishes the rows in blocks of R (forward, scalars,

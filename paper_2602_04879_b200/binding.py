@@ -371,6 +371,20 @@ def dppo_loss_fwd_bwd_host(logits, sampled_ids, mu_logp, advantages, token_mask=
 
 
 SAMPLE_MAX_TOPK = 1024
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _adr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _on(dev, stream, call):
+    """``call(stream handle)`` with ``dev`` current: these entry points are called once a token, where switching to a device that is
+    current already would cost as much as the launch."""
+    if torch.cuda.current_device() == dev.index:
+        return call(_raw_stream(dev.index) if stream is None else stream.cuda_stream)
+    with torch.cuda.device(dev):
+        return call(_raw_stream(dev.index) if stream is None else stream.cuda_stream)
 
 
 def dppo_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, token_mask=None, K=0, out=None, status=None,
@@ -385,7 +399,7 @@ def dppo_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p
     dev = logits.device
     for name, t, dt in (("uniform", uniform, torch.float64), ("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
                         ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32), ("token_mask", token_mask, torch.uint8)):
-        assert t is None or (t.device == dev and t.dtype == dt and t.shape == (T,) and t.is_contiguous()), name
+        assert t is None or (t.dtype == dt and t.shape == (T,) and t.device == dev and t.is_contiguous()), name
     if out is None:
         out = dict(sampled_ids=torch.empty(T, dtype=torch.int32, device=dev), mu_logp=torch.empty(T, dtype=torch.float32, device=dev),
                    mu_topk_ids=torch.empty((T, K), dtype=torch.int32, device=dev) if K > 0 else None,
@@ -397,11 +411,10 @@ def dppo_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p
             assert (t is None and len(shape) == 2 and K == 0) or (t.device == dev and t.dtype == dt and t.shape == shape and t.is_contiguous()), name
     if status is None:
         status = torch.zeros(1, dtype=torch.int32, device=dev)
-    st = stream if stream is not None else torch.cuda.current_stream(dev)
-    with torch.cuda.device(dev):
-        rc = lib().dppo_sample(_ptr(logits), T, V, logits.stride(0) if T > 1 else V, _dtype_code(logits), _ptr(uniform), _ptr(temperature),
-                               _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(token_mask), int(K), _ptr(out["sampled_ids"]), _ptr(out["mu_logp"]),
-                               _ptr(out.get("mu_topk_ids")), _ptr(out.get("mu_topk_p")), _ptr(status), c_void_p(st.cuda_stream))
+    rc = _on(dev, stream, lambda st: lib().dppo_sample(
+        logits.data_ptr(), T, V, logits.stride(0) if T > 1 else V, _dtype_code(logits), uniform.data_ptr(), _adr(temperature), _adr(top_k), _adr(top_p),
+        _adr(min_p), _adr(token_mask), int(K), out["sampled_ids"].data_ptr(), out["mu_logp"].data_ptr(), _adr(out.get("mu_topk_ids")),
+        _adr(out.get("mu_topk_p")), status.data_ptr(), st))
     if rc != 0:
         raise DppoError(rc, "dppo_sample")
     return dict(sampled_ids=out["sampled_ids"], mu_logp=out["mu_logp"], mu_topk_ids=out.get("mu_topk_ids"), mu_topk_p=out.get("mu_topk_p"),
@@ -409,12 +422,11 @@ def dppo_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p
 
 
 def _fp8_pair(rows, cols, block_rows, dtype, dev):
-    """An 8-bit matrix whose rows start on 16-byte boundaries and its scales [row blocks, column blocks], stored block column after
-    block column: what dppo_gemm_tn_fp8 reads fastest."""
-    q = torch.empty((rows, -(-cols // 16) * 16), dtype=dtype, device=dev)[:, :cols]
+    """An 8-bit matrix whose rows start on 16-byte boundaries (what dppo_gemm_tn_fp8 needs) and its scales [row blocks, column blocks],
+    stored block column after block column (what it reads fastest)."""
     n = -(-rows // block_rows)
-    scale = torch.empty((-(-cols // 128), -(-n // 4) * 4), dtype=torch.float32, device=dev)[:, :n].t()
-    return q, scale
+    return (torch.empty_strided((rows, cols), (-(-cols // 16) * 16, 1), dtype=dtype, device=dev),
+            torch.empty_strided((n, -(-cols // 128)), (1, max(1, n)), dtype=torch.float32, device=dev))
 
 
 def dppo_fp8_quantize(x, dtype=torch.float8_e4m3fn, block_rows=1, rowwise=True, transposed=False, status=None, stream=None):
@@ -433,13 +445,12 @@ def dppo_fp8_quantize(x, dtype=torch.float8_e4m3fn, block_rows=1, rowwise=True, 
         qt, qt_scale = _fp8_pair(cols, rows, block, dtype, dev)
     if status is None:
         status = torch.zeros(1, dtype=torch.int32, device=dev)
-    st = stream if stream is not None else torch.cuda.current_stream(dev)
 
-    def strides(m, s):
-        return (m.stride(0), _ptr(s), s.stride(0), s.stride(1)) if m is not None else (0, None, 0, 0)
-    with torch.cuda.device(dev):
-        rc = lib().dppo_fp8_quantize(_ptr(x), rows, cols, x.stride(0) if rows > 1 else cols, _dtype_code(x), FP8_FORMATS[dtype], int(block_rows),
-                                     _ptr(q), *strides(q, scale), _ptr(qt), *strides(qt, qt_scale), _ptr(status), c_void_p(st.cuda_stream))
+    def place(m, s):
+        return (m.data_ptr(), m.stride(0), s.data_ptr(), s.stride(0), s.stride(1)) if m is not None else (None, 0, None, 0, 0)
+    rc = _on(dev, stream, lambda st: lib().dppo_fp8_quantize(
+        x.data_ptr(), rows, cols, x.stride(0) if rows > 1 else cols, _dtype_code(x), FP8_FORMATS[dtype], int(block_rows), *place(q, scale),
+        *place(qt, qt_scale), status.data_ptr(), st))
     if rc != 0:
         raise DppoError(rc, "dppo_fp8_quantize")
     return dict(q=q, scale=scale, qt=qt, qt_scale=qt_scale, status=status)
@@ -461,14 +472,12 @@ def dppo_gemm_tn_fp8(A, a_scale, B, b_scale, a_block_rows=1, b_block_rows=128, o
     assert C.device == A.device and C.shape == (M, N) and (N <= 1 or C.stride(1) == 1)
     if status is None:
         status = torch.zeros(1, dtype=torch.int32, device=A.device)
-    st = stream if stream is not None else torch.cuda.current_stream(A.device)
     up16 = -(-K // 16) * 16                               # a single row has no pitch of its own
-    with torch.cuda.device(A.device):
-        rc = lib().dppo_gemm_tn_fp8(_ptr(A), A.stride(0) if M > 1 else up16, FP8_FORMATS[A.dtype], int(a_block_rows), _ptr(a_scale),
-                                    a_scale.stride(0), a_scale.stride(1), _ptr(B), B.stride(0) if N > 1 else up16, FP8_FORMATS[B.dtype],
-                                    int(b_block_rows), _ptr(b_scale), b_scale.stride(0), b_scale.stride(1), M, N, K, _ptr(C), _dtype_code(C),
-                                    C.stride(0) if M > 1 else N, _ptr(status),
-                                    ctypes.byref(_opts(wait_limit_us=wait_limit_us, test_inject=test_inject)), c_void_p(st.cuda_stream))
+    opts = None if wait_limit_us == 0 and test_inject == 0 else ctypes.byref(_opts(wait_limit_us=wait_limit_us, test_inject=test_inject))
+    rc = _on(A.device, stream, lambda st: lib().dppo_gemm_tn_fp8(
+        A.data_ptr(), A.stride(0) if M > 1 else up16, FP8_FORMATS[A.dtype], int(a_block_rows), a_scale.data_ptr(), a_scale.stride(0), a_scale.stride(1),
+        B.data_ptr(), B.stride(0) if N > 1 else up16, FP8_FORMATS[B.dtype], int(b_block_rows), b_scale.data_ptr(), b_scale.stride(0),
+        b_scale.stride(1), M, N, K, C.data_ptr(), _dtype_code(C), C.stride(0) if M > 1 else N, status.data_ptr(), opts, st))
     if rc != 0:
         raise DppoError(rc, "dppo_gemm_tn_fp8")
     return C, status

@@ -17,11 +17,15 @@
 //   list      the kk-th largest group maximum bounds the kk-th largest element from below, and only the few groups whose
 //             maximum reaches it can hold one of the kk largest: those groups alone are read again, and what passes the bound
 //             is sorted in shared memory.  This is all that top-k and the top-K record need.
-//   search    cuts that lie below the list (top-p over a broad row, top_k > 1024, ties by the thousand) are bracketed by passes
-//             over the row (from L2), all CTAs of the cluster counting and summing above three pivots at a time, until what
-//             lies between two pivots fits the list.
+//   search    for cuts that lie below the list (top-p over a broad row, top_k > 1024): a histogram of the row over steps of 1/16
+//             octave of weight tells where the cut should be; a second pass sums exactly what lies above that neighbourhood and
+//             lists what lies in it.  Where that misses, or thousands of equal logits meet the cut, the cut is bracketed by passes
+//             with three pivots at a time until it is found.
 //   draw      inside the list, or, when the kept set is larger, in the one chunk that the running sum of the chunks' sums
 //             points to.
+//
+// Bounded by the 64-bit units: 8 operations an element in the passes that sum (t, its rounding, the remainder, four for the
+// polynomial, the sum) at 64 lanes a cycle and SM, 8 elements a cycle; HBM delivers about 12 bf16 elements in that time.
 #include <cooperative_groups.h>
 #include <limits.h>
 
@@ -33,8 +37,8 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kSThreads = 512, kSWarps = kSThreads / 32;
-constexpr int kSMaxChunks = 320;       // chunks of a row; a longer row has longer chunks
+constexpr int kSWarps = 16;             // most warps of a CTA
+constexpr int kSMaxChunks = 256;       // chunks of a row; a longer row has longer chunks
 constexpr int kSList = 4096;           // entries of the sorted list
 constexpr int kSMaxTop = DPPO_SAMPLE_MAX_TOPK;      // largest list that is asked for
 constexpr int kSProbe = 256;           // list length tried first for top-p / min-p alone
@@ -57,17 +61,18 @@ struct SampleParams {
   int32_t* status;
 };
 
-enum { OP_DONE = 0, OP_PIVOTS, OP_COMPACT, OP_EQUAL, OP_CDF };
+enum { OP_DONE = 0, OP_PIVOTS, OP_COMPACT, OP_EQUAL, OP_CDF, OP_HIST, OP_SPLIT };
+constexpr int kSBins = 1024;           // histogram: steps of 1/16 octave of weight below the maximum, 64 octaves
 struct Cmd {
   int op;
   uint32_t lo, hi;       // OP_COMPACT: keys [lo, hi)
-  float v[3];            // OP_PIVOTS: ascending; OP_EQUAL, OP_CDF: v[0]
-  int tie;               // OP_CDF
+  float v[3];            // OP_PIVOTS: ascending; OP_EQUAL, OP_CDF: v[0]; OP_SPLIT: summed from v[0] up, listed from v[1] up to it; OP_HIST:
+  int tie;               // counted below v[0] and tie (as in a Cut)
 };
 
 struct SampleSmem {
   double csum[kSMaxChunks];
-  double tab[32];                         // 2^(i/32)
+  double cref[kSMaxChunks];               // pass A: log2 of what the chunk's sum is relative to; NaN: relative to its maximum
   double red[kSWarps];
   double mass[kSMaxCluster][3];           // OP_PIVOTS results of the cluster's CTAs
   unsigned long long cnt[kSMaxCluster][3];
@@ -78,11 +83,13 @@ struct SampleSmem {
     float gmax[kSMaxChunks * 32];         // until the list is made
     double pref[kSList];                  // then: running sums along the list
   };
+  unsigned long long cfix[kSMaxChunks];   // kept weights of listed elements by chunk, in units of 2^-52
+  unsigned bins[kSBins];
   float cmax[kSMaxChunks];
   float rec_z[kSMaxTop];
   int rec_id[kSMaxTop];
-  int hist[256];
   Cmd cmd;
+  int wsum[kSWarps];
   int n_list;
   int pick;
   double dval;
@@ -108,20 +115,35 @@ __device__ __forceinline__ float warp_max_nan(float v) {
   return __int_as_float(m >= 0 ? m : m ^ 0x7fffffff);
 }
 
-// 2^x for -1020 <= x <= 1000: x = n/32 + f, 2^x = 2^(n>>5) tab[n & 31] 2^f, |f| <= 1/64, with the Taylor polynomial of 2^f
-// to the fourth power: the fifth term is below 1.3e-12.
-__device__ __forceinline__ double exp2_tab(double d, double c, const double* tab) {       // 2^(d c)
-  constexpr double kMagic = 6755399441055744.0 / 32.0;       // 1.5 2^52 / 32: adding it rounds to multiples of 1/32
-  const double t = fma(d, c, kMagic);
-  const double f = fma(d, c, -(t - kMagic));
-  double p = fma(f, 9.6181291076284772e-3, 5.5504108664821580e-2);     // ln2^4 / 24, ln2^3 / 6
-  p = fma(p, f, 2.4022650695910071e-1);                                // ln2^2 / 2
-  p = fma(p, f, 6.9314718055994531e-1);
-  p = fma(p, f, 1.0);
-  const int n = __double2loint(t);
-  const double s = tab[n & 31];
-  return p * __hiloint2double(__double2hiint(s) + ((n >> 5) << 20), __double2loint(s));
-}
+// 2^(z c - R) for -1020 <= z c - R <= 1000: = 2^(n>>5) 2^((n & 31)/32) 2^f with n the nearest integer to 32 (z c - R) and |f| <= 1/64.
+// R is a multiple of 1/32, so that the addition of a large constant that finds n can subtract R in the same step.  2^f by
+// its Taylor polynomial of degree 4 (the next term is below 1.3e-12); 2^(i/32) is held by lane i of the warp (a table in shared
+// memory would be read with bank conflicts).  All lanes of the warp have to take part.
+struct Exp2 {
+  static constexpr double kMagic = 6755399441055744.0 / 32.0;       // 1.5 2^52 / 32: adding it rounds to multiples of 1/32
+  double c, K, off;          // K = kMagic - R; where |max c| reaches 2^30, R = 0 and z - off takes z's place;
+                             // FAR = false leaves out the subtraction and is for off = 0 only
+  __device__ __forceinline__ void set(double c_, double ref, bool& far, double& log2_ref) {
+    c = c_;
+    far = !(fabs(ref * c_) < 1073741824.0);
+    off = far ? ref : 0.0;
+    const double R = far ? 0.0 : (fma(ref, c_, kMagic) - kMagic);
+    K = kMagic - R;
+    log2_ref = R;
+  }
+  template <bool FAR> __device__ __forceinline__ void parts(float z, int tab_hi, int tab_lo, double& p, double& s) const {
+    const double x = FAR ? (double)z - off : (double)z;
+    const double t = fma(x, c, K);
+    const double f = fma(x, c, -(t - K));
+    p = fma(f, 9.6181291076284772e-3, 5.5504108664821580e-2);     // ln2^4 / 24, ln2^3 / 6
+    p = fma(p, f, 2.4022650695910071e-1);                         // ln2^2 / 2
+    p = fma(p, f, 6.9314718055994531e-1);
+    p = fma(p, f, 1.0);
+    const int n = __double2loint(t);
+    const int hi = __shfl_sync(0xffffffffu, tab_hi, n), lo = __shfl_sync(0xffffffffu, tab_lo, n);
+    s = __hiloint2double(hi + ((n & ~31) << 15), lo);
+  }
+};
 
 template <typename T> struct Row;
 template <> struct Row<__nv_bfloat16> {
@@ -138,6 +160,11 @@ template <> struct Row<__nv_bfloat16> {
     w[e >> 1] = (e & 1) ? ((w[e >> 1] & 0xffffu) | (b << 16)) : ((w[e >> 1] & 0xffff0000u) | b);
   }
   static constexpr uint32_t kFill = 0xff80ff80u;      // -inf twice
+  static __device__ __forceinline__ float max_of(const uint4& v) {
+    auto h = [](uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); };
+    const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(h(v.x), h(v.y)), __hmax2_nan(h(v.z), h(v.w)));
+    return max_nan(__low2float(m), __high2float(m));
+  }
 };
 template <> struct Row<float> {
   static constexpr int N = 4;
@@ -148,6 +175,9 @@ template <> struct Row<float> {
   static __device__ __forceinline__ float at(const void* p, int64_t j) { return __uint_as_float(bits(p, j)); }
   static __device__ __forceinline__ void put(uint4& v, int e, uint32_t b) { (&v.x)[e] = b; }
   static constexpr uint32_t kFill = 0xff800000u;
+  static __device__ __forceinline__ float max_of(const uint4& v) {
+    return max_nan(max_nan(__uint_as_float(v.x), __uint_as_float(v.y)), max_nan(__uint_as_float(v.z), __uint_as_float(v.w)));
+  }
 };
 
 // One row as 16-byte vectors: vector s holds the elements [s N - head, s N - head + N), head = elements between the 16-byte
@@ -176,8 +206,9 @@ __device__ __forceinline__ Cut tighter(const Cut& a, const Cut& b) {
   return a.tie < b.tie ? a : b;
 }
 
-template <typename T>
+template <typename T, int NT>             // NT: threads of a CTA
 struct Worker {
+  static constexpr int NW = NT / 32;
   const SampleParams& p;
   SampleSmem& s;
   RowView<T> row;
@@ -185,7 +216,12 @@ struct Worker {
   int rank, C;
   double c;                                // log2(e) / tau
   double itau;                             // 1 / tau
+  double span;                             // 1000 / c: logits further below a maximum weigh less than 2^-1000 of it
+  int tab_hi, tab_lo;                      // 2^(lane/32)
   double M;                                // row maximum (known after pass A)
+  Exp2 eM;                                 // weights relative to (nearly) M; corr makes them relative to M
+  bool far;
+  double corr;
   static constexpr int N = Row<T>::N;
 
   __device__ __forceinline__ int tid() const { return threadIdx.x; }
@@ -199,82 +235,174 @@ struct Worker {
   }
   __device__ __forceinline__ double weight(float z) const { return exp(((double)z - M) * itau); }
   // smallest float whose weight relative to `ref` is worth counting (2^-1000 and more)
-  __device__ __forceinline__ float low_of(double ref) const { return __double2float_ru(ref - 1000.0 / c); }
+  __device__ __forceinline__ float low_of(double ref) const { return __double2float_ru(ref - span); }
+  __device__ __forceinline__ void set_max(double m) {
+    M = m;
+    double R;
+    eM.set(c, m, far, R);
+    corr = far ? 1.0 : exp2(fma(-m, c, R));
+  }
 
-  // f(z, element index) over this thread's part of chunk ch
-  template <typename F> __device__ __forceinline__ void each(int ch, F f) const {
-    for (int i = 0; i < p.vecs; ++i) {
-      const int sv = (ch * p.vecs + i) * 32 + lane();
-      const uint4 v = row.load(sv);
-      float z[N];
-      Row<T>::unpack(v, z);
-      const int j0 = sv * N - row.head;
+  // f(4 vectors, vector index of the first) over this lane's part of chunk ch, up to four vectors at a time; absent ones are -inf
+  template <typename F> __device__ __forceinline__ void vectors(int ch, F f) const {
+    const int s0 = ch * p.vecs * 32;
+    // whole vectors throughout: no bounds to look at
+    const bool inside = (int64_t)s0 * N >= row.head && (int64_t)(s0 + p.vecs * 32) * N - row.head <= row.V;
+    const uint4 none = make_uint4(Row<T>::kFill, Row<T>::kFill, Row<T>::kFill, Row<T>::kFill);
+    for (int i = 0; i < p.vecs; i += 4) {
+      uint4 v[4];
+      if (inside) {
+        const uint4* src = reinterpret_cast<const uint4*>(row.row + ((int64_t)(s0 + i * 32 + lane()) * N - row.head));
 #pragma unroll
-      for (int e = 0; e < N; ++e) f(z[e], j0 + e);
+        for (int k = 0; k < 4; ++k) v[k] = i + k < p.vecs ? __ldg(src + k * 32) : none;
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = i + k < p.vecs ? row.load(s0 + (i + k) * 32 + lane()) : none;
+      }
+      f(v, s0 + i * 32 + lane(), min(4, p.vecs - i));
     }
+  }
+  // f(z, element index) over this lane's part of chunk ch
+  template <typename F> __device__ __forceinline__ void each(int ch, F f) const {
+    vectors(ch, [&](const uint4* v, int s0, int n) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (k >= n) break;
+        float z[N];
+        Row<T>::unpack(v[k], z);
+        const int j0 = (s0 + k * 32) * N - row.head;
+#pragma unroll
+        for (int e = 0; e < N; ++e) f(z[e], j0 + e);
+      }
+    });
+  }
+  // sum of 2^(z c - R) over the elements of chunk ch.  Those below `low` count as `low`, less than 2^-800: where |max c| < 2^30 a float's
+  // steps are less than 128 octaves.  Far from zero they are left out, because `low` may round up to the maximum.
+  template <bool FAR> __device__ __forceinline__ double weigh_all(int ch, const Exp2& x, float low) const {
+    double sum = 0.0;
+    vectors(ch, [&](const uint4* v, int, int n) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (k >= n) break;
+        float z[N];
+        Row<T>::unpack(v[k], z);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          double q, w;
+          x.parts<FAR>(fmaxf(z[e], low), tab_hi, tab_lo, q, w);
+          if (!FAR || z[e] >= low) sum = fma(q, w, sum);
+        }
+      }
+    });
+    return warp_sum(sum);
+  }
+  // sum over the elements that are worth counting and for which take(z, index) holds
+  template <typename F> __device__ __forceinline__ double weigh(int ch, const Exp2& x, float low, F take) const {
+    double sum = 0.0;
+    each(ch, [&](float z, int j) {
+      double q, w;
+      x.parts<true>(fmaxf(z, low), tab_hi, tab_lo, q, w);
+      if (take(z, j) && z >= low) sum = fma(q, w, sum);
+    });
+    return warp_sum(sum);
+  }
+  // the same and the counts above three borders at once
+  __device__ __forceinline__ void weigh3(int ch, float low, const float* border, double* sum, unsigned* n) const {
+    double a[3] = {0, 0, 0};
+    unsigned b[3] = {0, 0, 0};
+    each(ch, [&](float z, int) {
+      double q, w;
+      eM.parts<true>(fmaxf(z, low), tab_hi, tab_lo, q, w);
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+        if (z >= border[i]) { ++b[i]; if (z >= low) a[i] = fma(q, w, a[i]); }
+    });
+#pragma unroll
+    for (int i = 0; i < 3; ++i) { sum[i] = warp_sum(a[i]); n[i] += __reduce_add_sync(0xffffffffu, b[i]); }
   }
 
   // ---- pass A ----
   __device__ void pass_a(bool want_sum, bool want_groups) const {
     SampleSmem* lead = smem_of(0);
-    for (int ch = c_begin + warp(); ch < c_end; ch += kSWarps) {
+    for (int ch = c_begin + warp(); ch < c_end; ch += NW) {
       float mx = -INFINITY;
-      for (int i = 0; i < p.vecs; i += 4) {
-        uint4 v[4];
+      vectors(ch, [&](const uint4* v, int, int n) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) if (i + k < p.vecs) v[k] = row.load((ch * p.vecs + i + k) * 32 + lane());
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (i + k < p.vecs) {
-            float z[N];
-            Row<T>::unpack(v[k], z);
-#pragma unroll
-            for (int e = 0; e < N; ++e) mx = max_nan(mx, z[e]);
-          }
-      }
+        for (int k = 0; k < 4; ++k) if (k < n) mx = max_nan(mx, Row<T>::max_of(v[k]));
+      });
       if (want_groups) lead->gmax[ch * 32 + lane()] = mx;
       const float cm = warp_max_nan(mx);
-      double sum = 0.0;
+      double sum = 0.0, ref = 0.0;
       if (want_sum && cm > -INFINITY && cm < INFINITY) {
+        Exp2 x;
+        bool far_ch;
+        x.set(c, (double)cm, far_ch, ref);
         const float low = low_of((double)cm);
-        each(ch, [&](float z, int) { const double w = exp2_tab((double)z - (double)cm, c, s.tab); if (z >= low) sum += w; });
-        sum = warp_sum(sum);
+        sum = far_ch ? weigh_all<true>(ch, x, low) : weigh_all<false>(ch, x, low);
+        if (far_ch) ref = NAN;
       }
-      if (lane() == 0) { lead->cmax[ch] = cm; lead->csum[ch] = sum; }
+      if (lane() == 0) { lead->cmax[ch] = cm; lead->csum[ch] = sum; lead->cref[ch] = ref; }
     }
   }
+
+  // which step of 1/16 octave of weight below the maximum (a monotone function of z)
+  __device__ __forceinline__ int bin_of(float z, float scale) const { return (int)fmaxf(0.f, fminf(((float)M - z) * scale, (float)(kSBins - 1))); }
+  // smallest float (above -inf) that falls into a bin below b; +inf if there is none
+  __device__ float border(int b) const {
+    uint32_t lo = kKeyNegInf, hi = kKeyInf;              // bin_of(lo) >= b (or lo = -inf), bin_of(hi) < b (or hi = inf)
+    while (hi - lo > 1) {
+      const uint32_t mid = lo + (hi - lo) / 2;
+      if (bin_of(of_key(mid), bin_scale()) < b) hi = mid; else lo = mid;
+    }
+    return of_key(hi);
+  }
+  __device__ __forceinline__ float bin_scale() const { return (float)(16.0 * c); }
 
   // ---- passes that the leader asks for ----
   __device__ void execute(const Cmd& k) const {
     SampleSmem* lead = smem_of(0);
-    if (k.op == OP_PIVOTS) {
+    const float low = low_of(M);
+    if (k.op == OP_PIVOTS || k.op == OP_SPLIT) {
+      // masses and counts above three borders; OP_SPLIT: above one, chunk sums too, and a list of what reaches a second one
       double m[3] = {0, 0, 0};
       unsigned n[3] = {0, 0, 0};
-      const float low = low_of(M);
-      for (int ch = c_begin + warp(); ch < c_end; ch += kSWarps)
-        each(ch, [&](float z, int) {
-          if (z >= k.v[0]) {
-            const double w = z >= low ? exp2_tab((double)z - M, c, s.tab) : 0.0;
+      for (int ch = c_begin + warp(); ch < c_end; ch += NW) {
+        if (k.op == OP_PIVOTS) {
+          double one[3];
+          weigh3(ch, low, k.v, one, n);
 #pragma unroll
-            for (int i = 0; i < 3; ++i) if (z >= k.v[i]) { m[i] += w; ++n[i]; }
-          }
-        });
-#pragma unroll
-      for (int i = 0; i < 3; ++i) {
-        const double mm = warp_sum(m[i]);
-        const unsigned nn = __reduce_add_sync(0xffffffffu, n[i]);
-        if (lane() == 0) { s.wmass[warp()][i] = mm; s.wcnt[warp()][i] = nn; }
+          for (int i = 0; i < 3; ++i) m[i] += one[i];
+        } else {
+          unsigned cnt = 0;
+          auto above = [&](float z, int j) {
+            const bool top = z >= k.v[0];
+            if (z >= k.v[1] && !top) {
+              const int at = atomicAdd(&lead->n_list, 1);
+              if (at < kSList) lead->list[at] = ((unsigned long long)~key_of(z) << 32) | (uint32_t)j;
+            }
+            cnt += top;
+            return top;
+          };
+          const double sum = corr * weigh(ch, eM, low, above);
+          if (lane() == 0) lead->csum[ch] = sum;
+          m[0] += sum;
+          n[0] += __reduce_add_sync(0xffffffffu, cnt);
+        }
       }
+      // (every lane holds its warp's totals)
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+        if (lane() == 0) { s.wmass[warp()][i] = k.op == OP_PIVOTS ? corr * m[i] : m[i]; s.wcnt[warp()][i] = n[i]; }
       __syncthreads();
       if (tid() < 3) {
         double a = 0.0;
         unsigned long long b = 0;
-        for (int w = 0; w < kSWarps; ++w) { a += s.wmass[w][tid()]; b += s.wcnt[w][tid()]; }
+        for (int w = 0; w < NW; ++w) { a += s.wmass[w][tid()]; b += s.wcnt[w][tid()]; }
         lead->mass[rank][tid()] = a;
         lead->cnt[rank][tid()] = b;
       }
     } else if (k.op == OP_COMPACT) {
-      for (int ch = c_begin + warp(); ch < c_end; ch += kSWarps)
+      for (int ch = c_begin + warp(); ch < c_end; ch += NW)
         each(ch, [&](float z, int j) {
           const uint32_t key = key_of(z);
           if (key >= k.lo && key < k.hi) {
@@ -283,7 +411,7 @@ struct Worker {
           }
         });
     } else if (k.op == OP_EQUAL) {
-      for (int ch = c_begin + warp(); ch < c_end; ch += kSWarps) {
+      for (int ch = c_begin + warp(); ch < c_end; ch += NW) {
         unsigned n = 0;
         each(ch, [&](float z, int) { n += (z == k.v[0]); });
         n = __reduce_add_sync(0xffffffffu, n);
@@ -291,13 +419,21 @@ struct Worker {
       }
     } else if (k.op == OP_CDF) {
       const Cut cut = {k.v[0], k.tie};
-      const float low = low_of(M);
-      for (int ch = c_begin + warp(); ch < c_end; ch += kSWarps) {
-        double sum = 0.0;
-        each(ch, [&](float z, int j) { if (z >= low && kept(cut, z, j)) sum += exp2_tab((double)z - M, c, s.tab); });
-        sum = warp_sum(sum);
+      auto take = [&](float z, int j) { return kept(cut, z, j); };
+      for (int ch = c_begin + warp(); ch < c_end; ch += NW) {
+        const double sum = corr * weigh(ch, eM, low, take);
         if (lane() == 0) lead->csum[ch] = sum;
       }
+    } else if (k.op == OP_HIST) {
+      for (int i = tid(); i < kSBins; i += NT) s.bins[i] = 0;
+      __syncthreads();
+      const float scale = bin_scale();
+      for (int ch = c_begin + warp(); ch < c_end; ch += NW)
+        each(ch, [&](float z, int j) {
+          const int b = z > -INFINITY ? bin_of(z, scale) : kSBins - 1;
+          if (b < kSBins - 1 && !(z > k.v[0] || (z == k.v[0] && j <= k.tie))) atomicAdd(&s.bins[b], 1u);       // (the last step takes all that is 64 octaves down and is not looked at)
+        });
+      __syncthreads();
     }
   }
   // Leader: hands a command to every CTA of the cluster and takes part; returns when all are done.
@@ -320,7 +456,7 @@ struct Worker {
     if (lane() == 31) s.red[warp()] = inc;
     __syncthreads();
     double before = 0.0, all = 0.0;
-    for (int w = 0; w < kSWarps; ++w) { if (w < warp()) before += s.red[w]; all += s.red[w]; }
+    for (int w = 0; w < NW; ++w) { if (w < warp()) before += s.red[w]; all += s.red[w]; }
     total = all;
     return before + (inc - v);
   }
@@ -334,23 +470,30 @@ struct Worker {
     return s.pick;
   }
   __device__ int block_count(int v) const {
-    __syncthreads();
-    if (tid() == 0) s.pick = 0;
-    __syncthreads();
     v = __reduce_add_sync(0xffffffffu, v);
-    if (lane() == 0) atomicAdd(&s.pick, v);
+    __syncthreads();                       // (the last call's sums have been read)
+    if (lane() == 0) s.wsum[warp()] = v;
     __syncthreads();
-    return s.pick;
+    return __reduce_add_sync(0xffffffffu, lane() < NW ? s.wsum[lane()] : 0);
   }
   // ascending sort of list[0, n): logits descending, ids ascending
   __device__ void sort_list(int n) const {
+    if (n <= NT) {                  // by rank: every entry counts those before it (all entries differ)
+      const unsigned long long mine = tid() < n ? s.list[tid()] : 0;
+      int r = 0;
+      if (tid() < n) for (int j = 0; j < n; ++j) r += s.list[j] < mine;
+      __syncthreads();
+      if (tid() < n) s.list[r] = mine;
+      __syncthreads();
+      return;
+    }
     int P = 32;
     while (P < n) P <<= 1;
-    for (int i = n + tid(); i < P; i += kSThreads) s.list[i] = ~0ull;
+    for (int i = n + tid(); i < P; i += NT) s.list[i] = ~0ull;
     __syncthreads();
     for (int k = 2; k <= P; k <<= 1)
       for (int j = k >> 1; j > 0; j >>= 1) {
-        for (int t = tid(); t < P / 2; t += kSThreads) {
+        for (int t = tid(); t < P / 2; t += NT) {
           const int i = ((t & ~(j - 1)) << 1) | (t & (j - 1)), l = i | j;
           const unsigned long long a = s.list[i], b = s.list[l];
           if ((a > b) == ((i & k) == 0)) { s.list[i] = b; s.list[l] = a; }
@@ -362,12 +505,12 @@ struct Worker {
   __device__ __forceinline__ int list_id(int i) const { return (int)(uint32_t)s.list[i]; }
   // pref[i] = sum of the first i + 1 weights of the list's first n entries
   __device__ double list_prefix(int n) const {
-    const int per = (n + kSThreads - 1) / kSThreads, b = tid() * per, e = min(n, b + per);
+    const int per = (n + NT - 1) / NT, b = tid() * per, e = min(n, b + per);
     double v = 0.0;
-    for (int i = b; i < e; ++i) v += weight(list_z(i));
+    for (int i = b; i < e; ++i) { v += weight(list_z(i)); s.pref[i] = v; }
     double total;
-    double run = block_scan(v, total);
-    for (int i = b; i < e; ++i) { run += weight(list_z(i)); s.pref[i] = run; }
+    const double run = block_scan(v, total);
+    for (int i = b; i < e; ++i) s.pref[i] += run;
     __syncthreads();
     return n > 0 ? s.pref[n - 1] : 0.0;
   }
@@ -375,7 +518,7 @@ struct Worker {
   __device__ int draw_from_list(int n, double u) const {
     const double target = u * s.pref[n - 1];
     int best = INT_MAX, last = -1;
-    if (n <= kSThreads / 2) {
+    if (n <= NT / 2) {
       if (tid() < n) {
         const int me = list_id(tid());
         double run = 0.0;
@@ -386,10 +529,10 @@ struct Worker {
     } else {
       __syncthreads();
       // turned round in place: ids in front, position in the list (for the weight) behind
-      for (int i = tid(); i < n; i += kSThreads) s.list[i] = ((unsigned long long)(uint32_t)list_id(i) << 32) | (uint32_t)i;
+      for (int i = tid(); i < n; i += NT) s.list[i] = ((unsigned long long)(uint32_t)list_id(i) << 32) | (uint32_t)i;
       __syncthreads();
       sort_list(n);
-      const int per = (n + kSThreads - 1) / kSThreads, b = tid() * per, e = min(n, b + per);
+      const int per = (n + NT - 1) / NT, b = tid() * per, e = min(n, b + per);
       double v = 0.0;
       for (int i = b; i < e; ++i) { const int j = (int)(uint32_t)s.list[i]; v += s.pref[j] - (j ? s.pref[j - 1] : 0.0); }
       double total;
@@ -416,42 +559,103 @@ struct Worker {
     before = s.dval;
     return ch;
   }
-  // lowest element of chunk ch at which before + running sum of w(z, j) exceeds target; the last one with w > 0 otherwise
+  // lowest element of chunk ch at which before + running sum of w(z, j) exceeds target; the last one with w > 0 otherwise.  A vector
+  // per thread.  (w is evaluated by whole warps.)
   template <typename F> __device__ int find_in_chunk(int ch, double before, double target, F w) const {
-    __syncthreads();
-    if (warp() == 0) {
-      int best = INT_MAX, last = -1;
-      double run = before;
-      for (int i = 0; i < p.vecs && best == INT_MAX; ++i) {
-        const int sv = (ch * p.vecs + i) * 32 + lane();
-        const uint4 v = row.load(sv);
-        float z[N];
-        Row<T>::unpack(v, z);
-        const int j0 = sv * N - row.head;
-        double x[N], mine = 0.0;
+    int best = INT_MAX, last = -1;
+    double run = before;
+    for (int v0 = 0; v0 < p.vecs * 32; v0 += NT) {
+      const int sv = ch * p.vecs * 32 + v0 + tid();
+      const uint4 none = make_uint4(Row<T>::kFill, Row<T>::kFill, Row<T>::kFill, Row<T>::kFill);
+      const uint4 v = v0 + tid() < p.vecs * 32 ? row.load(sv) : none;
+      float z[N];
+      Row<T>::unpack(v, z);
+      const int j0 = sv * N - row.head;
+      double x[N], mine = 0.0, total;
 #pragma unroll
-        for (int e = 0; e < N; ++e) { x[e] = w(z[e], j0 + e); mine += x[e]; if (x[e] > 0.0) last = j0 + e; }
-        double inc = mine;
+      for (int e = 0; e < N; ++e) { x[e] = w(z[e], j0 + e); mine += x[e]; if (x[e] > 0.0) last = j0 + e; }
+      double r = run + block_scan(mine, total);
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) { const double y = __shfl_up_sync(0xffffffffu, inc, o); if (lane() >= o) inc += y; }
-        double r = run + (inc - mine);
-        int b = INT_MAX;
-#pragma unroll
-        for (int e = 0; e < N; ++e) { r += x[e]; if (b == INT_MAX && x[e] > 0.0 && r > target) b = j0 + e; }
-        best = __reduce_min_sync(0xffffffffu, b);
-        run = run + __shfl_sync(0xffffffffu, inc, 31);
-      }
-      last = __reduce_max_sync(0xffffffffu, last);
-      if (lane() == 0) s.pick = best != INT_MAX ? best : last;
+      for (int e = 0; e < N; ++e) { r += x[e]; if (best == INT_MAX && x[e] > 0.0 && r > target) best = j0 + e; }
+      run += total;
     }
+    best = block_min(best);
+    return best != INT_MAX ? best : -block_min(-last);
+  }
+
+  // find_cut's first try: the cut's neighbourhood from a histogram, then exactly.  False if it was missed.  On success csum + cfix are
+  // the chunks' sums of the prefix.
+  // known: the n_known largest are listed and weigh known_mass together; the estimate is about the others.
+  __device__ bool guess(bool by_mass, unsigned long long count, double target, int n_known, double known_mass, Cut& cut, double& top_mass) const {
+    Cmd k = {};
+    k.op = OP_HIST;
+    k.v[0] = n_known > 0 ? list_z(n_known - 1) : INFINITY;
+    k.tie = n_known > 0 ? list_id(n_known - 1) : 0;
+    issue(k);
+    // each thread some adjacent bins: counts and estimated masses in order, then the bin in which the running sum gets there
+    constexpr int kPer = kSBins / NT;
+    double w[kPer], sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int b = tid() * kPer + i;
+      unsigned c_ = 0;
+      for (int r = 0; r < C; ++r) c_ += smem_of(r)->bins[b];
+      w[i] = by_mass ? (double)c_ * exp2(-((double)b + 0.5) / 16.0) : (double)c_;
+      sum += w[i];
+    }
+    double total;
+    double run = (by_mass ? known_mass : (double)n_known) + block_scan(sum, total);
+    const double goal = by_mass ? target : (double)count;
+    int at = INT_MAX;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) { run += w[i]; if (at == INT_MAX && w[i] > 0.0 && run >= goal) at = tid() * kPer + i; }
+    at = block_min(at);
+    if (at == INT_MAX) { if (!by_mass) return false; at = kSBins - 2; }
+    // one bin to either side (counts are exact and need none), as far as the list holds them
+    const int side = by_mass ? 1 : 0;
+    k.v[0] = border(max(0, at - side));
+    k.v[1] = border(min(kSBins - 1, at + side + 1));
     __syncthreads();
-    return s.pick;
+    if (tid() == 0) s.n_list = 0;
+    k.op = OP_SPLIT;
+    issue(k);
+    if (s.n_list > kSList || s.n_list == 0) return false;
+    const int m = s.n_list;
+    double above = 0.0;
+    unsigned long long n_above = 0;
+    for (int r = 0; r < C; ++r) { above += s.mass[r][0]; n_above += s.cnt[r][0]; }
+    sort_list(m);
+    list_prefix(m);
+    int pos;
+    if (by_mass) {
+      if ((n_above > 0 && above >= target) || above + s.pref[m - 1] < target) return false;
+      int b = INT_MAX;
+      for (int i = tid(); i < m; i += NT) if (above + s.pref[i] >= target) { b = i; break; }
+      pos = block_min(b);
+    } else {
+      if (n_above >= count || n_above + (unsigned long long)m < count) return false;
+      pos = (int)(count - n_above) - 1;
+    }
+    cut.z = list_z(pos); cut.tie = list_id(pos);
+    top_mass = above + s.pref[pos];
+    // the listed part of the prefix joins its chunks (integers: no order to depend on)
+    if (tid() < nchunks) s.cfix[tid()] = 0;
+    __syncthreads();
+    for (int i = tid(); i <= pos; i += NT)
+      atomicAdd(&s.cfix[(list_id(i) + row.head) / (N * 32 * p.vecs)], (unsigned long long)(weight(list_z(i)) * 4503599627370496.0));
+    __syncthreads();
+    if (tid() < nchunks) s.csum[tid()] += (double)s.cfix[tid()] * (1.0 / 4503599627370496.0);
+    __syncthreads();
+    return true;
   }
 
   // The cut after which the kept prefix (of all finite entries, in order) has `count` tokens (by_mass false), or is the
   // shortest one with mass >= target (by_mass true).  *top_mass: mass of that prefix.  False if the whole row is kept.
-  // Overwrites list, pref and csum.
-  __device__ bool find_cut(bool by_mass, unsigned long long count, double target, double tau, Cut& cut, double& top_mass) const {
+  // Overwrites list, pref and csum; *summed: csum holds the prefix's chunk sums.
+  __device__ bool find_cut(bool by_mass, unsigned long long count, double target, double tau, int n_known, double known_mass, Cut& cut,
+                           double& top_mass, bool* summed) const {
+    *summed = false;
+    if (guess(by_mass, count, target, n_known, known_mass, cut, top_mass)) { *summed = true; return true; }
     uint32_t lo = kKeyNegInf + 1, hi = kKeyInf;          // crit(key >= lo) holds, crit(key >= hi) does not
     unsigned long long n_hi = 0, n_lo = ~0ull;
     double m_hi = 0.0;
@@ -501,7 +705,7 @@ struct Worker {
       int at = n - 1;
       if (by_mass) {
         int b = INT_MAX;
-        for (int i = tid(); i < n; i += kSThreads) if (m_hi + s.pref[i] >= target) { b = i; break; }
+        for (int i = tid(); i < n; i += NT) if (m_hi + s.pref[i] >= target) { b = i; break; }
         b = block_min(b);
         if (b != INT_MAX) at = b;
       } else {
@@ -534,62 +738,67 @@ struct Worker {
     uint32_t bound = kKeyNegInf + 1;
     const int G = nchunks * 32;
     if (kk < G) {
-      // the two upper digits of the kk-th largest group maximum, by counting
-      uint32_t prefix = 0;
-      int want = kk;
-      for (int d = 0; d < 2; ++d) {
-        const int shift = 24 - 8 * d;
-        for (int i = tid(); i < 256; i += kSThreads) s.hist[i] = 0;
-        __syncthreads();
-        for (int g = tid(); g < G; g += kSThreads) {
-          const uint32_t k = key_of(s.gmax[g]);
-          if (d == 0 || (k >> 24) == (prefix >> 24)) atomicAdd(&s.hist[(k >> shift) & 255], 1);
-        }
-        __syncthreads();
-        if (warp() == 0) {                    // lane i: digits 255 - 8 i down to 248 - 8 i
-          int n = 0;
-          for (int q = 0; q < 8; ++q) n += s.hist[255 - 8 * lane() - q];
-          int inc = n;
+      // A bound that at least kk group maxima reach and not many more, from an interval of values [lo, hi) that is cut in three at
+      // a time (of keys now and then, which ends it whatever the values are).  The lowest chunk maximum is a lower end if there
+      // are kk chunks; otherwise one is looked for in growing steps.
+      constexpr int kPer = kSMaxChunks * 32 / NT;
+      uint32_t g[kPer];
 #pragma unroll
-          for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, inc, o); if (lane() >= o) inc += x; }
-          int run = inc - n;
-          if (run < want && inc >= want) {
-            for (int q = 0; q < 8; ++q) {
-              const int dg = 255 - 8 * lane() - q, h = s.hist[dg];
-              if (run + h >= want) { s.pick = dg; s.n_list = run; break; }
-              run += h;
-            }
-          }
+      for (int i = 0; i < kPer; ++i) { const int at = tid() + i * NT; g[i] = at < G ? key_of(s.gmax[at]) : 0u; }
+      float low_max = INFINITY;
+      for (int ch = lane(); ch < nchunks; ch += 32) low_max = fminf(low_max, s.cmax[ch]);
+      low_max = -warp_max_nan(-low_max);
+      uint32_t lo = bound, hi = key_of((float)M) + 1;
+      bool open = kk > nchunks;                      // lo is not known to be one
+      if (!open) lo = max(lo, key_of(low_max));
+      float step = (float)M - low_max;
+      for (int it = 0; it < 64 && hi - lo > 1; ++it) {
+        const float vl = of_key(lo), vh = of_key(hi - 1);
+        uint32_t a, b;                               // lo < a <= b < hi
+        if (open && step > 0.f && step < 1e30f) {
+          a = key_of(vh - 3.f * step); b = key_of(vh - step);
+          step *= 4.f;
+        } else if (!open && (it & 7) != 7) {
+          a = key_of(vl + (vh - vl) * (1.f / 3.f)); b = key_of(vl + (vh - vl) * (2.f / 3.f));
+        } else {
+          a = lo + (hi - lo) / 3; b = lo + (hi - lo) / 3 * 2;
         }
-        __syncthreads();
-        prefix |= (uint32_t)s.pick << shift;
-        want -= s.n_list;
-        __syncthreads();
+        a = min(max(a, lo + 1), hi - 1);
+        b = min(max(b, a), hi - 1);
+        int n = 0;                                   // two counts, 16 bits each
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) n += (g[i] >= a ? 1 : 0) + (g[i] >= b ? 65536 : 0);
+        n = block_count(n);
+        const int na = n & 0xffff, nb = (int)((unsigned)n >> 16);
+        if (nb >= kk) lo = b; else { hi = b; if (na >= kk) lo = a; else hi = a; }
+        const int got = nb >= kk ? nb : na;
+        if (got >= kk) { open = false; if (got <= 2 * kk + 32) break; }
       }
-      bound = max(bound, prefix);
+      bound = lo;
     }
     __syncthreads();
     if (tid() == 0) s.n_list = 0;
     __syncthreads();
-    // a thread per vector of each group that reaches the bound
-    for (int g0 = 0; g0 < G; g0 += kSThreads) {
-      const int g = g0 + tid();
-      const bool hit = g < G && key_of(s.gmax[g]) >= bound;
-      if (hit) {
-        const int ch = g >> 5, ln = g & 31;
-        for (int i = 0; i < p.vecs; ++i) {
-          const int sv = (ch * p.vecs + i) * 32 + ln;
-          const uint4 v = row.load(sv);
-          float z[N];
-          Row<T>::unpack(v, z);
+    // the groups that reach the bound (their numbers take the place of sorting space), then a thread per vector of each
+    int* hits = reinterpret_cast<int*>(s.bins);
+    if (tid() == 0) s.pick = 0;
+    __syncthreads();
+    for (int g = tid(); g < G; g += NT)
+      if (key_of(s.gmax[g]) >= bound) { const int at = atomicAdd(&s.pick, 1); if (at < kSBins) hits[at] = g; }
+    __syncthreads();
+    const int n_hits = s.pick;
+    if (n_hits > kSBins) return false;
+    for (int i = tid(); i < n_hits * p.vecs; i += NT) {
+      const int g = hits[i / p.vecs], sv = ((g >> 5) * p.vecs + i % p.vecs) * 32 + (g & 31);
+      const uint4 v = row.load(sv);
+      float z[N];
+      Row<T>::unpack(v, z);
 #pragma unroll
-          for (int e = 0; e < N; ++e) {
-            const uint32_t key = key_of(z[e]);
-            if (key >= bound) {
-              const int at = atomicAdd(&s.n_list, 1);
-              if (at < kSList) s.list[at] = ((unsigned long long)~key << 32) | (uint32_t)(sv * N - row.head + e);
-            }
-          }
+      for (int e = 0; e < N; ++e) {
+        const uint32_t key = key_of(z[e]);
+        if (key >= bound) {
+          const int at = atomicAdd(&s.n_list, 1);
+          if (at < kSList) s.list[at] = ((unsigned long long)~key << 32) | (uint32_t)(sv * N - row.head + e);
         }
       }
     }
@@ -598,8 +807,11 @@ struct Worker {
   }
 };
 
-template <typename T>
-__global__ void __launch_bounds__(kSThreads, 2) dppo_sample_kernel(SampleParams p, int C) {
+// 512 threads an SM (as one CTA where CTAs share rows, as two otherwise, so that one row's end overlaps another's pass) with 128
+// registers each: the 64-bit chains need several elements in flight per thread more than they need warps.
+template <typename T, int NT>
+__global__ void __launch_bounds__(NT, 512 / NT) dppo_sample_kernel(SampleParams p, int C) {
+  constexpr int NW = NT / 32;
   extern __shared__ __align__(16) unsigned char smem_raw[];
   SampleSmem& s = *reinterpret_cast<SampleSmem*>(smem_raw);
   const int rank = (C == 1) ? 0 : (int)cluster_ctarank();
@@ -609,7 +821,7 @@ __global__ void __launch_bounds__(kSThreads, 2) dppo_sample_kernel(SampleParams 
   auto drop = [&](int bit) {
     if (rank == 0) {
       if (tid == 0) { p.ids[t] = 0; p.logp[t] = 0.f; if (bit) atomicOr(p.status, bit); }
-      for (int i = tid; i < p.K; i += kSThreads) { p.topk_ids[t * p.K + i] = 0; p.topk_p[t * p.K + i] = 0.f; }
+      for (int i = tid; i < p.K; i += NT) { p.topk_ids[t * p.K + i] = 0; p.topk_p[t * p.K + i] = 0.f; }
     }
   };
   if (p.token_mask && p.token_mask[t] == 0) { drop(0); return; }          // the same decision in every CTA of the cluster
@@ -634,10 +846,12 @@ __global__ void __launch_bounds__(kSThreads, 2) dppo_sample_kernel(SampleParams 
   row.head = (int)(((uintptr_t)base & 15) / sizeof(T));
   row.nvec = (int)(((int64_t)row.head + p.V + Row<T>::N - 1) / Row<T>::N);
   const int nchunks = (row.nvec + 32 * p.vecs - 1) / (32 * p.vecs), per = (nchunks + C - 1) / C;
-  Worker<T> w = {p, s, row, nchunks, min(nchunks, rank * per), min(nchunks, (rank + 1) * per), rank, C, kLog2eD / tau, 1.0 / tau, 0.0};
+  Worker<T, NT> w = {p, s, row, nchunks, min(nchunks, rank * per), min(nchunks, (rank + 1) * per), rank, C, kLog2eD / tau, 1.0 / tau, 1000.0 * tau / kLog2eD};
 
-  if (tid < 32) s.tab[tid] = exp2((double)tid / 32.0);
-  w.csync();                                         // tables ready; every CTA of the cluster runs
+  const double mine = exp2((double)(tid & 31) / 32.0);
+  w.tab_hi = __double2hiint(mine);
+  w.tab_lo = __double2loint(mine);
+  if (C > 1) w.csync();                              // every CTA of the cluster runs
   w.pass_a(!small_k, kk > 0);
   w.csync();
 
@@ -646,12 +860,12 @@ __global__ void __launch_bounds__(kSThreads, 2) dppo_sample_kernel(SampleParams 
   float mx = -INFINITY;
   for (int ch = threadIdx.x & 31; ch < nchunks; ch += 32) mx = max_nan(mx, lead->cmax[ch]);
   mx = warp_max_nan(mx);
-  w.M = (double)mx;
   if (!(mx > -INFINITY && mx < INFINITY)) {          // a NaN, an infinity, or nothing but -inf: every CTA sees the same
     drop(DPPO_STATUS_NONFINITE_ROW);
     w.csync();                                       // the leader's shared memory was read by all
     return;
   }
+  w.set_max((double)mx);
   if (rank != 0) {                                   // passes that the leader asks for, until it is done
     for (;;) {
       w.csync();
@@ -668,7 +882,8 @@ __global__ void __launch_bounds__(kSThreads, 2) dppo_sample_kernel(SampleParams 
     // chunk sums relative to the row maximum, and the whole mass
     double v = 0.0;
     if (tid < nchunks) {
-      v = s.csum[tid] > 0.0 ? s.csum[tid] * exp(((double)s.cmax[tid] - w.M) * w.itau) : 0.0;
+      const double ref = s.cref[tid];                // (NaN: relative to the chunk's maximum)
+      if (s.csum[tid] > 0.0) v = s.csum[tid] * (ref == ref ? exp2(fma(-w.M, w.c, ref)) : exp(((double)s.cmax[tid] - w.M) * w.itau));
       s.csum[tid] = v;
     }
     w.block_scan(v, W);
@@ -682,7 +897,8 @@ __global__ void __launch_bounds__(kSThreads, 2) dppo_sample_kernel(SampleParams 
       // ties or an order that puts thousands of the largest into few groups: the exact cut of the kk largest
       Cut kc = {-INFINITY, -1};
       double dummy;
-      w.find_cut(false, (unsigned long long)kk, 0.0, tau, kc, dummy);
+      bool summed;
+      w.find_cut(false, (unsigned long long)kk, 0.0, tau, 0, 0.0, kc, dummy, &summed);
       // the kk entries themselves
       __syncthreads();
       if (tid == 0) s.n_list = 0;
@@ -690,7 +906,7 @@ __global__ void __launch_bounds__(kSThreads, 2) dppo_sample_kernel(SampleParams 
       cmd.op = OP_COMPACT; cmd.lo = key_of(kc.z) + 1; cmd.hi = kKeyInf;
       w.issue(cmd);
       // of the value at the cut the ones up to its tie, by a walk over the leader's view of the row
-      for (int ch = tid >> 5; ch < nchunks; ch += kSWarps)
+      for (int ch = tid >> 5; ch < nchunks; ch += NW)
         w.each(ch, [&](float z, int j) {
           if (z == kc.z && j <= kc.tie) {
             const int at = atomicAdd(&s.n_list, 1);
@@ -707,7 +923,7 @@ __global__ void __launch_bounds__(kSThreads, 2) dppo_sample_kernel(SampleParams 
     n_list = s.n_list;
     w.sort_list(n_list);
     n_rec = min(n_list, p.K);
-    for (int i = tid; i < n_rec; i += kSThreads) { s.rec_z[i] = w.list_z(i); s.rec_id[i] = w.list_id(i); }
+    for (int i = tid; i < n_rec; i += NT) { s.rec_z[i] = w.list_z(i); s.rec_id[i] = w.list_id(i); }
     if (small_k || p_on || m_on) {
       if (small_k) n_list = min(n_list, (int)k);
       const double total = w.list_prefix(n_list);
@@ -719,13 +935,13 @@ __global__ void __launch_bounds__(kSThreads, 2) dppo_sample_kernel(SampleParams 
         if (p_on) {
           const double target = top_p * W;
           int b = INT_MAX;
-          for (int i = tid; i < n_list; i += kSThreads) if (s.pref[i] >= target) { b = i; break; }
+          for (int i = tid; i < n_list; i += NT) if (s.pref[i] >= target) { b = i; break; }
           b = w.block_min(b);
           if (b != INT_MAX) { n = min(n, b + 1); in_list = true; }
         }
         if (m_on) {
           int cnt = 0;
-          for (int i = tid; i < n_list; i += kSThreads) cnt += (w.weight(w.list_z(i)) >= min_p);
+          for (int i = tid; i < n_list; i += NT) cnt += (w.weight(w.list_z(i)) >= min_p);
           cnt = w.block_count(cnt);
           if (cnt < n_list || small_k) { n = min(n, cnt); in_list = true; }
         }
@@ -742,34 +958,43 @@ __global__ void __launch_bounds__(kSThreads, 2) dppo_sample_kernel(SampleParams 
     __syncthreads();
     pick = w.draw_from_list(n, u);
   } else {
+    bool summed = !(k_on || p_on || m_on);           // csum holds the sums of what is kept
     if (k_on) {                                      // top_k above kSMaxTop
       Cut kc;
       double mass;
-      if (w.find_cut(false, (unsigned long long)k, 0.0, tau, kc, mass)) { cut = kc; cut_on = true; W = mass; }
+      if (w.find_cut(false, (unsigned long long)k, 0.0, tau, 0, 0.0, kc, mass, &summed)) { cut = kc; cut_on = true; W = mass; }
     }
     if (p_on) {
       Cut pc;
       double mass;
-      if (w.find_cut(true, 0, top_p * W, tau, pc, mass)) { cut = cut_on ? tighter(cut, pc) : pc; cut_on = true; }
+      if (w.find_cut(true, 0, top_p * W, tau, k_on ? 0 : n_list, k_on || n_list == 0 ? 0.0 : s.pref[n_list - 1], pc, mass, &summed)) {
+        if (cut_on) { const Cut both = tighter(cut, pc); summed = summed && both.z == pc.z && both.tie == pc.tie; cut = both; }
+        else cut = pc;
+        cut_on = true;
+      }
     }
     if (m_on) {
       const Cut mc = {__double2float_ru(w.M + tau * log(min_p)), INT_MAX};
-      cut = cut_on ? tighter(cut, mc) : mc;
+      const Cut both = cut_on ? tighter(cut, mc) : mc;
+      summed = summed && cut_on && both.z == cut.z && both.tie == cut.tie;
+      cut = both;
       cut_on = true;
     }
-    if (cut_on) {
+    if (!summed) {
       Cmd cmd = {};
       cmd.op = OP_CDF; cmd.v[0] = cut.z; cmd.tie = cut.tie;
       w.issue(cmd);
-      w.block_scan(tid < nchunks ? s.csum[tid] : 0.0, W);
-      __syncthreads();
     }
+    w.block_scan(tid < nchunks ? s.csum[tid] : 0.0, W);
+    __syncthreads();
     const double target = u * W;
     double before;
     const int ch = w.find_chunk(target, before);
     const float low = w.low_of(w.M);
     pick = w.find_in_chunk(ch, before, target, [&](float z, int j) {
-      return (z >= low && (!cut_on || kept(cut, z, j))) ? exp2_tab((double)z - w.M, w.c, s.tab) : 0.0;
+      double q, x;
+      w.eM.template parts<true>(fmaxf(z, low), w.tab_hi, w.tab_lo, q, x);
+      return (z >= low && (!cut_on || kept(cut, z, j))) ? w.corr * (q * x) : 0.0;
     });
   }
   if (tid == 0) {
@@ -777,7 +1002,7 @@ __global__ void __launch_bounds__(kSThreads, 2) dppo_sample_kernel(SampleParams 
     p.logp[t] = (float)(((double)Row<T>::at(base, pick) - w.M) / tau - log(W));
   }
   // the record: the largest K in order, with what the draw gave them
-  for (int i = tid; i < n_rec; i += kSThreads) {
+  for (int i = tid; i < n_rec; i += NT) {
     p.topk_ids[t * p.K + i] = s.rec_id[i];
     p.topk_p[t * p.K + i] = (!cut_on || kept(cut, s.rec_z[i], s.rec_id[i])) ? (float)(w.weight(s.rec_z[i]) / W) : 0.f;
   }
@@ -796,14 +1021,14 @@ __global__ void __launch_bounds__(kSThreads, 2) dppo_sample_kernel(SampleParams 
   w.issue(done);
 }
 
-template <typename T>
+template <typename T, int NT>
 cudaError_t launch_sample(const SampleParams& p, int64_t T_rows, int C, cudaStream_t st) {
-  auto kernel = dppo_sample_kernel<T>;
+  auto kernel = dppo_sample_kernel<T, NT>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SampleSmem));
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(T_rows * C));
-  cfg.blockDim = dim3(kSThreads);
+  cfg.blockDim = dim3(NT);
   cfg.dynamicSmemBytes = sizeof(SampleSmem);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
@@ -837,15 +1062,21 @@ extern "C" int dppo_sample(const void* logits, int64_t T, int64_t V, int64_t log
   cudaGetDevice(&dev);
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   const int64_t nvec = (V * es + 15) / 16 + 1;             // one more for a row that starts inside a vector
-  SampleParams p = {logits, V, logits_row_stride, uniform, temperature, top_p, min_p, top_k, token_mask, K,
-                    (int)((nvec + 32 * kSMaxChunks - 1) / (32 * kSMaxChunks)),
-                    sampled_ids, mu_logp, mu_topk_ids, mu_topk_p, status};
-  // few rows: several SMs share a row, as long as there are SMs and chunks enough for all of them
+  // few rows: several SMs share a row, as long as there are SMs and vectors enough for all of their warps
   int C = 1;
-  const int64_t chunks = (nvec + 32 * (int64_t)p.vecs - 1) / (32 * (int64_t)p.vecs);
-  while (C < kSMaxCluster && T * C * 2 <= sms && chunks >= 2 * C * kSWarps) C *= 2;
+  while (C < kSMaxCluster && T * C * 2 <= sms && nvec >= 64 * 2 * C * kSWarps) C *= 2;
+  // vectors per lane and chunk: at most kSMaxChunks chunks; four where a CTA has the row to itself and chunks enough
+  // (what a chunk costs besides its elements is spread over more of them), no more than needed where the row is shared
+  int vecs = (int)((nvec + 32 * kSMaxChunks - 1) / (32 * kSMaxChunks));
+  if (C == 1 && vecs < 4 && nvec >= 32 * 4 * 4 * kSWarps) vecs = 4;
+  SampleParams p = {logits, V, logits_row_stride, uniform, temperature, top_p, min_p, top_k, token_mask, K, vecs,
+                    sampled_ids, mu_logp, mu_topk_ids, mu_topk_p, status};
   if (T > INT32_MAX / C) return DPPO_ERR_SHAPE;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
-  const cudaError_t e = logits_dtype == DPPO_BF16 ? launch_sample<__nv_bfloat16>(p, T, C, st) : launch_sample<float>(p, T, C, st);
+  // a row to a CTA of 256 threads once there are more rows than SMs; 512 threads, on one SM or several, otherwise
+  const bool many = T > sms;
+  cudaError_t e;
+  if (logits_dtype == DPPO_BF16) e = many ? launch_sample<__nv_bfloat16, 256>(p, T, C, st) : launch_sample<__nv_bfloat16, 512>(p, T, C, st);
+  else e = many ? launch_sample<float, 256>(p, T, C, st) : launch_sample<float, 512>(p, T, C, st);
   return e == cudaSuccess ? DPPO_OK : DPPO_ERR_CUDA;
 }
