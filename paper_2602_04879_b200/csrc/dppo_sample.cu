@@ -84,7 +84,7 @@ struct SampleSmem {
     double pref[kSList];                  // then: running sums along the list
   };
   unsigned long long cfix[kSMaxChunks];   // kept weights of listed elements by chunk, in units of 2^-52
-  unsigned bins[kSBins];
+  alignas(16) unsigned bins[kSBins];
   float cmax[kSMaxChunks];
   float rec_z[kSMaxTop];
   int rec_id[kSMaxTop];
@@ -131,17 +131,41 @@ struct Exp2 {
     K = kMagic - R;
     log2_ref = R;
   }
-  template <bool FAR> __device__ __forceinline__ void parts(float z, int tab_hi, int tab_lo, double& p, double& s) const {
-    const double x = FAR ? (double)z - off : (double)z;
-    const double t = fma(x, c, K);
-    const double f = fma(x, c, -(t - K));
-    p = fma(f, 9.6181291076284772e-3, 5.5504108664821580e-2);     // ln2^4 / 24, ln2^3 / 6
-    p = fma(p, f, 2.4022650695910071e-1);                         // ln2^2 / 2
-    p = fma(p, f, 6.9314718055994531e-1);
-    p = fma(p, f, 1.0);
-    const int n = __double2loint(t);
-    const int hi = __shfl_sync(0xffffffffu, tab_hi, n), lo = __shfl_sync(0xffffffffu, tab_lo, n);
-    s = __hiloint2double(hi + ((n & ~31) << 15), lo);
+  // The same for a group of G logits at once, weight = q * s: step by step for all of them, because one chain of dependent 64-bit
+  // operations leaves the units idle most of the time.
+  template <bool FAR, int G> __device__ __forceinline__ void group(const float* z, int tab_hi, int tab_lo, double* q, double* s) const {
+    double f[G];
+    int n[G];
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+      const double x = FAR ? (double)z[i] - off : (double)z[i];
+      const double t = fma(x, c, K);
+      f[i] = fma(x, c, -(t - K));
+      n[i] = __double2loint(t);
+    }
+#pragma unroll
+    for (int i = 0; i < G; ++i) q[i] = fma(f[i], 9.6181291076284772e-3, 5.5504108664821580e-2);     // ln2^4 / 24, ln2^3 / 6
+#pragma unroll
+    for (int i = 0; i < G; ++i) q[i] = fma(q[i], f[i], 2.4022650695910071e-1);                     // ln2^2 / 2
+#pragma unroll
+    for (int i = 0; i < G; ++i) q[i] = fma(q[i], f[i], 6.9314718055994531e-1);
+#pragma unroll
+    for (int i = 0; i < G; ++i) q[i] = fma(q[i], f[i], 1.0);
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+      const int hi = __shfl_sync(0xffffffffu, tab_hi, n[i]), lo = __shfl_sync(0xffffffffu, tab_lo, n[i]);
+      s[i] = __hiloint2double(hi + ((n[i] & ~31) << 15), lo);
+    }
+  }
+  template <bool FAR> __device__ __forceinline__ void parts(float z, int tab_hi, int tab_lo, double& q, double& s) const {
+    group<FAR, 1>(&z, tab_hi, tab_lo, &q, &s);
+  }
+  // sum[i] += weight of z[i], add_group
+  template <bool FAR, int G, typename F> __device__ __forceinline__ void add_group(const float* z, int tab_hi, int tab_lo, double* sum, F take) const {
+    double q[G], s[G];
+    group<FAR, G>(z, tab_hi, tab_lo, q, s);
+#pragma unroll
+    for (int i = 0; i < G; ++i) if (take(i)) sum[i] = fma(q[i], s[i], sum[i]);
   }
 };
 
@@ -222,7 +246,7 @@ struct Worker {
   Exp2 eM;                                 // weights relative to (nearly) M; corr makes them relative to M
   bool far;
   double corr;
-  static constexpr int N = Row<T>::N;
+  static constexpr int N = Row<T>::N, kGroup = 4;
 
   __device__ __forceinline__ int tid() const { return threadIdx.x; }
   __device__ __forceinline__ int lane() const { return threadIdx.x & 31; }
@@ -298,12 +322,24 @@ struct Worker {
   }
   // sum over the elements that are worth counting and for which take(z, index) holds
   template <typename F> __device__ __forceinline__ double weigh(int ch, const Exp2& x, float low, F take) const {
-    double sum = 0.0;
-    each(ch, [&](float z, int j) {
-      double q, w;
-      x.parts<true>(fmaxf(z, low), tab_hi, tab_lo, q, w);
-      if (take(z, j) && z >= low) sum = fma(q, w, sum);
+    double sums[kGroup] = {};
+    vectors(ch, [&](const uint4* v, int s0, int n) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (k >= n) break;
+        float z[N], y[N];
+        Row<T>::unpack(v[k], z);
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] = fmaxf(z[e], low);
+        const int j0 = (s0 + k * 32) * N - row.head;
+#pragma unroll
+        for (int e = 0; e < N; e += kGroup)
+          x.template add_group<true, kGroup>(y + e, tab_hi, tab_lo, sums, [&](int i) { return take(z[e + i], j0 + e + i) && z[e + i] >= low; });
+      }
     });
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i) sum += sums[i];
     return warp_sum(sum);
   }
   // the same and the counts above three borders at once
@@ -324,22 +360,54 @@ struct Worker {
   // ---- pass A ----
   __device__ void pass_a(bool want_sum, bool want_groups) const {
     SampleSmem* lead = smem_of(0);
+    // Sums are of 2^(z c) as it stands where 2^(max z c) is well inside the range of doubles, so that maximum and sum come from one
+    // look at the elements; what lies below 2^-900 then counts as 2^-900.  Otherwise (set apart after the maximum is known) the
+    // chunk is summed relative to its maximum.
+    Exp2 plain;
+    bool far0;
+    double zero;
+    plain.set(c, 0.0, far0, zero);
+    const float floor0 = __double2float_ru(-0.9 * span), safe = (float)(0.8 * span);
     for (int ch = c_begin + warp(); ch < c_end; ch += NW) {
       float mx = -INFINITY;
-      vectors(ch, [&](const uint4* v, int, int n) {
+      double sum = 0.0, ref = 0.0, sums[kGroup] = {};
+      if (want_sum) {
+        vectors(ch, [&](const uint4* v, int, int n) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) if (k < n) mx = max_nan(mx, Row<T>::max_of(v[k]));
-      });
+          for (int k = 0; k < 4; ++k) {
+            if (k >= n) break;
+            mx = max_nan(mx, Row<T>::max_of(v[k]));
+            float z[N];
+            Row<T>::unpack(v[k], z);
+#pragma unroll
+            for (int e = 0; e < N; ++e) z[e] = fmaxf(z[e], floor0);
+#pragma unroll
+            for (int e = 0; e < N; e += kGroup) plain.add_group<false, kGroup>(z + e, tab_hi, tab_lo, sums, [](int) { return true; });
+          }
+        });
+      } else {
+        vectors(ch, [&](const uint4* v, int, int n) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) if (k < n) mx = max_nan(mx, Row<T>::max_of(v[k]));
+        });
+      }
       if (want_groups) lead->gmax[ch * 32 + lane()] = mx;
       const float cm = warp_max_nan(mx);
-      double sum = 0.0, ref = 0.0;
-      if (want_sum && cm > -INFINITY && cm < INFINITY) {
-        Exp2 x;
-        bool far_ch;
-        x.set(c, (double)cm, far_ch, ref);
-        const float low = low_of((double)cm);
-        sum = far_ch ? weigh_all<true>(ch, x, low) : weigh_all<false>(ch, x, low);
-        if (far_ch) ref = NAN;
+      if (want_sum) {
+        if (fabsf(cm) < safe) {
+#pragma unroll
+          for (int i = 0; i < kGroup; ++i) sum += sums[i];
+          sum = warp_sum(sum);
+        } else if (cm > -INFINITY && cm < INFINITY) {
+          Exp2 x;
+          bool far_ch;
+          x.set(c, (double)cm, far_ch, ref);
+          const float low = low_of((double)cm);
+          sum = far_ch ? weigh_all<true>(ch, x, low) : weigh_all<false>(ch, x, low);
+          if (far_ch) ref = NAN;
+        } else {
+          sum = 0.0;
+        }
       }
       if (lane() == 0) { lead->cmax[ch] = cm; lead->csum[ch] = sum; lead->cref[ch] = ref; }
     }
@@ -481,7 +549,10 @@ struct Worker {
     if (n <= NT) {                  // by rank: every entry counts those before it (all entries differ)
       const unsigned long long mine = tid() < n ? s.list[tid()] : 0;
       int r = 0;
-      if (tid() < n) for (int j = 0; j < n; ++j) r += s.list[j] < mine;
+      if (tid() < n) {
+#pragma unroll 16
+        for (int j = 0; j < n; ++j) r += s.list[j] < mine ? 1 : 0;
+      }
       __syncthreads();
       if (tid() < n) s.list[r] = mine;
       __syncthreads();
@@ -522,7 +593,9 @@ struct Worker {
       if (tid() < n) {
         const int me = list_id(tid());
         double run = 0.0;
-        for (int j = 0; j < n; ++j) if (list_id(j) <= me) run += s.pref[j] - (j ? s.pref[j - 1] : 0.0);
+        double before = 0.0;
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) { const double at = s.pref[j]; if (list_id(j) <= me) run += at - before; before = at; }
         if (run > target) best = me;
         last = me;
       }
@@ -737,7 +810,27 @@ struct Worker {
   __device__ bool make_list(int kk) const {
     uint32_t bound = kKeyNegInf + 1;
     const int G = nchunks * 32;
-    if (kk < G) {
+    if (kk * 10 <= nchunks * 9) {
+      // The kk-th largest chunk maximum: kk chunks hold an element that reaches it, and with n chunks alike about
+      // -n log(1 - kk / n) elements do.  Every chunk counts those before it; their numbers, in the place of the keys' last 8 bits
+      // (which the bound then lacks), keep equal ones apart.
+      static_assert(kSMaxChunks <= 256, "chunk numbers of 8 bits");
+      __syncthreads();
+      const uint32_t me = tid() < nchunks ? (key_of(s.cmax[tid()]) & ~255u) | (uint32_t)tid() : 0u;
+      if (tid() < kSMaxChunks) s.bins[tid()] = me;
+      __syncthreads();
+      if (tid() < nchunks) {
+        int r = 0;
+#pragma unroll 8
+        for (int i = 0; i < nchunks; i += 4) {
+          const uint4 x = *reinterpret_cast<const uint4*>(s.bins + i);
+          r += (int)(x.x > me) + (int)(x.y > me) + (int)(x.z > me) + (int)(x.w > me);
+        }
+        if (r == kk - 1) s.pick = (int)(me & ~255u);
+      }
+      __syncthreads();
+      bound = max(bound, (uint32_t)s.pick);
+    } else if (kk < G) {
       // A bound that at least kk group maxima reach and not many more, from an interval of values [lo, hi) that is cut in three at
       // a time (of keys now and then, which ends it whatever the values are).  The lowest chunk maximum is a lower end if there
       // are kk chunks; otherwise one is looked for in growing steps.
@@ -783,8 +876,10 @@ struct Worker {
     int* hits = reinterpret_cast<int*>(s.bins);
     if (tid() == 0) s.pick = 0;
     __syncthreads();
+    const float reach = of_key(bound);
+#pragma unroll 4
     for (int g = tid(); g < G; g += NT)
-      if (key_of(s.gmax[g]) >= bound) { const int at = atomicAdd(&s.pick, 1); if (at < kSBins) hits[at] = g; }
+      if (s.gmax[g] >= reach) { const int at = atomicAdd(&s.pick, 1); if (at < kSBins) hits[at] = g; }
     __syncthreads();
     const int n_hits = s.pick;
     if (n_hits > kSBins) return false;
@@ -835,9 +930,6 @@ __global__ void __launch_bounds__(NT, 512 / NT) dppo_sample_kernel(SampleParams 
   if (tau == 0.0) { tau = 1.0; k = 1; }
   const bool k_on = k > 0 && k < p.V, small_k = k_on && k <= kSMaxTop;
   const bool p_on = top_p < 1.0, m_on = min_p > 0.0;
-  int kk = p.K;
-  if (small_k) kk = max(kk, (int)k);
-  else if (p_on || m_on) kk = max(kk, kSProbe);
 
   const T* base = reinterpret_cast<const T*>(p.logits) + t * p.ld;
   RowView<T> row;
@@ -846,6 +938,9 @@ __global__ void __launch_bounds__(NT, 512 / NT) dppo_sample_kernel(SampleParams 
   row.head = (int)(((uintptr_t)base & 15) / sizeof(T));
   row.nvec = (int)(((int64_t)row.head + p.V + Row<T>::N - 1) / Row<T>::N);
   const int nchunks = (row.nvec + 32 * p.vecs - 1) / (32 * p.vecs), per = (nchunks + C - 1) / C;
+  int kk = p.K;                                      // length of the list that is asked for
+  if (small_k) kk = max(kk, (int)k);
+  else if (p_on || m_on) kk = max(kk, min(kSProbe, max(1, nchunks * 3 / 4)));
   Worker<T, NT> w = {p, s, row, nchunks, min(nchunks, rank * per), min(nchunks, (rank + 1) * per), rank, C, kLog2eD / tau, 1.0 / tau, 1000.0 * tau / kLog2eD};
 
   const double mine = exp2((double)(tid & 31) / 32.0);
