@@ -9,10 +9,11 @@
 // one multiplication by the rounded reciprocal and Markstein's correction step (P. Markstein, IBM J. Res. Dev. 34, 1990),
 // with the divisor scaled into [1, 2) first so that the remainder cannot underflow.
 //
-// Bounded by memory: 2 (or 4) bytes in, 1 byte out per orientation.  A CTA owns a tile of 128 columns and 16 R rows; each
-// thread holds an R x 8 block of it in registers, so the input is read once, whatever is written: row scales come from a
-// reduction over the 16 threads of a row, column scales (transposed form) from one over shared memory.  The transposed
-// bytes are turned round in shared memory, 8 x 8 bytes per thread, placed so that neither side collides on the banks.
+// Bounded by memory (2 or 4 bytes in, 1 byte out per orientation), and close behind it by instructions.  A CTA owns a tile of 128
+// columns and 16 R rows; each thread holds an R x 8 block of it in registers, so the input is read once, whatever is written: row
+// maxima come from the 16 threads of a row, column maxima (transposed form) from shared memory; one thread per row and one per column
+// then works out the scale; products and corrections go in packed fp32 pairs.  The transposed bytes are turned round in shared
+// memory, 8 x 8 bytes per thread, placed so that neither side collides on the banks.
 #include <cuda_fp8.h>
 
 #include "dppo_common.cuh"
@@ -25,7 +26,7 @@ constexpr int kQThreads = 256;
 struct QuantParams {
   const void* x;
   int64_t rows, cols, ldx;
-  int block_rows, e5m2, vec;       // vec: 16-byte loads allowed (aligned base and row stride)
+  int block_rows, vec;             // vec: 16-byte loads allowed (aligned base and row stride)
   uint8_t* q;
   int64_t ldq;
   float* scale;
@@ -39,34 +40,25 @@ struct QuantParams {
   int64_t col_tiles;
 };
 
-// What turns an element of a block into its 8-bit value: num = x f, q = num / b.
-struct BlockScale {
-  float f, b, r;                   // f = 7/8 2^(n - e), b = amax 2^-e in [1, 2), r = 1 / b
-  int bad;
-};
-__device__ __forceinline__ BlockScale block_scale(uint32_t amax_bits, int e5m2, float& scale) {
-  BlockScale s;
-  s.bad = amax_bits >= 0x7f800000u;                          // an infinity or a NaN in the block
-  const float amax = fmaxf(__uint_as_float(s.bad ? 0x3f800000u : amax_bits), 0x1p-100f);
-  scale = s.bad ? __int_as_float(0x7fffffff) : __fdiv_rn(amax, e5m2 ? 57344.f : 448.f);
+// What turns an element of a block into its 8-bit value: num = x f, q = num / b; f = 7/8 2^(n - e), b = amax 2^-e in [1, 2), r = 1 / b
+// (kept: f, -b, r and the scale).
+// A block with an infinity or a NaN has f = NaN: all its values, and its scale, come out as NaN.
+template <bool E5M2> __device__ __forceinline__ float4 block_scale(uint32_t amax_bits) {
+  if (amax_bits >= 0x7f800000u) { const float nan = __int_as_float(0x7fffffff); return make_float4(nan, -1.f, 1.f, nan); }
+  const float amax = fmaxf(__uint_as_float(amax_bits), 0x1p-100f);
   const int e = (int)(__float_as_uint(amax) >> 23) - 127;    // amax is a normal number
-  s.b = __uint_as_float((__float_as_uint(amax) & 0x007fffffu) | 0x3f800000u);
-  s.r = __frcp_rn(s.b);
-  s.f = 0.875f * __uint_as_float((uint32_t)((e5m2 ? 16 : 9) - e + 127) << 23);
-  return s;
+  const float b = __uint_as_float((__float_as_uint(amax) & 0x007fffffu) | 0x3f800000u);
+  return make_float4(0.875f * __uint_as_float((uint32_t)((E5M2 ? 16 : 9) - e + 127) << 23), -b, __frcp_rn(b), __fdiv_rn(amax, E5M2 ? 57344.f : 448.f));
 }
-__device__ __forceinline__ float quotient(float x, const BlockScale& s) {
-  const float num = x * s.f, q = num * s.r;
-  return fmaf(fmaf(-q, s.b, num), s.r, q);
-}
-__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d, int e5m2) {
-  const __nv_fp8_interpretation_t t = e5m2 ? __NV_E5M2 : __NV_E4M3;
-  const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, t);
-  const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, t);
-  return lo | (hi << 16);
+// two elements of blocks with the same scale, as two bytes
+template <bool E5M2> __device__ __forceinline__ uint32_t round2(float x, float y, const float4& s) {
+  const float2 num = __fmul2_rn(make_float2(x, y), make_float2(s.x, s.x)), r = make_float2(s.z, s.z);
+  float2 q = __fmul2_rn(num, r);
+  q = __ffma2_rn(__ffma2_rn(q, make_float2(s.y, s.y), num), r, q);
+  return __nv_cvt_float2_to_fp8x2(q, __NV_SATFINITE, E5M2 ? __NV_E5M2 : __NV_E4M3);
 }
 
-// Eight consecutive elements of one row, as loaded.
+// Eight consecutive elements of one row, as loaded; Max: their magnitudes' running maximum, NaNs and infinities above all else.
 template <typename T> struct Oct;
 template <> struct Oct<__nv_bfloat16> {
   uint4 v;
@@ -80,6 +72,15 @@ template <> struct Oct<__nv_bfloat16> {
     const uint32_t w = (&v.x)[i >> 1];
     return __uint_as_float((i & 1) ? (w & 0xffff0000u) : (w << 16));
   }
+  static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {         // of two pairs of magnitudes
+    const __nv_bfloat162 m = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&m);
+  }
+  __device__ __forceinline__ uint32_t pair(int k) const { return (&v.x)[k] & 0x7fff7fffu; }
+  __device__ __forceinline__ uint32_t row_max() const {      // as fp32 bits
+    const uint32_t m = max2(max2(pair(0), pair(1)), max2(pair(2), pair(3)));
+    return max(m << 16, m & 0xffff0000u);
+  }
 };
 template <> struct Oct<float> {
   float4 a, b;
@@ -90,131 +91,161 @@ template <> struct Oct<float> {
   }
   __device__ __forceinline__ void put(int i, float x) { if (i < 4) (&a.x)[i] = x; else (&b.x)[i - 4] = x; }
   __device__ __forceinline__ float at(int i) const { return i < 4 ? (&a.x)[i] : (&b.x)[i - 4]; }
+  __device__ __forceinline__ uint32_t mag(int i) const { return __float_as_uint(at(i)) & 0x7fffffffu; }
+  __device__ __forceinline__ uint32_t row_max() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, mag(j));
+    return m;
+  }
 };
-__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+// maxima of eight columns over R rows, as fp32 bits
+template <int R> __device__ __forceinline__ void col_max(const Oct<__nv_bfloat16>* v, uint32_t* m) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    uint32_t x = v[0].pair(k);
+#pragma unroll
+    for (int i = 1; i < R; ++i) x = Oct<__nv_bfloat16>::max2(x, v[i].pair(k));
+    m[2 * k] = x << 16;
+    m[2 * k + 1] = x & 0xffff0000u;
+  }
+}
+template <int R> __device__ __forceinline__ void col_max(const Oct<float>* v, uint32_t* m) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    uint32_t x = 0;
+#pragma unroll
+    for (int i = 0; i < R; ++i) x = max(x, v[i].mag(j));
+    m[j] = x;
+  }
+}
 
 // R rows per thread: 8 for whole 128 x 128 tiles (needed for 128 x 128 blocks and for the transposed form), less otherwise.
-template <typename T, int R>
+template <typename T, int R, bool E5M2>
 __global__ void __launch_bounds__(kQThreads) dppo_quantize_kernel(QuantParams p) {
-  __shared__ uint32_t colmax[R == 8 ? 8 : 1][128];
+  static_assert(R == 8 || R == 1, "rows per thread");
+  constexpr bool kTile = R == 8;
+  __shared__ __align__(16) uint32_t colmax[kTile ? 8 : 1][kTile ? 128 : 4];
+  __shared__ float4 row_s[16 * R], col_s[kTile ? 128 : 1];
   __shared__ uint32_t blockmax[8];
-  __shared__ __align__(16) unsigned char tile[R == 8 ? 128 * 128 : 16];
+  __shared__ __align__(16) unsigned char tile[kTile ? 128 * 128 : 16];
   const int tid = threadIdx.x, cg = tid & 15, rg = tid >> 4, warp = tid >> 5;
   const int64_t rt = blockIdx.x / p.col_tiles, ct = blockIdx.x - rt * p.col_tiles;
   const int64_t r0 = rt * (16 * R) + rg * R, c0 = ct * 128 + cg * 8;      // this thread's block
   const T* x = reinterpret_cast<const T*>(p.x);
   Oct<T> v[R];
+  const bool inner = p.vec && c0 + 8 <= p.cols && r0 + R <= p.rows;
+  if (inner) {
+    const T* src = x + r0 * p.ldx + c0;
 #pragma unroll
-  for (int i = 0; i < R; ++i) {
-    v[i].zero();
-    const int64_t r = r0 + i;
-    if (r < p.rows) {
-      const T* src = x + r * p.ldx + c0;
-      if (p.vec && c0 + 8 <= p.cols) {
-        v[i].load(src);
-      } else {
+    for (int i = 0; i < R; ++i) v[i].load(src + i * p.ldx);
+  } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) if (c0 + j < p.cols) v[i].put(j, src[j]);
+    for (int i = 0; i < R; ++i) {
+      v[i].zero();
+      if (r0 + i < p.rows) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) if (c0 + j < p.cols) v[i].put(j, x[(r0 + i) * p.ldx + c0 + j]);
       }
     }
   }
-  uint32_t rowmax[R];
+  bool bad = false;
+  const bool whole = kTile && p.block_rows == 128;           // one scale for the tile
+  if (whole || p.q) {
+    uint32_t m[R];
 #pragma unroll
-  for (int i = 0; i < R; ++i) {
-    uint32_t m = 0;
+    for (int i = 0; i < R; ++i) m[i] = v[i].row_max();
+    if (whole) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v[i].at(j)));
-    rowmax[i] = m;
+      for (int i = 1; i < R; ++i) m[0] = max(m[0], m[i]);
+      m[0] = __reduce_max_sync(0xffffffffu, m[0]);
+      if ((tid & 31) == 0) blockmax[warp] = m[0];
+    } else {
+      // maxima over the 16 threads of a row, rows shared out on the way: with R = 8, thread cg ends up with row cg / 2
+      int row = 0;
+#pragma unroll
+      for (int n = R / 2, o = 8; n > 0; n >>= 1, o >>= 1) {
+        const bool up = cg & o;
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+          const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? m[i] : m[i + n], o);
+          m[i] = max(up ? m[i + n] : m[i], got);
+        }
+        row += up ? n : 0;
+      }
+#pragma unroll
+      for (int o = R == 8 ? 1 : 8; o > 0; o >>= 1) m[0] = max(m[0], __shfl_xor_sync(0xffffffffu, m[0], o));
+      const float4 s = block_scale<E5M2>(m[0]);
+      bad |= s.w != s.w;
+      if ((cg & (16 / R - 1)) == 0) {
+        row_s[rg * R + row] = s;
+        if (r0 + row < p.rows) p.scale[(r0 + row) * p.s_row + ct * p.s_k] = s.w;
+      }
+    }
   }
-  int bad = 0;
-  BlockScale bs = {};
-  float block_value = 0.f;
-  if (R == 8 && p.block_rows == 128) {
-    uint32_t m = 0;
+  if (kTile && p.qt && !whole) {
+    uint32_t m[8];
+    col_max<R>(v, m);
 #pragma unroll
-    for (int i = 0; i < R; ++i) m = max(m, rowmax[i]);
-    m = __reduce_max_sync(0xffffffffu, m);
-    if ((tid & 31) == 0) blockmax[warp] = m;
-    __syncthreads();
-    m = 0;
+    for (int j = 0; j < 8; ++j) m[j] = max(m[j], __shfl_xor_sync(0xffffffffu, m[j], 16));
+    if ((tid & 31) < 16) {
+      uint4* dst = reinterpret_cast<uint4*>(&colmax[kTile ? warp : 0][kTile ? cg * 8 : 0]);
+      dst[0] = make_uint4(m[0], m[1], m[2], m[3]);
+      dst[kTile ? 1 : 0] = make_uint4(m[4], m[5], m[6], m[7]);
+    }
+  }
+  __syncthreads();
+  float4 bs = make_float4(0.f, -1.f, 1.f, 0.f);
+  if (whole) {
+    uint32_t m = 0;
 #pragma unroll
     for (int w = 0; w < 8; ++w) m = max(m, blockmax[w]);
-    bs = block_scale(m, p.e5m2, block_value);
-    bad |= bs.bad;
+    bs = block_scale<E5M2>(m);
+    bad |= bs.w != bs.w;
     if (tid == 0) {
-      if (p.q) p.scale[rt * p.s_row + ct * p.s_k] = block_value;
-      if (p.qt) p.scale_t[ct * p.st_row + rt * p.st_k] = block_value;
+      if (p.q) p.scale[rt * p.s_row + ct * p.s_k] = bs.w;
+      if (p.qt) p.scale_t[ct * p.st_row + rt * p.st_k] = bs.w;
     }
+  } else if (kTile && p.qt) {
+    if (tid < 128) {                                         // a thread per column
+      uint32_t m = 0;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) m = max(m, colmax[kTile ? w : 0][kTile ? tid : 0]);
+      const float4 s = block_scale<E5M2>(m);
+      col_s[kTile ? (tid & ~7) | ((tid ^ (tid >> 3)) & 7) : 0] = s;       // (place: the readers take every eighth column at a time)
+      bad |= s.w != s.w;
+      if (ct * 128 + tid < p.cols) p.scale_t[(ct * 128 + tid) * p.st_row + rt * p.st_k] = s.w;
+    }
+    __syncthreads();
   }
   if (p.q) {
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-      BlockScale s = bs;
-      if (p.block_rows == 1) {
-        uint32_t m = rowmax[i];
+      const float4 s = whole ? bs : row_s[rg * R + i];
+      uint32_t o[4];
 #pragma unroll
-        for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-        float sv;
-        s = block_scale(m, p.e5m2, sv);
-        bad |= s.bad;
-        if (cg == 0 && r0 + i < p.rows) p.scale[(r0 + i) * p.s_row + ct * p.s_k] = sv;
-      }
-      float y[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = quotient(v[i].at(j), s);
-      uint2 o = make_uint2(pack4(y[0], y[1], y[2], y[3], p.e5m2), pack4(y[4], y[5], y[6], y[7], p.e5m2));
-      if (s.bad) o = make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);
+      for (int j = 0; j < 4; ++j) o[j] = round2<E5M2>(v[i].at(2 * j), v[i].at(2 * j + 1), s);
+      const uint2 b = make_uint2(o[0] | (o[1] << 16), o[2] | (o[3] << 16));
       if (r0 + i < p.rows) {
         uint8_t* dst = p.q + (r0 + i) * p.ldq + c0;
         if (p.qvec && c0 + 8 <= p.cols) {
-          *reinterpret_cast<uint2*>(dst) = o;
+          *reinterpret_cast<uint2*>(dst) = b;
         } else {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) if (c0 + j < p.cols) dst[j] = (uint8_t)((j < 4 ? o.x : o.y) >> (8 * (j & 3)));
+          for (int j = 0; j < 8; ++j) if (c0 + j < p.cols) dst[j] = (uint8_t)((j < 4 ? b.x : b.y) >> (8 * (j & 3)));
         }
       }
     }
   }
-  if (R == 8 && p.qt) {
-    BlockScale s = bs;
-    if (p.block_rows == 1) {
-      uint32_t cm[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int i = 0; i < R; ++i) m = max(m, abs_bits(v[i].at(j)));
-        cm[j] = max(m, __shfl_xor_sync(0xffffffffu, m, 16));
-      }
-      if ((tid & 31) < 16) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) colmax[R == 8 ? warp : 0][cg * 8 + j] = cm[j];
-      }
-      __syncthreads();
-      // one thread per column: its scale, and what the column's threads need of it
-      if (tid < 128) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int w = 0; w < 8; ++w) m = max(m, colmax[R == 8 ? w : 0][tid]);
-        colmax[0][tid] = m;
-      }
-      __syncthreads();
-    }
+  if (kTile && p.qt) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int c = cg * 8 + j;
-      if (p.block_rows == 1) {
-        float sv;
-        s = block_scale(colmax[0][c], p.e5m2, sv);
-        bad |= s.bad;
-        if (rg == 0 && c0 + j < p.cols) p.scale_t[(c0 + j) * p.st_row + rt * p.st_k] = sv;
-      }
-      float y[8];
+      const float4 s = whole ? bs : col_s[kTile ? cg * 8 + ((j ^ cg) & 7) : 0];
+      uint32_t o[4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = quotient(v[R == 8 ? i : 0].at(j), s);
-      uint2 o = make_uint2(pack4(y[0], y[1], y[2], y[3], p.e5m2), pack4(y[4], y[5], y[6], y[7], p.e5m2));
-      if (s.bad) o = make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);
-      *reinterpret_cast<uint2*>(tile + c * 128 + ((rg ^ (c >> 3)) * 8)) = o;
+      for (int i = 0; i < 4; ++i) o[i] = round2<E5M2>(v[kTile ? 2 * i : 0].at(j), v[kTile ? 2 * i + 1 : 0].at(j), s);
+      *reinterpret_cast<uint2*>(tile + (kTile ? c * 128 + ((rg ^ (c >> 3)) * 8) : 0)) = make_uint2(o[0] | (o[1] << 16), o[2] | (o[3] << 16));
     }
     __syncthreads();
     const int64_t row0 = rt * 128 + cg * 8;                  // first of the eight input rows of this thread's piece
@@ -223,7 +254,7 @@ __global__ void __launch_bounds__(kQThreads) dppo_quantize_kernel(QuantParams p)
       const int c = i * 16 + rg;
       const int64_t col = ct * 128 + c;
       if (col < p.cols) {
-        const uint2 o = *reinterpret_cast<const uint2*>(tile + c * 128 + ((cg ^ (c >> 3)) * 8));
+        const uint2 o = *reinterpret_cast<const uint2*>(tile + (kTile ? c * 128 + ((cg ^ (c >> 3)) * 8) : 0));
         uint8_t* dst = p.qt + col * p.ldqt + row0;
         if (p.qtvec && row0 + 8 <= p.rows) {
           *reinterpret_cast<uint2*>(dst) = o;
@@ -237,17 +268,17 @@ __global__ void __launch_bounds__(kQThreads) dppo_quantize_kernel(QuantParams p)
   if (bad) atomicOr(p.status, DPPO_STATUS_NONFINITE_ROW);
 }
 
-template <typename T>
+template <typename T, bool E5M2>
 cudaError_t launch_quantize(QuantParams p, cudaStream_t st) {
   p.col_tiles = (p.cols + 127) / 128;
   if (p.qt || p.block_rows == 128) {
     const int64_t grid = p.col_tiles * ((p.rows + 127) / 128);
     if (grid > INT32_MAX) return cudaErrorInvalidValue;
-    dppo_quantize_kernel<T, 8><<<(unsigned)grid, kQThreads, 0, st>>>(p);
+    dppo_quantize_kernel<T, 8, E5M2><<<(unsigned)grid, kQThreads, 0, st>>>(p);
   } else {
     const int64_t grid = p.col_tiles * ((p.rows + 15) / 16);
     if (grid > INT32_MAX) return cudaErrorInvalidValue;
-    dppo_quantize_kernel<T, 1><<<(unsigned)grid, kQThreads, 0, st>>>(p);
+    dppo_quantize_kernel<T, 1, E5M2><<<(unsigned)grid, kQThreads, 0, st>>>(p);
   }
   return cudaGetLastError();
 }
@@ -280,7 +311,7 @@ extern "C" int dppo_fp8_quantize(const void* x, int64_t rows, int64_t cols, int6
   const int es = x_dtype == DPPO_BF16 ? 2 : 4;
   if (((uintptr_t)x % es) || ((uintptr_t)q_scale % 4) || ((uintptr_t)qt_scale % 4)) return DPPO_ERR_ALIGN;
   QuantParams p = {};
-  p.x = x; p.rows = rows; p.cols = cols; p.ldx = x_row_stride; p.block_rows = block_rows; p.e5m2 = fp8_format == DPPO_E5M2;
+  p.x = x; p.rows = rows; p.cols = cols; p.ldx = x_row_stride; p.block_rows = block_rows;
   p.vec = ((uintptr_t)x % 16) == 0 && (x_row_stride * es) % 16 == 0;
   p.q = reinterpret_cast<uint8_t*>(q); p.ldq = q_row_stride; p.scale = q_scale; p.s_row = q_scale_row_stride; p.s_k = q_scale_k_stride;
   p.qt = reinterpret_cast<uint8_t*>(qt); p.ldqt = qt_row_stride; p.scale_t = qt_scale; p.st_row = qt_scale_row_stride; p.st_k = qt_scale_k_stride;
@@ -288,6 +319,8 @@ extern "C" int dppo_fp8_quantize(const void* x, int64_t rows, int64_t cols, int6
   p.qvec = ((uintptr_t)q % 8) == 0 && q_row_stride % 8 == 0;
   p.qtvec = ((uintptr_t)qt % 8) == 0 && qt_row_stride % 8 == 0;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
-  const cudaError_t e = x_dtype == DPPO_BF16 ? launch_quantize<__nv_bfloat16>(p, st) : launch_quantize<float>(p, st);
+  cudaError_t e;
+  if (fp8_format == DPPO_E5M2) e = x_dtype == DPPO_BF16 ? launch_quantize<__nv_bfloat16, true>(p, st) : launch_quantize<float, true>(p, st);
+  else e = x_dtype == DPPO_BF16 ? launch_quantize<__nv_bfloat16, false>(p, st) : launch_quantize<float, false>(p, st);
   return e == cudaSuccess ? DPPO_OK : DPPO_ERR_CUDA;
 }
