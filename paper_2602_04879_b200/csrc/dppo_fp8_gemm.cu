@@ -118,7 +118,6 @@ __device__ __forceinline__ uint32_t elect_one() {
 }
 // named barriers: promotion warps and one helper warp; one of each kind per P_kb buffer
 constexpr int BAR_THREADS = PROMO_WARPS * 32 + 32;
-__device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 __device__ __forceinline__ void full_sync(uint32_t b) {
   if (b) asm volatile("barrier.cta.sync 4, %0;" ::"n"(BAR_THREADS) : "memory"); else asm volatile("barrier.cta.sync 3, %0;" ::"n"(BAR_THREADS) : "memory");
 }
@@ -353,9 +352,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tn_fp8_kernel(const __grid_co
         float* part_sums = reinterpret_cast<float*>(smem) + (q * 32) * PART_PITCH + part * COLS;
 #pragma unroll
         for (int j = 0; j < COLS / 2; ++j) *reinterpret_cast<float2*>(part_sums + pair_row(j) * PART_PITCH + pair_col(j)) = acc[j];
-      } else if (!live) {
-        continue;
-      } else if (p.tma_store) {
+      } else if (live) {
         // Blocks of 32 rows x 128 bytes (32 fp32 or 64 bf16 columns), 16-byte pieces placed by the 128-byte swizzle, two of them in
         // the warp's 8 KB at a time: one wait for the stores before, one proxy fence.  (Rows of 64 bytes took the copy engine,
         // which the operand loads need too, twice as long.)
@@ -363,7 +360,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tn_fp8_kernel(const __grid_co
 #pragma unroll
         for (int g = 0; g < 2; ++g) {                // bf16: all four quarters of the columns at once; fp32: two and two
           if (g == 1 && p.c_bf16) break;
-          if (lane == 0) gemm::bulk_wait_read<0>();
+          if (p.tma_store && lane == 0) gemm::bulk_wait_read<0>();
           __syncwarp();
           if (p.c_bf16) {
 #pragma unroll
@@ -384,30 +381,35 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tn_fp8_kernel(const __grid_co
               else st128(at, __float_as_uint(acc[j].x), __float_as_uint(acc[j].y), __float_as_uint(acc[j + 1].x), __float_as_uint(acc[j + 1].y));
             }
           }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) {
-            for (int c = 0; c < 2; ++c) {
-              const int col = n0 + (2 * g + c) * ncol;
-              if (col < n_end) gemm::tma_store_2d(&map_c, wbuf + c * 4096u, col, m0);
+          if (p.tma_store) {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+              for (int c = 0; c < 2; ++c) {
+                const int col = n0 + (2 * g + c) * ncol;
+                if (col < n_end) gemm::tma_store_2d(&map_c, wbuf + c * 4096u, col, m0);
+              }
+              gemm::bulk_commit();
             }
-            gemm::bulk_commit();
-          }
-        }
-      } else {
+          } else {
+            // a C that no tensor map describes (its rows do not start on 16-byte boundaries): the blocks' rows by plain stores of
+            // adjacent elements
+            __syncwarp();
+            const unsigned char* blocks = out_stage + (warp - 4) * 8192;
+            const int rows = min(32, p.M - m0);
+            for (int r = 0; r < rows; ++r) {
 #pragma unroll
-        for (int j = 0; j < COLS / 2; ++j) {
-          const int row = m0 + pair_row(j), col = n0 + pair_col(j);
-          if (row < p.M) {
-            const int64_t at = (int64_t)row * p.ldc + col;
-            if (p.c_bf16) {
-              __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.C) + at;
-              if (col < n_end) dst[0] = __float2bfloat16_rn(acc[j].x);
-              if (col + 1 < n_end) dst[1] = __float2bfloat16_rn(acc[j].y);
-            } else {
-              float* dst = reinterpret_cast<float*>(p.C) + at;
-              if (col < n_end) dst[0] = acc[j].x;
-              if (col + 1 < n_end) dst[1] = acc[j].y;
+              for (int i = 0; i < 4; ++i) {
+                if (i >= 2 && !p.c_bf16) break;
+                const int in = i * 32 + lane, col = n0 + 2 * g * ncol + in;      // bf16: 128 columns, fp32: 64
+                if (col >= n_end) continue;
+                const unsigned char* src = blocks + (in / ncol) * 4096 + r * 128;
+                const int byte = (in % ncol) * (p.c_bf16 ? 2 : 4);
+                src += (((byte >> 4) ^ (r & 7)) << 4) | (byte & 15);
+                const int64_t at = (int64_t)(m0 + r) * p.ldc + col;
+                if (p.c_bf16) reinterpret_cast<unsigned short*>(p.C)[at] = *reinterpret_cast<const unsigned short*>(src);
+                else reinterpret_cast<float*>(p.C)[at] = *reinterpret_cast<const float*>(src);
+              }
             }
           }
         }

@@ -119,6 +119,16 @@ def test_a_row_does_not_depend_on_how_many_share_the_call():
         assert all(torch.equal(part[n], again[n]) for n in part)
 
 
+def test_more_rows_than_sms():
+    """Above 148 rows a CTA has fewer threads and a row to itself: the same ids as when SMs share the rows."""
+    for V, dtype in ((151936, torch.bfloat16), (4097, torch.float32)):
+        z, u, s = _rows(300, V, dtype, seed=6), _uniform(300, 6), _settings(300, 6, "tkP")
+        whole = _on_gpu(z, u, 30, s)
+        part = _on_gpu(z[200:260], u[200:260], 30, {n: v[200:260] for n, v in s.items()})
+        assert torch.equal(part["sampled_ids"], whole["sampled_ids"][200:260]) and torch.equal(part["mu_topk_ids"], whole["mu_topk_ids"][200:260])
+        _check(whole, z, u, 30, s, rows=range(0, 300, 7))
+
+
 NEG = float("-inf")
 
 
