@@ -148,18 +148,28 @@ __device__ __forceinline__ void promote_rows(float2* acc, const uint32_t* r, flo
 #pragma unroll
   for (int j = 0; j < 32; ++j) acc[j] = __ffma2_rn(make_float2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1])), s2, acc[j]);
 }
-// acc += s0, s1 (the two rows) * sb (the columns') * r: a fragment of 16 rows x 64 columns.  The thread needs only every fourth pair
+// Reads a fragment of 16 rows x 64 columns (LAST: of buffer b); acc += s0, s1 (the two rows) * sb (the columns') * fragment.  The thread needs only every fourth pair
 // of the column scales: read by one row per thread, each warp would fetch all 128 of them for every block, and the shared
 // memory's 128 bytes a cycle would be what bounds the kernel.
-__device__ __forceinline__ void promote_fragment(float2* acc, const uint32_t* r, float s0, float s1, const float* sb) {
-  const float2 a0 = make_float2(s0, s0), a1 = make_float2(s1, s1);
+// (The products of the scales are formed before the fragment is waited for.)
+template <bool LAST> __device__ __forceinline__ void read_and_promote(uint32_t taddr, float2* acc, float s0, float s1, const float* sb, uint32_t b) {
+  float2 w0[8], w1[8];
 #pragma unroll
   for (int g = 0; g < 8; ++g) {
     const float2 w = *reinterpret_cast<const float2*>(sb + 8 * g);
-    const float2 u = __fmul2_rn(make_float2(__uint_as_float(r[4 * g]), __uint_as_float(r[4 * g + 1])), w);
-    const float2 v = __fmul2_rn(make_float2(__uint_as_float(r[4 * g + 2]), __uint_as_float(r[4 * g + 3])), w);
-    acc[2 * g] = __ffma2_rn(u, a0, acc[2 * g]);
-    acc[2 * g + 1] = __ffma2_rn(v, a1, acc[2 * g + 1]);
+    w0[g] = __fmul2_rn(w, make_float2(s0, s0));
+    w1[g] = __fmul2_rn(w, make_float2(s1, s1));
+  }
+  uint32_t r[32];
+  read_fragment(taddr, r);
+  if (LAST) {                              // buffer b read
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    empty_arrive(b);
+  }
+#pragma unroll
+  for (int g = 0; g < 8; ++g) {
+    acc[2 * g] = __ffma2_rn(make_float2(__uint_as_float(r[4 * g]), __uint_as_float(r[4 * g + 1])), w0[g], acc[2 * g]);
+    acc[2 * g + 1] = __ffma2_rn(make_float2(__uint_as_float(r[4 * g + 2]), __uint_as_float(r[4 * g + 3])), w1[g], acc[2 * g + 1]);
   }
 }
 
@@ -314,7 +324,6 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tn_fp8_kernel(const __grid_co
       for (int kb = 0; kb < kblocks; ++kb, ++it) {
         const uint32_t b = it & 1u, taddr = tmem_base + ((uint32_t)(q * 32) << 16) + b * BN + part * COLS;
         const float* sc = sring + (it % SRING) * SCALES;
-        uint32_t r[64];
         full_sync(b);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         if (B_ROW_SCALES) {
@@ -322,19 +331,14 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tn_fp8_kernel(const __grid_co
           const float* sr = sc + (p.a_shift ? 0 : q * 32 + (lane >> 2));
           const int r8 = p.a_shift ? 0 : 8;
           const float s0 = sr[0], s1 = sr[r8];
-          read_fragment(taddr, r);
-          promote_fragment(acc, r, s0, s1, sv);
-          read_fragment(taddr + 64, r);
-          promote_fragment(acc + 16, r, s0, s1, sv + 64);
+          read_and_promote<false>(taddr, acc, s0, s1, sv, b);
+          read_and_promote<false>(taddr + 64, acc + 16, s0, s1, sv + 64, b);
           const float s2 = sr[2 * r8], s3 = sr[3 * r8];
-          read_fragment(taddr + (16u << 16), r);
-          promote_fragment(acc + 32, r, s2, s3, sv);
-          read_fragment(taddr + 64 + (16u << 16), r);
-          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-          empty_arrive(b);                           // buffer read
-          promote_fragment(acc + 48, r, s2, s3, sv + 64);
+          read_and_promote<false>(taddr + (16u << 16), acc + 32, s2, s3, sv, b);
+          read_and_promote<true>(taddr + 64 + (16u << 16), acc + 48, s2, s3, sv + 64, b);
         } else {
           const float sa = sc[p.a_shift ? 0 : q * 32 + lane], sb = sc[BM + part];
+          uint32_t r[64];
           read_rows(taddr, r);
           const float x = sa * sb;
           promote_rows(acc, r, x);
