@@ -17,7 +17,7 @@
 //   list      the kk-th largest group maximum bounds the kk-th largest element from below, and only the few groups whose
 //             maximum reaches it can hold one of the kk largest: those groups alone are read again, and what passes the bound
 //             is sorted in shared memory.  This is all that top-k and the top-K record need.
-//   search    for cuts that lie below the list (top-p over a broad row, top_k > 1024): a histogram of the row over steps of 1/16
+//   search    for cuts that lie below the list (top-p over a broad row, top_k > 1024): a histogram of the row over steps of 1/32
 //             octave of weight tells where the cut should be; a second pass sums exactly what lies above that neighbourhood and
 //             lists what lies in it.  Where that misses, or thousands of equal logits meet the cut, the cut is bracketed by passes
 //             with three pivots at a time until it is found.
@@ -62,7 +62,7 @@ struct SampleParams {
 };
 
 enum { OP_DONE = 0, OP_PIVOTS, OP_COMPACT, OP_EQUAL, OP_CDF, OP_HIST, OP_SPLIT };
-constexpr int kSBins = 1024;           // histogram: steps of 1/16 octave of weight below the maximum, 64 octaves
+constexpr int kSBins = 2048;           // histogram: steps of 1/32 octave of weight below the maximum, 64 octaves
 struct Cmd {
   int op;
   uint32_t lo, hi;       // OP_COMPACT: keys [lo, hi)
@@ -413,7 +413,7 @@ struct Worker {
     }
   }
 
-  // which step of 1/16 octave of weight below the maximum (a monotone function of z)
+  // which step of 1/32 octave of weight below the maximum (a monotone function of z)
   __device__ __forceinline__ int bin_of(float z, float scale) const { return (int)fmaxf(0.f, fminf(((float)M - z) * scale, (float)(kSBins - 1))); }
   // smallest float (above -inf) that falls into a bin below b; +inf if there is none
   __device__ float border(int b) const {
@@ -424,7 +424,7 @@ struct Worker {
     }
     return of_key(hi);
   }
-  __device__ __forceinline__ float bin_scale() const { return (float)(16.0 * c); }
+  __device__ __forceinline__ float bin_scale() const { return (float)(32.0 * c); }
 
   // ---- passes that the leader asks for ----
   __device__ void execute(const Cmd& k) const {
@@ -673,7 +673,7 @@ struct Worker {
       const int b = tid() * kPer + i;
       unsigned c_ = 0;
       for (int r = 0; r < C; ++r) c_ += smem_of(r)->bins[b];
-      w[i] = by_mass ? (double)c_ * exp2(-((double)b + 0.5) / 16.0) : (double)c_;
+      w[i] = by_mass ? (double)c_ * exp2(-((double)b + 0.5) / 32.0) : (double)c_;
       sum += w[i];
     }
     double total;
