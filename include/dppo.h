@@ -336,7 +336,7 @@ int dppo_exact_divergence(const void* logits, const void* mu_logits, int64_t T, 
  * drawn and never kept.
  *
  *  logits         [T, V] row-major, row stride in elements (>= V; rows may start at any element), DPPO_F32 or DPPO_BF16;
- *                 V < 2^31.
+ *                 V <= 2^30.
  *  uniform        [T] double in [0, 1): one random number per row (8-byte aligned).  Doubles, because an fp32 uniform's steps
  *                 of 2^-24 are coarser than the probabilities in the tail of a large vocabulary.
  *  temperature    [T] fp32 >= 0, finite; NULL = 1 for all rows.        top_k   [T] int32; NULL = off.
@@ -348,7 +348,7 @@ int dppo_exact_divergence(const void* logits, const void* mu_logits, int64_t T, 
  *  mu_topk_p      [T, K] out: their mu (0 for tokens that are not kept).  Both may be NULL when K == 0.
  *  status         device word: DPPO_STATUS_NONFINITE_ROW (a NaN or +inf logit, or nothing but -inf), DPPO_STATUS_BAD_SAMPLING
  *                 (a setting or the uniform number outside its range); such rows give zeros.
- * Needs no workspace; one kernel launch.  The same inputs give the same bits.
+ * Outputs must not overlap inputs or one another.  Needs no workspace; one kernel launch.  The same inputs give the same bits.
  */
 #define DPPO_SAMPLE_MAX_TOPK 1024
 int dppo_sample(const void* logits, int64_t T, int64_t V, int64_t logits_row_stride, int logits_dtype,
@@ -373,6 +373,8 @@ int dppo_sample(const void* logits, int64_t T, int64_t V, int64_t logits_row_str
  *  qt          [cols, rows] out: the same for the transposed matrix (blocks run along x's columns), or NULL.  With
  *              block_rows = 128 its bytes and scales are those of q, transposed.  At least one of q and qt is given.
  *  status      device word: DPPO_STATUS_NONFINITE_ROW if a block holds a NaN or an infinity; its scale and all its bytes are NaN.
+ * rows * cols <= 2^38, in at most 2^31 - 1 tiles of 128 columns and 16 rows (128 rows with qt or block_rows = 128).  Outputs must
+ * not overlap x or one another.  One kernel launch.
  */
 int dppo_fp8_quantize(const void* x, int64_t rows, int64_t cols, int64_t x_row_stride, int x_dtype, int fp8_format,
                       int block_rows, void* q, int64_t q_row_stride, float* q_scale, int64_t q_scale_row_stride,
@@ -391,7 +393,7 @@ int dppo_fp8_quantize(const void* x, int64_t rows, int64_t cols, int64_t x_row_s
  *  a_scale     scale of row (block) i and K block k at a_scale[i * a_scale_row_stride + k * a_scale_k_stride]; b_scale alike.
  *              With row stride 1 the kernel reads them in whole lines.
  *  C           [M, N], c_dtype DPPO_F32 or DPPO_BF16 (rounded once, from the fp32 sum), row stride ldc elements (>= N).
- *  K = 0 gives C = 0.  status: device word, DPPO_STATUS_WAIT_LIMIT (may be NULL).  opts: wait_limit_us, test_inject.
+ *  M, N, K <= 2^30 each.  C must not overlap the operands or their scales.  K = 0 gives C = 0.  status: device word, DPPO_STATUS_WAIT_LIMIT (may be NULL).  opts: wait_limit_us, test_inject.
  */
 int dppo_gemm_tn_fp8(const void* A, int64_t lda, int a_format, int a_block_rows, const float* a_scale,
                      int64_t a_scale_row_stride, int64_t a_scale_k_stride,

@@ -542,7 +542,8 @@ extern "C" int dppo_gemm_tn_fp8(const void* A, int64_t lda, int a_format, int a_
                                 int M, int N, int K, void* C, int c_dtype, int64_t ldc,
                                 int32_t* status, const dppo_opts* opts, void* cuda_stream) {
   using namespace dppo;
-  if (M < 0 || N < 0 || K < 0) return DPPO_ERR_SHAPE;
+  const int most = 1 << 30;                              // tile bounds are counted in int
+  if (M < 0 || N < 0 || K < 0 || M > most || N > most || K > most) return DPPO_ERR_SHAPE;
   if (a_format != DPPO_E4M3 && a_format != DPPO_E5M2) return DPPO_ERR_DTYPE;
   if (b_format != DPPO_E4M3 && b_format != DPPO_E5M2) return DPPO_ERR_DTYPE;
   if (c_dtype != DPPO_F32 && c_dtype != DPPO_BF16) return DPPO_ERR_DTYPE;
@@ -555,7 +556,7 @@ extern "C" int dppo_gemm_tn_fp8(const void* A, int64_t lda, int a_format, int a_
   if (ldc < N || (K > 0 && (lda < K || ldb < K))) return DPPO_ERR_STRIDE;
   if (K > 0 && (a_scale_row_stride < 0 || a_scale_k_stride < 0 || b_scale_row_stride < 0 || b_scale_k_stride < 0)) return DPPO_ERR_STRIDE;
   const int es = c_dtype == DPPO_BF16 ? 2 : 4;
-  if ((uintptr_t)C % es) return DPPO_ERR_ALIGN;
+  if ((uintptr_t)C % es || (uintptr_t)status % 4) return DPPO_ERR_ALIGN;
   if (K > 0 && (((uintptr_t)A % 16) || ((uintptr_t)B % 16) || (lda % 16) || (ldb % 16) || ((uintptr_t)a_scale % 4) || ((uintptr_t)b_scale % 4)))
     return DPPO_ERR_ALIGN;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);

@@ -273,11 +273,9 @@ cudaError_t launch_quantize(QuantParams p, cudaStream_t st) {
   p.col_tiles = (p.cols + 127) / 128;
   if (p.qt || p.block_rows == 128) {
     const int64_t grid = p.col_tiles * ((p.rows + 127) / 128);
-    if (grid > INT32_MAX) return cudaErrorInvalidValue;
     dppo_quantize_kernel<T, 8, E5M2><<<(unsigned)grid, kQThreads, 0, st>>>(p);
   } else {
     const int64_t grid = p.col_tiles * ((p.rows + 15) / 16);
-    if (grid > INT32_MAX) return cudaErrorInvalidValue;
     dppo_quantize_kernel<T, 1, E5M2><<<(unsigned)grid, kQThreads, 0, st>>>(p);
   }
   return cudaGetLastError();
@@ -291,7 +289,7 @@ extern "C" int dppo_fp8_quantize(const void* x, int64_t rows, int64_t cols, int6
                                  int64_t q_scale_k_stride, void* qt, int64_t qt_row_stride, float* qt_scale,
                                  int64_t qt_scale_row_stride, int64_t qt_scale_k_stride, int32_t* status, void* cuda_stream) {
   using namespace dppo;
-  const int64_t big = (int64_t)1 << 38;                      // 128 x 128 tiles of it still count in 31 bits
+  const int64_t big = (int64_t)1 << 38;                      // (the grid has to count in 31 bits too: below)
   if (rows < 0 || cols < 0 || (rows > 0 && cols > big / rows)) return DPPO_ERR_SHAPE;
   if (x_dtype != DPPO_F32 && x_dtype != DPPO_BF16) return DPPO_ERR_DTYPE;
   if (fp8_format != DPPO_E4M3 && fp8_format != DPPO_E5M2) return DPPO_ERR_DTYPE;
@@ -309,7 +307,9 @@ extern "C" int dppo_fp8_quantize(const void* x, int64_t rows, int64_t cols, int6
   if (q && !apart(q_scale_row_stride, q_scale_k_stride, rb, kb)) return DPPO_ERR_STRIDE;
   if (qt && !apart(qt_scale_row_stride, qt_scale_k_stride, rbt, kbt)) return DPPO_ERR_STRIDE;
   const int es = x_dtype == DPPO_BF16 ? 2 : 4;
-  if (((uintptr_t)x % es) || ((uintptr_t)q_scale % 4) || ((uintptr_t)qt_scale % 4)) return DPPO_ERR_ALIGN;
+  if (((uintptr_t)x % es) || ((uintptr_t)q_scale % 4) || ((uintptr_t)qt_scale % 4) || ((uintptr_t)status % 4)) return DPPO_ERR_ALIGN;
+  const int64_t tile_rows = qt || block_rows == 128 ? 128 : 16;
+  if (kb * ((rows + tile_rows - 1) / tile_rows) > INT32_MAX) return DPPO_ERR_SHAPE;
   QuantParams p = {};
   p.x = x; p.rows = rows; p.cols = cols; p.ldx = x_row_stride; p.block_rows = block_rows;
   p.vec = ((uintptr_t)x % 16) == 0 && (x_row_stride * es) % 16 == 0;

@@ -27,6 +27,7 @@
 // Bounded by the 64-bit units: 8 operations an element in the passes that sum (t, its rounding, the remainder, four for the
 // polynomial, the sum) at 64 lanes a cycle and SM, 8 elements a cycle; HBM delivers about 12 bf16 elements in that time.
 #include <cooperative_groups.h>
+#include <float.h>
 #include <limits.h>
 
 #include "dppo_common.cuh"
@@ -301,8 +302,9 @@ struct Worker {
     });
   }
   // sum of 2^(z c - R) over the elements of chunk ch.  Those below `low` count as `low`, less than 2^-800: where |max c| < 2^30 a float's
-  // steps are less than 128 octaves.  Far from zero they are left out, because `low` may round up to the maximum.
-  template <bool FAR> __device__ __forceinline__ double weigh_all(int ch, const Exp2& x, float low) const {
+  // steps are less than 128 octaves.  Where that fails (far from zero, because `low` may round up to the maximum; where temperature is so
+  // high that `low` would lie below all floats, because -inf must not count as one) EXACT leaves them out.
+  template <bool EXACT> __device__ __forceinline__ double weigh_all(int ch, const Exp2& x, float low) const {
     double sum = 0.0;
     vectors(ch, [&](const uint4* v, int, int n) {
 #pragma unroll
@@ -313,8 +315,8 @@ struct Worker {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
           double q, w;
-          x.parts<FAR>(fmaxf(z[e], low), tab_hi, tab_lo, q, w);
-          if (!FAR || z[e] >= low) sum = fma(q, w, sum);
+          x.parts<EXACT>(fmaxf(z[e], low), tab_hi, tab_lo, q, w);
+          if (!EXACT || z[e] >= low) sum = fma(q, w, sum);
         }
       }
     });
@@ -367,7 +369,7 @@ struct Worker {
     bool far0;
     double zero;
     plain.set(c, 0.0, far0, zero);
-    const float floor0 = __double2float_ru(-0.9 * span), safe = (float)(0.8 * span);
+    const float floor0 = __double2float_ru(-0.9 * span), safe = floor0 > -FLT_MAX ? (float)(0.8 * span) : -1.f;
     for (int ch = c_begin + warp(); ch < c_end; ch += NW) {
       float mx = -INFINITY;
       double sum = 0.0, ref = 0.0, sums[kGroup] = {};
@@ -403,7 +405,7 @@ struct Worker {
           bool far_ch;
           x.set(c, (double)cm, far_ch, ref);
           const float low = low_of((double)cm);
-          sum = far_ch ? weigh_all<true>(ch, x, low) : weigh_all<false>(ch, x, low);
+          sum = far_ch || low == -FLT_MAX ? weigh_all<true>(ch, x, low) : weigh_all<false>(ch, x, low);
           if (far_ch) ref = NAN;
         } else {
           sum = 0.0;
@@ -589,6 +591,11 @@ struct Worker {
   __device__ int draw_from_list(int n, double u) const {
     const double target = u * s.pref[n - 1];
     int best = INT_MAX, last = -1;
+    // (entries that weigh less than 2^-1000 come last in the list and are not drawn: rounding in pref may give them a step)
+    const float low = low_of(M);
+    int worth = 0;
+    for (int i = tid(); i < n; i += NT) worth += list_z(i) >= low;
+    n = block_count(worth);
     if (n <= NT / 2) {
       if (tid() < n) {
         const int me = list_id(tid());
@@ -978,7 +985,8 @@ __global__ void __launch_bounds__(NT, 512 / NT) dppo_sample_kernel(SampleParams 
     double v = 0.0;
     if (tid < nchunks) {
       const double ref = s.cref[tid];                // (NaN: relative to the chunk's maximum)
-      if (s.csum[tid] > 0.0) v = s.csum[tid] * (ref == ref ? exp2(fma(-w.M, w.c, ref)) : exp(((double)s.cmax[tid] - w.M) * w.itau));
+      // (a chunk without an element worth counting has no mass, so that no chunk is chosen in which nothing can be drawn)
+      if (s.cmax[tid] >= w.low_of(w.M)) v = s.csum[tid] * (ref == ref ? exp2(fma(-w.M, w.c, ref)) : exp(((double)s.cmax[tid] - w.M) * w.itau));
       s.csum[tid] = v;
     }
     w.block_scan(v, W);
@@ -1143,7 +1151,7 @@ extern "C" int dppo_sample(const void* logits, int64_t T, int64_t V, int64_t log
                            int32_t* sampled_ids, float* mu_logp, int32_t* mu_topk_ids, float* mu_topk_p,
                            int32_t* status, void* cuda_stream) {
   using namespace dppo;
-  if (T < 0 || V < 1 || V > INT32_MAX || K < 0 || (int64_t)K > V) return DPPO_ERR_SHAPE;
+  if (T < 0 || V < 1 || V > ((int64_t)1 << 30) || K < 0 || (int64_t)K > V) return DPPO_ERR_SHAPE;
   if (logits_dtype != DPPO_F32 && logits_dtype != DPPO_BF16) return DPPO_ERR_DTYPE;
   if (K > DPPO_SAMPLE_MAX_TOPK) return DPPO_ERR_UNSUPPORTED;
   if (!status) return DPPO_ERR_NULL;
@@ -1152,6 +1160,9 @@ extern "C" int dppo_sample(const void* logits, int64_t T, int64_t V, int64_t log
   if (logits_row_stride < V) return DPPO_ERR_STRIDE;
   const int es = logits_dtype == DPPO_BF16 ? 2 : 4;
   if (((uintptr_t)logits % es) || ((uintptr_t)uniform % 8)) return DPPO_ERR_ALIGN;
+  const uintptr_t words = (uintptr_t)temperature | (uintptr_t)top_k | (uintptr_t)top_p | (uintptr_t)min_p | (uintptr_t)sampled_ids | (uintptr_t)mu_logp |
+                          (uintptr_t)mu_topk_ids | (uintptr_t)mu_topk_p | (uintptr_t)status;
+  if (words % 4) return DPPO_ERR_ALIGN;
   if (T == 0) return DPPO_OK;
   int dev = 0, sms = 148;
   cudaGetDevice(&dev);
