@@ -378,13 +378,20 @@ def _adr(t):
     return None if t is None else t.data_ptr()
 
 
-def _on(dev, stream, call):
-    """``call(stream handle)`` with ``dev`` current: these entry points are called once a token, where switching to a device that is
-    current already would cost as much as the launch."""
+def _on(dev, call):
+    """``call(current stream's handle)`` with ``dev`` current: these entry points are called once a token, where switching to a device
+    that is current already would cost as much as the launch."""
     if torch.cuda.current_device() == dev.index:
-        return call(_raw_stream(dev.index) if stream is None else stream.cuda_stream)
+        return call(_raw_stream(dev.index))
     with torch.cuda.device(dev):
-        return call(_raw_stream(dev.index) if stream is None else stream.cuda_stream)
+        return call(_raw_stream(dev.index))
+
+
+def _status_word(status, dev):
+    if status is None:
+        return torch.zeros(1, dtype=torch.int32, device=dev)
+    assert status.device == dev and status.dtype == torch.int32 and status.numel() == 1, "status"
+    return status
 
 
 def dppo_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, token_mask=None, K=0, out=None, status=None,
@@ -393,7 +400,11 @@ def dppo_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p
     uniform numbers ``uniform`` [T] float64.  ``temperature``, ``top_p``, ``min_p`` [T] fp32 and ``top_k`` [T] int32 may each
     be None (off).  Returns dict(sampled_ids[T] int32, mu_logp[T], mu_topk_ids[T,K], mu_topk_p[T,K] (None for K = 0),
     status[1]), which ``dppo_loss_fwd_bwd`` takes as they are; ``out``: a dict of those tensors to write into.  Nothing is
-    synchronised."""
+    synchronised.  ``stream``: another than the current one; what is allocated here then belongs to it."""
+    if stream is not None:
+        assert stream.device == logits.device, "stream"
+        with torch.cuda.stream(stream):
+            return dppo_sample(logits, uniform, temperature, top_k, top_p, min_p, token_mask, K, out, status)
     assert logits.is_cuda and logits.dim() == 2 and (logits.shape[1] <= 1 or logits.stride(1) == 1)
     T, V = logits.shape
     dev = logits.device
@@ -409,9 +420,8 @@ def dppo_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p
                                 ("mu_topk_p", torch.float32, (T, K))):
             t = out.get(name)
             assert (t is None and len(shape) == 2 and K == 0) or (t.device == dev and t.dtype == dt and t.shape == shape and t.is_contiguous()), name
-    if status is None:
-        status = torch.zeros(1, dtype=torch.int32, device=dev)
-    rc = _on(dev, stream, lambda st: lib().dppo_sample(
+    status = _status_word(status, dev)
+    rc = _on(dev, lambda st: lib().dppo_sample(
         logits.data_ptr(), T, V, logits.stride(0) if T > 1 else V, _dtype_code(logits), uniform.data_ptr(), _adr(temperature), _adr(top_k), _adr(top_p),
         _adr(min_p), _adr(token_mask), int(K), out["sampled_ids"].data_ptr(), out["mu_logp"].data_ptr(), _adr(out.get("mu_topk_ids")),
         _adr(out.get("mu_topk_p")), status.data_ptr(), st))
@@ -434,6 +444,10 @@ def dppo_fp8_quantize(x, dtype=torch.float8_e4m3fn, block_rows=1, rowwise=True, 
     torch.float8_e5m2; ``block_rows`` 1 or 128.  Returns dict(q, scale, qt, qt_scale, status): q [rows,cols] and its scales
     [row blocks, column blocks] with ``rowwise``, qt [cols,rows] and its scales with ``transposed`` (None otherwise); the rows of
     q and qt start on 16-byte boundaries, as ``dppo_gemm_tn_fp8`` wants them.  Nothing is synchronised."""
+    if stream is not None:
+        assert stream.device == x.device, "stream"
+        with torch.cuda.stream(stream):
+            return dppo_fp8_quantize(x, dtype, block_rows, rowwise, transposed, status)
     assert x.is_cuda and x.dim() == 2 and (x.shape[1] <= 1 or x.stride(1) == 1) and dtype in FP8_FORMATS and (rowwise or transposed)
     rows, cols = x.shape
     dev = x.device
@@ -443,12 +457,11 @@ def dppo_fp8_quantize(x, dtype=torch.float8_e4m3fn, block_rows=1, rowwise=True, 
         q, scale = _fp8_pair(rows, cols, block, dtype, dev)
     if transposed:
         qt, qt_scale = _fp8_pair(cols, rows, block, dtype, dev)
-    if status is None:
-        status = torch.zeros(1, dtype=torch.int32, device=dev)
+    status = _status_word(status, dev)
 
     def place(m, s):
         return (m.data_ptr(), m.stride(0), s.data_ptr(), s.stride(0), s.stride(1)) if m is not None else (None, 0, None, 0, 0)
-    rc = _on(dev, stream, lambda st: lib().dppo_fp8_quantize(
+    rc = _on(dev, lambda st: lib().dppo_fp8_quantize(
         x.data_ptr(), rows, cols, x.stride(0) if rows > 1 else cols, _dtype_code(x), FP8_FORMATS[dtype], int(block_rows), *place(q, scale),
         *place(qt, qt_scale), status.data_ptr(), st))
     if rc != 0:
@@ -461,6 +474,10 @@ def dppo_gemm_tn_fp8(A, a_scale, B, b_scale, a_block_rows=1, b_block_rows=128, o
     """C[M,N] = A[M,K] . B[N,K]^T for 8-bit CUDA matrices (torch.float8_e4m3fn / torch.float8_e5m2, last dimension contiguous, rows on
     16-byte boundaries) with fp32 scales [row blocks, ceil(K/128)] of any strides.  ``a_block_rows`` / ``b_block_rows``: rows that
     share a scale, 1 or 128.  Returns (C, status), C fp32 or bf16; nothing is synchronised."""
+    if stream is not None:
+        assert stream.device == A.device, "stream"
+        with torch.cuda.stream(stream):
+            return dppo_gemm_tn_fp8(A, a_scale, B, b_scale, a_block_rows, b_block_rows, out_dtype, C, status, None, wait_limit_us, test_inject)
     assert A.is_cuda and B.is_cuda and A.dtype in FP8_FORMATS and B.dtype in FP8_FORMATS and A.dim() == 2 and B.dim() == 2
     M, K = A.shape
     N = B.shape[0]
@@ -470,11 +487,10 @@ def dppo_gemm_tn_fp8(A, a_scale, B, b_scale, a_block_rows=1, b_block_rows=128, o
     if C is None:
         C = torch.empty((M, N), dtype=out_dtype, device=A.device)
     assert C.device == A.device and C.shape == (M, N) and (N <= 1 or C.stride(1) == 1)
-    if status is None:
-        status = torch.zeros(1, dtype=torch.int32, device=A.device)
+    status = _status_word(status, A.device)
     up16 = -(-K // 16) * 16                               # a single row has no pitch of its own
     opts = None if wait_limit_us == 0 and test_inject == 0 else ctypes.byref(_opts(wait_limit_us=wait_limit_us, test_inject=test_inject))
-    rc = _on(A.device, stream, lambda st: lib().dppo_gemm_tn_fp8(
+    rc = _on(A.device, lambda st: lib().dppo_gemm_tn_fp8(
         A.data_ptr(), A.stride(0) if M > 1 else up16, FP8_FORMATS[A.dtype], int(a_block_rows), a_scale.data_ptr(), a_scale.stride(0), a_scale.stride(1),
         B.data_ptr(), B.stride(0) if N > 1 else up16, FP8_FORMATS[B.dtype], int(b_block_rows), b_scale.data_ptr(), b_scale.stride(0),
         b_scale.stride(1), M, N, K, C.data_ptr(), _dtype_code(C), C.stride(0) if M > 1 else N, status.data_ptr(), opts, st))
