@@ -17,7 +17,7 @@
 //   warps 4-11   promotion: a warp owns 32 rows (its quarter of the tensor-memory lanes) and 128 of the columns, its fp32 sums in
 //                registers (setmaxnreg moves registers from warps 0-3 to these); finished tiles leave through shared memory and
 //                bulk tensor stores
-// With few tiles and a long K a cluster of S CTAs shares a tile: each sums S-th part of the K blocks, leaves its sums in its shared
+// With few tiles and a long K a cluster of S CTAs shares a tile: each sums an S-th part of the K blocks, leaves its sums in its shared
 // memory, and all add up a part of the rows each, CTA after CTA (a fixed order), through distributed shared memory.
 // Every wait is bounded (dppo_pipe.cuh).
 //
@@ -434,9 +434,9 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tn_fp8_kernel(const __grid_co
     cooperative_groups::cluster_group cl = cooperative_groups::this_cluster();
     cl.sync();
     const int m0 = (group % tiles_m) * BM, n0 = (group / tiles_m) * bn, n_end = min(p.N, n0 + bn);
-    const int rows = BM / p.split;
+    const int r_first = BM * rank / p.split, rows = BM * (rank + 1) / p.split - r_first;
     for (int i = tid; i < rows * (BN / 4); i += THREADS) {
-      const int r = rank * rows + i / (BN / 4), c = (i % (BN / 4)) * 4, row = m0 + r, col = n0 + c;
+      const int r = r_first + i / (BN / 4), c = (i % (BN / 4)) * 4, row = m0 + r, col = n0 + c;
       if (row >= p.M || col >= n_end) continue;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       for (int o = 0; o < p.split; ++o) {
@@ -501,18 +501,22 @@ bool make_map(CUtensorMap* map, CUtensorMapDataType type, int es, const void* ba
 template <bool B_ROW_SCALES>
 cudaError_t launch(Params p, const void* A, int64_t lda, const void* B, int64_t ldb, int K, int sms, cudaStream_t st) {
   // Tile width (whole blocks of 128 columns) and split: the time of a K block of a tile hardly depends on the width (the hand-over's
-  // latency), so a block is counted as 256 + width, a shared tile's exchange as two blocks, and the cheapest choice is taken.  Measured:
-  // 64 x 2048 x 151936 86 us shared by clusters, 497 us without; 512 x 2048 x 8192 19 and 35 us; 4096 x 151936 x 2048 1.17 ms in
-  // tiles of 256, 1.79 ms in tiles of 128; where few tiles leave SMs idle the narrow ones win by a tenth.
+  // latency), so a block is counted as 256 + width, a shared tile's exchange as two blocks (four in clusters of 3, 5, 6 or 7, which
+  // take a microsecond or two longer: 30 x 1215 x 2500 12.4 us in sevens, 10.4 in eights), and the cheapest choice is taken.
+  // Measured: 600 x 2048 x 151936 210 us in threes, 292 in pairs; 64 x 2048 x 151936 86 us in eights, 497 alone; 512 x 2048 x 8192 19
+  // and 35 us; 4096 x 151936 x 2048 1.17 ms in tiles of 256, 1.79 ms in tiles of 128; where few tiles leave SMs idle the narrow
+  // ones win by a tenth.
   const int64_t tm = (p.M + BM - 1) / BM;
   int64_t best = INT64_MAX;
   for (int w = BN; w >= 128; w -= 128) {
     const int64_t tiles = tm * ((p.N + w - 1) / w);
     if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
-    for (int S = 1; S <= MAX_SPLIT; S *= 2) {
-      // (clusters of 8 do not fit the SMs of every GPC without a rest: 112 of 148 SMs can be counted on)
-      if (S > 1 && (tiles * S > (S == 8 ? sms * 3 / 4 : sms) || p.kblocks < 2 * S)) break;
-      const int64_t cost = ((tiles * S + sms - 1) / sms) * ((p.kblocks + S - 1) / S + (S > 1 ? 2 : 0)) * (256 + w);
+    for (int S = 1; S <= MAX_SPLIT; ++S) {
+      // (a cluster lies in one GPC, whose SMs are not a multiple of every size: of 148 SMs 112 can be counted on for clusters of 5 to
+      // 8, nine in ten for 3, whose tiles would otherwise take a second round)
+      const int64_t room = S > 4 ? sms * 3 / 4 : S == 3 ? sms * 9 / 10 : sms;
+      if (S > 1 && (tiles * S > room || p.kblocks < 2 * S)) continue;
+      const int64_t cost = ((tiles * S + sms - 1) / sms) * ((p.kblocks + S - 1) / S + (S == 1 ? 0 : (S & (S - 1)) ? 4 : 2)) * (256 + w);
       if (cost < best) { best = cost; p.bn = w; p.split = S; }
     }
   }
