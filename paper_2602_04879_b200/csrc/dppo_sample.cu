@@ -29,7 +29,7 @@
 // elements a cycle and SM, where HBM delivers about 12 in bf16.  The leader's phases after pass A (list, sort, draw) are latency,
 // hidden behind another row's pass where an SM has two rows.
 //
-// Measured on B200 (V = 151936): 2048 rows bf16 at tau = 1 with a record of 20: 449 us = 1.39 TB/s of logits (95 us would be HBM's
+// Measured on B200 (V = 151936): 2048 rows bf16 at tau = 1 with a record of 64: 449 us = 1.39 TB/s of logits (95 us would be HBM's
 // time); 61 rows with all four settings mixed: 82 us; 256 fp32 rows of 50257 with top-p 0.9: 86 us; one row with top-k 50: 12 us.
 // 2048 rows with top-k 50, which need no sums over the row: 203 us = 3.1 TB/s.
 #include <cooperative_groups.h>
