@@ -57,12 +57,6 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const W
     }
   }
 }
-// One lane of a warp waits for all.
-__device__ __forceinline__ bool mbar_wait_lane0(uint32_t bar, uint32_t parity, const WaitCtl& w) {
-  int ok = 0;
-  if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity, w);
-  return __shfl_sync(0xffffffffu, ok, 0) != 0;
-}
 // All lanes of a warp wait; the warp proceeds only if every lane saw the phase complete.
 __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, const WaitCtl& w) {
   const bool ok = mbar_wait(bar, parity, w);
