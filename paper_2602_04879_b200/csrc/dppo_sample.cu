@@ -50,6 +50,8 @@ constexpr int kSList = 4096;           // entries of the sorted list
 constexpr int kSMaxTop = DPPO_SAMPLE_MAX_TOPK;      // largest list that is asked for
 constexpr int kSProbe = 256;           // list length tried first for top-p / min-p alone
 constexpr int kSMaxCluster = 8;
+constexpr unsigned long long kFixOne = 1ull << 51;        // weight 1 in the fixed-point sums by chunk: all of a list may lie in one chunk
+static_assert(kSList <= ~0ull / kFixOne, "the list's weights, 1 each at most, add up in 64 bits");
 constexpr double kLog2eD = 1.4426950408889634074;
 
 struct SampleParams {
@@ -90,7 +92,7 @@ struct SampleSmem {
     float gmax[kSMaxChunks * 32];         // until the list is made
     double pref[kSList];                  // then: running sums along the list
   };
-  unsigned long long cfix[kSMaxChunks];   // kept weights of listed elements by chunk, in units of 2^-52
+  unsigned long long cfix[kSMaxChunks];   // kept weights of listed elements by chunk, in units of 1 / kFixOne
   alignas(16) unsigned bins[kSBins];
   float cmax[kSMaxChunks];
   float rec_z[kSMaxTop];
@@ -724,13 +726,14 @@ struct Worker {
     }
     cut.z = list_z(pos); cut.tie = list_id(pos);
     top_mass = above + s.pref[pos];
-    // the listed part of the prefix joins its chunks (integers: no order to depend on)
+    // the listed part of the prefix joins its chunks (integers: no order to depend on; cut off at 2^-51, the whole list's error is below
+    // 2e-12 of the largest weight, which the mass holds)
     if (tid() < nchunks) s.cfix[tid()] = 0;
     __syncthreads();
     for (int i = tid(); i <= pos; i += NT)
-      atomicAdd(&s.cfix[(list_id(i) + row.head) / (N * 32 * p.vecs)], (unsigned long long)(weight(list_z(i)) * 4503599627370496.0));
+      atomicAdd(&s.cfix[(list_id(i) + row.head) / (N * 32 * p.vecs)], (unsigned long long)(weight(list_z(i)) * (double)kFixOne));
     __syncthreads();
-    if (tid() < nchunks) s.csum[tid()] += (double)s.cfix[tid()] * (1.0 / 4503599627370496.0);
+    if (tid() < nchunks) s.csum[tid()] += (double)s.cfix[tid()] * (1.0 / (double)kFixOne);
     __syncthreads();
     return true;
   }

@@ -282,3 +282,22 @@ def test_the_record_feeds_the_loss(K):
         torch.cuda.synchronize()
         assert int(r["status"].item()) == 0 and bool(r["mask"].all()) and float(r["divergence"].abs().max()) <= 1e-5
         assert abs(float(r["loss"].item()) + 1.0) <= 1e-5                      # -mean(r A) with r = 1, A = 1
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("setting,rest", [({"top_p": 0.9999}, -30.0), ({"top_k": 4096}, -30.0), ({"top_k": 4096, "top_p": 0.9999}, -30.0),
+                                          ({"top_p": 0.9999, "temperature": 1e36}, -3e38)])
+def test_a_full_list_of_the_largest_weight_in_one_chunk(dtype, setting, rest):
+    """4096 tokens of weight 1 side by side, as many as the sorted list holds, in one of a long row's chunks, and a few hundred light ones
+    all over the row: the cut takes in the whole list, whose weights add up within that chunk."""
+    V = 1 << 20
+    g = torch.Generator().manual_seed(33)
+    z = torch.full((3, V), NEG)
+    z[:, ::1500] = rest
+    for t, first in enumerate((64, 3 * 4352 + 100, 200 * 4224 + 50)):     # chunks of 4352 elements in bf16, of 4224 in fp32
+        z[t, (first // 4352 * 4352 if dtype == torch.bfloat16 else first // 4224 * 4224) + 64:][:4096] = 0.25
+    if "temperature" in setting:
+        z = torch.where(z == 0.25, torch.randn((3, V), generator=g), z)   # so hot that unlike logits all weigh 1
+    z, u = z.to(dtype), _uniform(3, 33)
+    s = {n: torch.full((3,), v, dtype=torch.int32 if n == "top_k" else torch.float32) for n, v in setting.items()}
+    assert _check(_on_gpu(z, u, 30, s), z, u, 30, s) >= 2
