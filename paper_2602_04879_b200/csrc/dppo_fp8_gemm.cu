@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tn_fp8_kernel(const __grid_co
   const int group = (int)blockIdx.x / p.split, ngroups = (int)gridDim.x / p.split;
 
   if (tid == 0) {
-    for (int i = 0; i < STAGES; ++i) { mbar_init(full0 + 8 * i, 1 + 32); mbar_init(done0 + 8 * i, 1); }
+    for (int i = 0; i < STAGES; ++i) { mbar_init(full0 + 8 * i, 1 + 32); mbar_init(done0 + 8 * i, 2); }
     for (int i = 0; i < 2; ++i) mbar_init(tempty0 + 8 * i, 1);
     *wc.flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -238,8 +238,10 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tn_fp8_kernel(const __grid_co
               gemm::tma_load_2d(a_dst, &map_a, kb * BK, m0, bar);
               gemm::tma_load_2d(a_dst + A_BYTES, &map_b, kb * BK, n0, bar);
             }
-            // The slot's last scales were those of 8 K blocks ago.  A stage is free once the MMAs of 3 blocks ago are done, and
-            // those began after every promotion warp had read the block 2 before them: nobody reads the slot any more.
+            // Scales are plain shared-memory data, which a commit does not order.  They reach the promotion warps through the issuer:
+            // its wait for `full` sees them landed, its own arrival on `done` passes that on, warp 3 and a named barrier hand it over.  And
+            // back: the slot's last scales were those of 8 K blocks ago; a stage is free once the issuer has arrived for the block 3
+            // before, after its wait for the buffer that every promotion warp had left with the block 5 before.  Nobody reads the slot.
             const uint32_t sc = ring + (it % SRING) * (SCALES * 4);
             if (!p.a_shift) {
 #pragma unroll
@@ -282,6 +284,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tn_fp8_kernel(const __grid_co
             for (int k = 0; k < BK / 32; ++k)        // 32 elements = 32 bytes along K inside the swizzle atom
               mma_f8(tmem_base + b * BN, adesc + (uint64_t)(k * 2), bdesc + (uint64_t)(k * 2), idesc, k != 0);
             gemm::mma_commit(done0 + 8 * s);         // the stage may be filled again, and P_kb is complete
+            mbar_arrive(done0 + 8 * s);              // (the commit speaks for the tensor cores, this for the scales: see the producer)
           }
           __syncwarp();
           if (++s == STAGES) { s = 0; ph ^= 1u; }

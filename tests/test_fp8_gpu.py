@@ -337,3 +337,26 @@ def test_lm_head_step_in_8_bits_end_to_end():
         slope = (loss(*args(1)) - loss(*args(-1))) / (2 * eps)
         # dlogits was formed from fp32 logits of bf16 operands: z is off by at most (256 + 1) 2^-24 of its magnitudes, so is the slope
         assert abs((ref * D).sum() - slope) <= 1e-4 * (np.abs(ref) * np.abs(D)).sum()
+
+
+@pytest.mark.parametrize("M,N,K", [(200, 300, 151936), (1500, 5000, 4100), (130, 40000, 1000)])
+@pytest.mark.parametrize("a_br,b_br", [(1, 128), (1, 1), (128, 128), (128, 1)])
+def test_every_block_meets_its_own_scales(M, N, K, a_br, b_br):
+    """Elements of +1 and -1 and scales of 1/2, 1 and 2 that change from block to block: every sum on the way is a multiple of 1/4 below
+    2^20, exact in fp32 in any order, so one scale of another block would show.  Tiles shared along K, several tiles per CTA, many K
+    blocks in a row."""
+    g = torch.Generator(device=DEV).manual_seed(M)
+    kb = -(-K // 128)
+
+    def operand(rows, br):
+        q = (torch.randint(0, 2, (rows, -(-K // 16) * 16), generator=g, device=DEV) * 2 - 1).float().to(torch.float8_e4m3fn)[:, :K]
+        return q, torch.exp2(torch.randint(-1, 2, (-(-rows // br), kb), generator=g, device=DEV).float())
+
+    def exact(q, scale, br):
+        return q.double() * scale.double().repeat_interleave(br, 0)[:q.shape[0]].repeat_interleave(128, 1)[:, :K]
+    A, sa = operand(M, a_br)
+    B, sb = operand(N, b_br)
+    assert 4 * K < 2 ** 20
+    C, status = dppo.dppo_gemm_tn_fp8(A, sa, B, sb, a_br, b_br)
+    assert int(status.item()) == 0
+    assert torch.equal(C.double(), exact(A, sa, a_br) @ exact(B, sb, b_br).t())
