@@ -124,9 +124,11 @@ template <int R> __device__ __forceinline__ void col_max(const Oct<float>* v, ui
   }
 }
 
-// R rows per thread: 8 for whole 128 x 128 tiles, needed for 128 x 128 blocks and for the transposed form, and faster as soon as there
-// are tiles for all SMs (1 x 128 blocks as stored, bf16: [2048, 151936] 158 us against 283 us, [4096, 2048] 8.5 against 10.4 us); 1
-// otherwise: eight times the CTAs, so that few rows still spread over the SMs ([512, 2048] 4.8 against 5.7 us).
+// R rows per thread: 8 for whole 128 x 128 tiles, needed for 128 x 128 blocks and for the transposed form, and faster for rows that allow
+// 16-byte loads once there are tiles for all SMs with more than half of their rows (1 x 128 blocks as stored, bf16: [2048, 151936] 158 us
+// against 283 us, [4096, 2048] 6.9 against 9.3 us, [128, 151936] 13.7 against 19.7 us); 1 otherwise: up to eight times the CTAs, so that few
+// rows still spread over the SMs, and rows on no 16-byte boundary are read by adjacent threads of many warps ([512, 2048] 4.8 against 5.7 us,
+// [4, 151936] 3.3 against 11.7 us, [61, 151936] 10.8 against 17.4 us, [1024, 50257] 57 against 63 us, in fp32 63 against 72 us).
 template <typename T, int R, bool E5M2>
 __global__ void __launch_bounds__(kQThreads) dppo_quantize_kernel(QuantParams p) {
   static_assert(R == 8 || R == 1, "rows per thread");
@@ -281,7 +283,7 @@ cudaError_t launch_quantize(QuantParams p, cudaStream_t st) {
   cudaGetDevice(&dev);
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   const int64_t grid = p.col_tiles * ((p.rows + 127) / 128);
-  if (p.qt || p.block_rows == 128 || grid >= 2 * sms) {
+  if (p.qt || p.block_rows == 128 || (p.vec && p.rows > 64 && grid >= 2 * sms)) {
     dppo_quantize_kernel<T, 8, E5M2><<<(unsigned)grid, kQThreads, 0, st>>>(p);
   } else {
     const int64_t grid = p.col_tiles * ((p.rows + 15) / 16);

@@ -27,3 +27,14 @@ def test_rowwise_alone_equals_both_ways(rows, cols, dtype, fmt):
     got = one["q"][:140].float().cpu().numpy().astype(np.float64)
     bad = got != val                       # fp32 inputs: 7/8 x and the quotient round by 2^-24 each, next to a tie either neighbour will do
     assert not bad.any() or (dtype == torch.float32 and np.all(np.abs(y[bad] - 0.5 * (got[bad] + val[bad])) <= 2.0 ** -23 * np.abs(y[bad])))
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 151936), (4, 151936), (16, 37889), (64, 40000), (65, 40000), (64, 40007), (200, 40003), (66, 40008)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_few_rows_of_a_wide_matrix(rows, cols, dtype):
+    """Few rows, and rows on no 16-byte boundary, take the kernel with a row per thread however many columns there are."""
+    g = torch.Generator().manual_seed(rows + cols)
+    xd = (torch.randn((rows, cols), generator=g) * torch.exp2(torch.randint(-9, 9, (rows, 1), generator=g).float())).to(dtype).to(DEV)
+    one, both = dppo.dppo_fp8_quantize(xd), dppo.dppo_fp8_quantize(xd, transposed=True)
+    assert int(one["status"].item()) == 0 and torch.equal(one["scale"], both["scale"])
+    assert torch.equal(one["q"].contiguous().view(torch.uint8), both["q"].contiguous().view(torch.uint8))
