@@ -371,7 +371,6 @@ def dppo_loss_fwd_bwd_host(logits, sampled_ids, mu_logp, advantages, token_mask=
 
 
 SAMPLE_MAX_TOPK = 1024
-_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _adr(t):
@@ -382,9 +381,9 @@ def _on(dev, call):
     """``call(current stream's handle)`` with ``dev`` current: these entry points are called once a token, where switching to a device
     that is current already would cost as much as the launch."""
     if torch.cuda.current_device() == dev.index:
-        return call(_raw_stream(dev.index))
+        return call(torch._C._cuda_getCurrentRawStream(dev.index))
     with torch.cuda.device(dev):
-        return call(_raw_stream(dev.index))
+        return call(torch._C._cuda_getCurrentRawStream(dev.index))
 
 
 def _status_word(status, dev):

@@ -2,6 +2,8 @@
 import ctypes
 import os
 import re
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -133,3 +135,15 @@ def test_rounding_restatement():
         assert np.array_equal(R.round8(mids, fmt), even)
         assert np.array_equal(R.round8(mids * (1 + 1e-12), fmt), vals[1:]) and np.array_equal(R.round8(mids * (1 - 1e-12), fmt), vals[:-1])
         assert R.round8(np.array([1e9]), fmt)[0] == R.MAX8[fmt]
+
+
+def test_import_where_torch_has_no_cuda():
+    """The package imports where torch was built without CUDA (such a build has no raw-stream query), and refuses at the call."""
+    pytest.importorskip("torch")
+    code = ("import torch\n"
+            "for n in [n for n in dir(torch._C) if 'urrentRawStream' in n]: delattr(torch._C, n)\n"
+            "import paper_2602_04879_b200 as dppo\n"
+            "for call in (lambda: dppo.dppo_sample(torch.zeros(2, 4), torch.zeros(2, dtype=torch.float64)), lambda: dppo.dppo_fp8_quantize(torch.zeros(2, 4))):\n"
+            "    try:\n        call()\n    except AssertionError:\n        pass\n    else:\n        raise SystemExit('CPU tensors were taken')\n")
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
