@@ -335,6 +335,11 @@ int dppo_exact_divergence(const void* logits, const void* mu_logits, int64_t T, 
  * the lowest id a with  sum_{j <= a} mu(j) > uniform.  Logits of -inf (and tokens whose weight is below 2^-1000) are never
  * drawn and never kept.
  *
+ * The record is of mu as drawn from.  The loss entry points set it against softmax(logits), without temperature or cuts: with the
+ * same weights ratio 1 and divergence 0 only for tau = 1 and no cut, or, for tau alone, where their logits have been divided by tau
+ * (their dlogits are then the gradient with respect to the divided logits).  Tokens cut off have mu = 0 in the record, and the mass
+ * that was cut counts as divergence.
+ *
  *  logits         [T, V] row-major, row stride in elements (>= V; rows may start at any element), DPPO_F32 or DPPO_BF16;
  *                 V <= 2^30.
  *  uniform        [T] double in [0, 1): one random number per row (8-byte aligned).  Doubles, because an fp32 uniform's steps

@@ -301,3 +301,70 @@ def test_a_full_list_of_the_largest_weight_in_one_chunk(dtype, setting, rest):
     z, u = z.to(dtype), _uniform(3, 33)
     s = {n: torch.full((3,), v, dtype=torch.int32 if n == "top_k" else torch.float32) for n, v in setting.items()}
     assert _check(_on_gpu(z, u, 30, s), z, u, 30, s) >= 2
+
+
+VARIANTS = (dppo.BINARY_TV, dppo.BINARY_KL, dppo.TOPK_TV, dppo.TOPK_KL)
+
+
+def test_the_readme_example_compares_like_distributions():
+    """The README's lines as they stand, with the trainer's logits equal to the rollout's: no divergence beyond fp32, nothing masked."""
+    import os
+    import textwrap
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
+    lines = textwrap.dedent(text[text.index("The rollout side"):].split("```python\n")[1].split("```")[0]).rstrip()
+    first, loss = lines.rsplit("\n", 1)
+    g = torch.Generator().manual_seed(3)
+    T, d, V = 96, 256, 1000
+    ns = dict(dppo=dppo, torch=torch, W=(0.2 * torch.randn((V, d), generator=g)).to(torch.bfloat16).to(DEV), uniform=_uniform(T, 3).to(DEV),
+              hidden=torch.randn((T, d), generator=g).to(torch.bfloat16).to(DEV), adv=torch.where(torch.rand(T, generator=g) < 0.5, -1.0, 1.0).to(DEV),
+              tau=torch.full((T,), 0.7, device=DEV), p=torch.full((T,), 0.9, device=DEV))
+    exec(first, ns)
+    ns["logits"] = ns["z"]
+    exec(loss, ns)
+    assert int(ns["r"]["status"].item()) == 0 and int(ns["o"]["status"].item()) == 0
+    assert bool(ns["r"]["mask"].all()) and float(ns["r"]["divergence"].abs().max()) <= 1e-5
+
+
+def test_a_record_at_another_temperature_feeds_the_loss_on_scaled_logits():
+    """The record is softmax(z / tau)'s.  Against logits divided by tau in fp32, each off by at most e = 2^-24 max |z / tau|, so that a
+    log probability is off by at most 2 e, the loss finds a ratio of 1 and no divergence: within its own 1e-5 (divergence) and 1e-4
+    (loss) and what 2 e does to them."""
+    T, V, K = 64, 32000, 20
+    z, u = _rows(T, V, torch.float32, seed=1), _uniform(T, 1)
+    tau = 0.4 + 1.2 * torch.rand(T, generator=torch.Generator().manual_seed(2))
+    scaled = z / tau[:, None]
+    e = 2.0 ** -24 * float(scaled.abs().max())
+    o = _on_gpu(z, u, K, {"temperature": tau})
+    for variant in VARIANTS:
+        r = dppo.dppo_loss_fwd_bwd(scaled.to(DEV), o["sampled_ids"], o["mu_logp"], torch.ones(T, device=DEV), None, variant, K, 1e-3, o["mu_topk_ids"], o["mu_topk_p"])
+        torch.cuda.synchronize()
+        assert int(r["status"].item()) == 0 and bool(r["mask"].all()) and float(r["divergence"].abs().max()) <= 1e-5 + 4 * e
+        assert abs(float(r["loss"].item()) + 1.0) <= 1e-4 + 2 * e
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_record_with_cuts_against_the_loss_oracle(dtype):
+    """Cut-off tokens stand in the record with probability 0.  The loss takes the record as it is: the truncated distribution against the
+    whole softmax, which differ by the mass that was cut."""
+    from oracle import dppo_oracle as O
+    from parity_util import check_dlogits, check_loss, check_scalars
+    T, V, K = 48, 3000, 20
+    z, u = _rows(T, V, dtype, seed=12, sigma=1.5), _uniform(T, 12)
+    g = torch.Generator().manual_seed(13)
+    s = {"top_k": torch.randint(1, 40, (T,), generator=g, dtype=torch.int32), "top_p": 0.5 + 0.5 * torch.rand(T, generator=g)}
+    o = _on_gpu(z, u, K, s)
+    assert bool((o["mu_topk_p"] == 0).any()) and float(o["mu_topk_p"].sum(1).min()) > 0
+    adv = torch.where(torch.rand(T, generator=g) < 0.5, -1.0, 1.0)
+    host = lambda t: t.cpu().numpy().astype(np.float64)  # noqa: E731
+    zs = (z + 0.05 * torch.randn((T, V), generator=g)).to(dtype)
+    for variant in VARIANTS:
+        r = dppo.dppo_loss_fwd_bwd(zs.to(DEV), o["sampled_ids"], o["mu_logp"], adv.to(DEV), None, variant, K, 0.3, o["mu_topk_ids"], o["mu_topk_p"])
+        torch.cuda.synchronize()
+        assert int(r["status"].item()) == 0
+        ora = O.dppo_loss_fwd_bwd(host(zs.float()), o["sampled_ids"].cpu().numpy(), host(o["mu_logp"]), host(adv), None, variant, K, 0.3, None,
+                                  o["mu_topk_ids"].cpu().numpy(), host(o["mu_topk_p"]))
+        check_scalars(r["divergence"].cpu().numpy(), r["mask"].cpu().numpy(), ora, {"token_mask": None}, 0.3)
+        check_loss(float(r["loss"].item()), ora["loss"], dtype == torch.bfloat16)
+        check_dlogits(r["dlogits"], ora["dlogits"], dtype == torch.bfloat16)
+        if variant == dppo.BINARY_TV:
+            assert float(r["divergence"].mean()) > 0.05
