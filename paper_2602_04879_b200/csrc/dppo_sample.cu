@@ -774,7 +774,7 @@ struct Worker {
         double m = 0.0;
         unsigned long long n = 0;
         for (int r = 0; r < C; ++r) { m += s.mass[r][i]; n += s.cnt[r][i]; }
-        const bool holds = by_mass ? m >= target : n >= count;
+        const bool holds = by_mass ? n > 0 && m >= target : n >= count;      // (a target of 0, top_p = 0, asks for one token too)
         if (holds) { lo = pv[i]; n_lo = n; break; }
         hi = pv[i]; n_hi = n; m_hi = m;
         if (it == 0 && i == 0) { top_mass = m; return false; }

@@ -368,3 +368,24 @@ def test_a_record_with_cuts_against_the_loss_oracle(dtype):
         check_dlogits(r["dlogits"], ora["dlogits"], dtype == torch.bfloat16)
         if variant == dppo.BINARY_TV:
             assert float(r["divergence"].mean()) > 0.05
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("top_p", [0.0, 1e-45, 1e-30])
+@pytest.mark.parametrize("top_k,temperature", [(1025, 1.0), (1500, 1.0), (5000, 30.0), (4500, 1e5), (3000, 0.01)])
+def test_a_top_p_of_nothing_within_a_long_top_k(dtype, top_p, top_k, temperature):
+    """A prefix of at least 0 of the mass still holds one token, also where ties or a high temperature put more tokens next to the
+    largest than the list holds, so that the cut is bracketed.  One row alone, rows that share the call, and one CTA per row."""
+    z = _special_rows(dtype)
+    T = z.shape[0]
+    u = _uniform(T, 17)
+
+    def settings(n):
+        return {"top_k": torch.full((n,), top_k, dtype=torch.int32), "top_p": torch.full((n,), top_p), "temperature": torch.full((n,), temperature)}
+    out = _on_gpu(z, u, 30, settings(T))
+    _check(out, z, u, 30, settings(T))
+    many = _on_gpu(z.repeat(20, 1), u.repeat(20), 30, settings(20 * T))
+    assert torch.equal(many["sampled_ids"].view(20, T), out["sampled_ids"].expand(20, T))
+    for t in (3, 4, 5):
+        one = _on_gpu(z[t:t + 1], u[t:t + 1], 0, settings(1))
+        assert int(one["sampled_ids"][0]) == int(out["sampled_ids"][t]) == int(z[t].float().argmax())
