@@ -65,7 +65,8 @@ struct Params {
   int kblocks;
   void* C;
   int64_t ldc;
-  int c_bf16, c_vec, tma_store;      // c_vec: 16-byte stores allowed; tma_store: map_c describes C
+  int c_bf16, c_vec;                 // c_vec: 16-byte stores allowed
+  int n_tma;                         // columns of C that map_c describes: whole 16-byte pieces of a row (0: no map)
   uint32_t formats;                  // bits of the instruction descriptor
   int32_t* status;
   unsigned long long wait_ns;
@@ -177,6 +178,14 @@ template <bool LAST> __device__ __forceinline__ void read_and_promote(uint32_t t
     acc[2 * g] = __ffma2_rn(make_float2(__uint_as_float(r[4 * g]), __uint_as_float(r[4 * g + 1])), w0[g], acc[2 * g]);
     acc[2 * g + 1] = __ffma2_rn(make_float2(__uint_as_float(r[4 * g + 2]), __uint_as_float(r[4 * g + 3])), w1[g], acc[2 * g + 1]);
   }
+}
+
+// element (r, in) of a warp's two staged blocks (32 rows x 128 bytes each, 128-byte swizzle) to C[at]
+__device__ __forceinline__ void store_staged(const Params& p, const unsigned char* blocks, int r, int in, int64_t at) {
+  const int ncol = p.c_bf16 ? 64 : 32, byte = (in % ncol) * (p.c_bf16 ? 2 : 4);
+  const unsigned char* src = blocks + (in / ncol) * 4096 + r * 128 + ((((byte >> 4) ^ (r & 7)) << 4) | (byte & 15));
+  if (p.c_bf16) reinterpret_cast<unsigned short*>(p.C)[at] = *reinterpret_cast<const unsigned short*>(src);
+  else reinterpret_cast<float*>(p.C)[at] = *reinterpret_cast<const float*>(src);
 }
 
 template <bool B_ROW_SCALES>       // b_block_rows = 1
@@ -373,7 +382,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tn_fp8_kernel(const __grid_co
 #pragma unroll
         for (int g = 0; g < 2; ++g) {                // bf16: all four quarters of the columns at once; fp32: two and two
           if (g == 1 && p.c_bf16) break;
-          if (p.tma_store && lane == 0) gemm::bulk_wait_read<0>();
+          if (p.n_tma && lane == 0) gemm::bulk_wait_read<0>();
           __syncwarp();
           if (p.c_bf16) {
 #pragma unroll
@@ -394,15 +403,23 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tn_fp8_kernel(const __grid_co
               else st128(at, __float_as_uint(acc[j].x), __float_as_uint(acc[j].y), __float_as_uint(acc[j + 1].x), __float_as_uint(acc[j + 1].y));
             }
           }
-          if (p.tma_store) {
+          if (p.n_tma) {
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) {
               for (int c = 0; c < 2; ++c) {
                 const int col = n0 + (2 * g + c) * ncol;
-                if (col < n_end) gemm::tma_store_2d(&map_c, wbuf + c * 4096u, col, m0);
+                if (col < n_end && col < p.n_tma) gemm::tma_store_2d(&map_c, wbuf + c * 4096u, col, m0);
               }
               gemm::bulk_commit();
+            }
+            // The copies write whole 16-byte pieces, beyond the map's last column too: where C's rows end inside a piece the map ends
+            // before it, and a lane per row stores what is left (1796 x 50257 x 1024 to fp32 with rows of 50260: 155 us, 233 us by
+            // the stores below).
+            const int first = max(p.n_tma, n0 + 2 * g * ncol), last = min(n_end, n0 + 2 * (g + 1) * ncol);
+            if (first < last && m0 + lane < p.M) {
+              const unsigned char* blocks = out_stage + (warp - 4) * 8192;
+              for (int col = first; col < last; ++col) store_staged(p, blocks, lane, col - n0 - 2 * g * ncol, (int64_t)(m0 + lane) * p.ldc + col);
             }
           } else {
             // a C that no tensor map describes (its rows do not start on 16-byte boundaries): the blocks' rows by plain stores of
@@ -416,12 +433,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tn_fp8_kernel(const __grid_co
                 if (i >= 2 && !p.c_bf16) break;
                 const int in = i * 32 + lane, col = n0 + 2 * g * ncol + in;      // bf16: 128 columns, fp32: 64
                 if (col >= n_end) continue;
-                const unsigned char* src = blocks + (in / ncol) * 4096 + r * 128;
-                const int byte = (in % ncol) * (p.c_bf16 ? 2 : 4);
-                src += (((byte >> 4) ^ (r & 7)) << 4) | (byte & 15);
-                const int64_t at = (int64_t)(m0 + r) * p.ldc + col;
-                if (p.c_bf16) reinterpret_cast<unsigned short*>(p.C)[at] = *reinterpret_cast<const unsigned short*>(src);
-                else reinterpret_cast<float*>(p.C)[at] = *reinterpret_cast<const float*>(src);
+                store_staged(p, blocks, r, in, (int64_t)(m0 + r) * p.ldc + col);
               }
             }
           }
@@ -527,8 +539,10 @@ cudaError_t launch(Params p, const void* A, int64_t lda, const void* B, int64_t 
   if (!make_map(&ma, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, A, p.M, K, lda, 128, BM)) return cudaErrorInvalidValue;
   if (!make_map(&mb, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, B, p.N, K, ldb, 128, p.bn)) return cudaErrorInvalidValue;
   mc = ma;
-  p.tma_store = p.c_vec && make_map(&mc, p.c_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, p.c_bf16 ? 2 : 4, p.C, p.M, p.N,
-                                    p.ldc, p.c_bf16 ? 64 : 32, 32);
+  p.n_tma = p.c_vec ? p.N & ~(p.c_bf16 ? 7 : 3) : 0;
+  if (p.n_tma && !make_map(&mc, p.c_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, p.c_bf16 ? 2 : 4, p.C, p.M, p.n_tma,
+                           p.ldc, p.c_bf16 ? 64 : 32, 32))
+    p.n_tma = 0;
   auto kernel = gemm_tn_fp8_kernel<B_ROW_SCALES>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
   if (e != cudaSuccess) return e;

@@ -360,3 +360,20 @@ def test_every_block_meets_its_own_scales(M, N, K, a_br, b_br):
     C, status = dppo.dppo_gemm_tn_fp8(A, sa, B, sb, a_br, b_br)
     assert int(status.item()) == 0
     assert torch.equal(C.double(), exact(A, sa, a_br) @ exact(B, sb, b_br).t())
+
+
+@pytest.mark.parametrize("M,N,K", [(40, 1, 256), (40, 3, 256), (129, 77, 130), (300, 78, 777), (70, 79, 128), (33, 130, 256), (257, 255, 384), (40, 257, 256), (1000, 1001, 640),
+                                   (200, 20001, 300), (64, 37, 8192)])
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("b_br", [1, 128])
+def test_product_into_columns_of_a_wider_matrix(M, N, K, out, b_br):
+    """C's rows start on 16-byte boundaries and end anywhere: what stands behind their last column stays as it was."""
+    A, sa = _operand(M, K, "e4m3", 1, seed=M)
+    B, sb = _operand(N, K, "e4m3", b_br, seed=N)
+    whole, _ = dppo.dppo_gemm_tn_fp8(A, sa, B, sb, 1, b_br, torch.float32)
+    piece = 16 // torch.empty((), dtype=out).element_size()
+    wide = torch.full((M + 1, -(-N // piece) * piece + piece), -3.0, dtype=out, device=DEV)
+    C, status = dppo.dppo_gemm_tn_fp8(A, sa, B, sb, 1, b_br, C=wide[:M, :N])
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0 and torch.equal(C, whole.to(out))
+    assert bool((wide[:M, N:] == -3).all()) and bool((wide[M] == -3).all())
