@@ -89,11 +89,11 @@ cudaError_t launch_gemm_cg(const void* A, int64_t lda, const void* B, int64_t ld
   if (!(B_MN ? make_map(&mb, B, p.K, p.N, ldb, gemm::BK) : make_map(&mb, B, p.N, p.K, ldb, C::B_COLS))) return cudaErrorInvalidValue;
   // plain outputs (every row of every tile goes to its own place in C) are stored through shared memory by bulk tensor
   // copies when the layout allows a tensor map (16-byte aligned base and row pitch)
-  p.tma_store = 0;
+  p.n_tma = 0;
   mc = ma;
   if (EPI == gemm::EPI_STORE_F32 && !p.row_map && !p.c_transposed && !p.m_live && !p.sk_part && p.ldc % 4 == 0 &&
-      ((uintptr_t)p.C % 16) == 0 && make_map_c(&mc, p.C, p.M, p.N, p.ldc))
-    p.tma_store = 1;
+      ((uintptr_t)p.C % 16) == 0 && p.N >= 4 && make_map_c(&mc, p.C, p.M, p.N & ~3, p.ldc))
+    p.n_tma = p.N & ~3;
   int dev = 0, sms = 0;
   cudaGetDevice(&dev);
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);

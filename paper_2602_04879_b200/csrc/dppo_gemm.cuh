@@ -100,8 +100,8 @@ struct Params {
   int inject;            // opts->test_inject
   int accumulate;        // EPI_STORE_F32 (no K split, no row map): the product is added to what C holds (by reductions
                          // performed in L2: the epilogue does not read C)
-  int tma_store;         // EPI_STORE_F32 (no row map, not transposed): map_c describes C (fp32, boxes of 32 x 32, 128-byte
-                         // swizzle) and the epilogue stores (or adds) its blocks through shared memory with bulk tensor
+  int n_tma;             // EPI_STORE_F32 (no row map, not transposed): columns of C that map_c describes, whole 16-byte pieces
+                         // of a row (0: no map; fp32, boxes of 32 x 32, 128-byte swizzle); the epilogue stores (or adds) its blocks through shared memory with bulk tensor
                          // copies: whole 128-byte lines per row instead of 16 bytes per thread and instruction
 };
 
@@ -419,11 +419,12 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tn_kernel(const __grid_consta
 #pragma unroll
           for (int j = 0; j < 32; j += 4) *reinterpret_cast<uint4*>(dst + c + j) = make_uint4(r[j], r[j + 1], r[j + 2], r[j + 3]);
         }
-      } else if (EPI == EPI_STORE_F32 && p.tma_store) {
+      } else if (EPI == EPI_STORE_F32 && p.n_tma) {
         // Through shared memory: the thread writes its row's 32 columns into the warp's 32 x 32 block (16-byte pieces
         // placed by the 128-byte swizzle, so that the 32 rows of a warp do not collide on the banks), one lane hands the
         // block to a bulk tensor copy, which stores it, or adds it to C, 128 contiguous bytes per row; rows and columns
-        // beyond C are clipped by the tensor map.  Two blocks per warp in turn.
+        // beyond C are clipped by the tensor map.  Two blocks per warp in turn.  (The copies write whole 16-byte pieces, beyond
+        // the map's last column too: where C's rows end inside a piece, the map ends before it and the threads store the rest.)
         const float sc = (row_ok && p.row_scale) ? p.row_scale[row] : 1.f;
         const uint32_t wbuf = smem_u32(out_stage) + (uint32_t)q * (2u * 4096u);
 #pragma unroll 1
@@ -446,11 +447,21 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_tn_kernel(const __grid_consta
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) {
-              if (p.accumulate) tma_reduce_add_2d(&map_c, buf, n0 + c, m0 + q * 32);
-              else tma_store_2d(&map_c, buf, n0 + c, m0 + q * 32);
+              if (n0 + c < p.n_tma) {
+                if (p.accumulate) tma_reduce_add_2d(&map_c, buf, n0 + c, m0 + q * 32);
+                else tma_store_2d(&map_c, buf, n0 + c, m0 + q * 32);
+              }
               bulk_commit();
             }
             ++out_it;
+            if (p.n_tma < p.N && n0 + c + 32 > p.n_tma && row_ok) {
+              float* dst = p.C + (int64_t)row * p.ldc + n0 + c;
+#pragma unroll
+              for (int j = 0; j < 32; ++j) {
+                if (n0 + c + j < p.n_tma || n0 + c + j >= p.N) continue;
+                if (p.accumulate) red_add_f32(dst + j, __uint_as_float(r[j])); else dst[j] = __uint_as_float(r[j]);
+              }
+            }
           }
         }
       } else if (EPI == EPI_STORE_F32) {

@@ -498,3 +498,21 @@ def test_fused_full_size_topk_sampled_rows():
     assert np.all(eh <= 2.0 ** -8 * (np.abs(orr["dlogits"]) @ np.abs(W64).T) + 1e-7 * np.abs(orr["dHidden"]).max())
     assert torch.isfinite(out["dW"]).all()
 
+
+
+@pytest.mark.parametrize("M,N,K", [(40, 1, 256), (40, 3, 256), (129, 77, 136), (300, 78, 776), (70, 79, 128), (33, 130, 256), (257, 255, 384), (300, 1001, 640), (200, 20001, 304)])
+@pytest.mark.parametrize("b_mn", [False, True])
+def test_gemm_bf16_into_columns_of_a_wider_matrix(M, N, K, b_mn, cta_group):
+    """C's rows start on 16-byte boundaries and end anywhere: what stands behind their last column stays as it was, and C is what a
+    matrix of its own gets."""
+    g = torch.Generator(device=DEV).manual_seed(M + N)
+    A = torch.randn((M, K), generator=g, device=DEV).to(torch.bfloat16)
+    wide_b = torch.randn((K if b_mn else N, -(-(N if b_mn else K) // 8) * 8), generator=g, device=DEV).to(torch.bfloat16)
+    B = wide_b[:, :N] if b_mn else wide_b[:, :K]
+    product = dppo.dppo_gemm_nn_bf16 if b_mn else dppo.dppo_gemm_tn_bf16
+    whole, _ = product(A, B, cta_group=cta_group)
+    wide = torch.full((M + 1, -(-N // 4) * 4 + 4), -3.0, device=DEV)
+    C, status = product(A, B, C=wide[:M, :N], cta_group=cta_group)
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0 and torch.equal(C, whole)
+    assert bool((wide[:M, N:] == -3).all()) and bool((wide[M] == -3).all())
