@@ -377,3 +377,51 @@ def test_product_into_columns_of_a_wider_matrix(M, N, K, out, b_br):
     torch.cuda.synchronize()
     assert int(status.item()) == 0 and torch.equal(C, whole.to(out))
     assert bool((wide[:M, N:] == -3).all()) and bool((wide[M] == -3).all())
+
+
+def test_8_bit_gradients_against_differences():
+    """dHidden and dW of the 8-bit step against central differences of the loss itself, along a direction made of the entries with little
+    cancellation, so that the operands' rounding leaves less than the slope: a gradient of zero, or of the other sign, fails.
+
+    An element rounds by at most 2^-3 (e5m2) or 2^-4 (e4m3) of itself, or, below the smallest normal value, by half a step of its block:
+    2^-17 / 57344 < 2^-32 or 2^-10 / 448 < 2^-18 of the block's largest.  The product adds (128 + blocks + 3) 2^-23 of the magnitudes.
+    dlogits come from fp32 logits, off by at most (256 + 1) 2^-24 of their magnitudes: 1e-4 of the slope's terms with room to spare."""
+    g = torch.Generator().manual_seed(3)
+    T, d, V = 96, 256, 1000
+    H, W = torch.randn((T, d), generator=g).to(torch.bfloat16).to(DEV), (0.08 * torch.randn((V, d), generator=g)).to(torch.bfloat16).to(DEV)
+    u = torch.rand(T, generator=g, dtype=torch.float64).to(DEV)
+    adv = torch.where(torch.rand(T, generator=g) < 0.5, -1.0, 1.0).to(DEV)
+    qw = dppo.dppo_fp8_quantize(W, block_rows=128, transposed=True)
+    z, _ = dppo.dppo_gemm_tn_bf16(H, W)
+    o = dppo.dppo_sample(z, u, K=20)
+    r = dppo.dppo_loss_fwd_bwd(z, o["sampled_ids"], o["mu_logp"], adv, None, dppo.TOPK_KL, 20, 1e9, o["mu_topk_ids"], o["mu_topk_p"])
+    dq = dppo.dppo_fp8_quantize(r["dlogits"], torch.float8_e5m2, transposed=True)
+    dH, _ = dppo.dppo_gemm_tn_fp8(dq["q"], dq["scale"], qw["qt"], qw["qt_scale"])
+    ht = dppo.dppo_fp8_quantize(H, rowwise=False, transposed=True)
+    dW, _ = dppo.dppo_gemm_tn_fp8(dq["qt"], dq["qt_scale"], ht["qt"], ht["qt_scale"], b_block_rows=1)
+    torch.cuda.synchronize()
+    Hd, Wd, dl = H.double().cpu().numpy(), W.double().cpu().numpy(), r["dlogits"].double().cpu().numpy()
+    a, lmu, A = o["sampled_ids"].cpu().numpy(), o["mu_logp"].double().cpu().numpy(), adv.double().cpu().numpy()
+    _check_slopes(dH.double().cpu().numpy(), dW.double().cpu().numpy(), Hd, Wd, dl, a, lmu, A)
+
+
+def _check_slopes(dH, dW, Hd, Wd, dl, a, lmu, A):
+    T = Hd.shape[0]
+
+    def loss(h, w):
+        zz = h @ w.T
+        m = zz.max(1)
+        lp = zz[np.arange(T), a] - m - np.log(np.exp(zz - m[:, None]).sum(1))
+        return -(np.exp(lp - lmu) * A).mean()
+    for G, left, other, at in ((dH, dl, Wd, lambda s: (Hd + s, Wd)), (dW, dl.T, Hd, lambda s: (Hd, Wd + s))):
+        ref, mag = left @ other, np.abs(left) @ np.abs(other)
+        blocks = -(-left.shape[1] // 128)
+        bound = (2.0 ** -3 + 2.0 ** -4 + 2.0 ** -7 + (128 + blocks + 3) * 2.0 ** -22) * mag
+        bound += 2.0 ** -17 * np.abs(other).max() * np.abs(left).sum(1, keepdims=True) + 2.0 ** -31 * np.abs(left).max() * np.abs(other).sum(0)
+        D = np.where(bound < 0.5 * np.abs(ref), np.sign(ref), 0.0)
+        assert (D != 0).sum() >= 200
+        eps = 1e-5
+        slope = (loss(*at(eps * D)) - loss(*at(-eps * D))) / (2 * eps)
+        tol = (bound * np.abs(D)).sum() + 1e-4 * (mag * np.abs(D)).sum()
+        assert tol < 0.6 * slope
+        assert abs((G * D).sum() - slope) <= tol
