@@ -425,3 +425,41 @@ def _check_slopes(dH, dW, Hd, Wd, dl, a, lmu, A):
         tol = (bound * np.abs(D)).sum() + 1e-4 * (mag * np.abs(D)).sum()
         assert tol < 0.6 * slope
         assert abs((G * D).sum() - slope) <= tol
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_quantize_more_than_2_31_elements(block_rows):
+    """[16389, 151936]: blocks behind element 2^31, as stored and transposed, are what a call on their rows alone gives."""
+    rows, cols, first = 16389, 151936, 16256
+    g = torch.Generator(device=DEV).manual_seed(7)
+    x = torch.empty((rows, cols), dtype=torch.bfloat16, device=DEV)
+    for i in range(0, rows, 2048):
+        x[i:i + 2048] = torch.randn((min(2048, rows - i), cols), generator=g, device=DEV)
+    assert first * cols > 2 ** 31 and first % 128 == 0
+    o = dppo.dppo_fp8_quantize(x, torch.float8_e5m2, block_rows, transposed=True)
+    one = dppo.dppo_fp8_quantize(x, torch.float8_e5m2, block_rows)
+    t = dppo.dppo_fp8_quantize(x[first:], torch.float8_e5m2, block_rows, transposed=True)
+    bits = lambda q: q.contiguous().view(torch.uint8)  # noqa: E731
+    assert int(o["status"].item()) == 0 and torch.equal(bits(o["q"][first:]), bits(t["q"])) and torch.equal(o["scale"][first // block_rows:], t["scale"])
+    assert torch.equal(bits(o["qt"][:, first:]), bits(t["qt"])) and torch.equal(o["qt_scale"][:, first // 128:], t["qt_scale"])
+    assert torch.equal(bits(one["q"][first:]), bits(t["q"])) and torch.equal(one["scale"], o["scale"])
+
+
+@pytest.mark.parametrize("M,N,K,out", [(16389, 151936, 256, torch.bfloat16), (43500, 50257, 128, torch.bfloat16), (43500, 50257, 128, torch.float32), (151936, 128, 16384, torch.float32)])
+def test_product_beyond_2_31_elements(M, N, K, out):
+    """Outputs by bulk tensor stores and by plain ones, and an operand, of more than 2^31 elements: the last rows, with elements of +1 and
+    -1 whose sums are exact in fp32."""
+    g = torch.Generator(device=DEV).manual_seed(8)
+
+    def operand(rows):
+        return ((torch.randint(0, 256, (rows, K), generator=g, dtype=torch.uint8, device=DEV) & 0x80) | 0x38).view(torch.float8_e4m3fn)
+    A, B = operand(M), operand(N)
+    sa = torch.exp2(torch.randint(-1, 2, (M, K // 128), generator=g, device=DEV).float())
+    sb = torch.exp2(torch.randint(-1, 2, (-(-N // 128), K // 128), generator=g, device=DEV).float())
+    C, status = dppo.dppo_gemm_tn_fp8(A, sa, B, sb, out_dtype=out)
+    assert int(status.item()) == 0 and max(M * N, M * K) > 2 ** 31
+    for first in (0, M - 300):
+        a = A[first:first + 300].double() * sa[first:first + 300].double().repeat_interleave(128, 1)
+        for n in range(0, N, 16384):
+            b = B[n:n + 16384].double() * sb.double().repeat_interleave(128, 0)[n:min(N, n + 16384)].repeat_interleave(128, 1)
+            assert torch.equal(C[first:first + 300, n:n + 16384], (a @ b.t()).float().to(out))

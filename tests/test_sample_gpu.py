@@ -389,3 +389,70 @@ def test_a_top_p_of_nothing_within_a_long_top_k(dtype, top_p, top_k, temperature
     for t in (3, 4, 5):
         one = _on_gpu(z[t:t + 1], u[t:t + 1], 0, settings(1))
         assert int(one["sampled_ids"][0]) == int(out["sampled_ids"][t]) == int(z[t].float().argmax())
+
+
+def test_more_than_2_31_logits():
+    """16384 rows of 151936: rows behind element 2^31 are what a call on them alone draws, and what the definition says."""
+    T, V, K = 16384, 151936, 20
+    g = torch.Generator(device=DEV).manual_seed(5)
+    z = torch.empty((T, V), dtype=torch.bfloat16, device=DEV)
+    for i in range(0, T, 2048):
+        z[i:i + 2048] = 3.0 * torch.randn((2048, V), generator=g, device=DEV)
+    u, s = _uniform(T, 5), _settings(T, 5, "tkP")
+    out = _on_gpu(z, u, K, s)
+    first = T - 400
+    assert first * V > 2 ** 31
+    tail = _on_gpu(z[first:], u[first:], K, {n: v[first:] for n, v in s.items()})
+    assert int(out["status"].item()) == 0 and all(torch.equal(out[n][first:], tail[n]) for n in ("sampled_ids", "mu_logp", "mu_topk_ids", "mu_topk_p"))
+    rows = torch.tensor([0, 7000, 14135, 14136, T - 1])
+    few = {n: v[rows.to(DEV)] for n, v in out.items() if n != "status"}
+    _check(dict(few, status=out["status"]), z[rows.to(DEV)], u[rows], K, {n: v[rows] for n, v in s.items()})
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_the_longest_rows(dtype):
+    """V = 2^30, the documented limit: equal weights everywhere, whose running sums are exact, and a thousand tokens far apart."""
+    V = 1 << 30
+    z = torch.full((2, V), 0.5, dtype=dtype, device=DEV)
+    u = torch.tensor([0.999999999, 0.123456789], dtype=torch.float64)
+    out = _on_gpu(z, u, 0, {})
+    assert out["sampled_ids"].tolist() == [int(x * V) for x in u.tolist()] and int(out["status"].item()) == 0
+    assert float((out["mu_logp"].double().cpu() + np.log(V)).abs().max()) <= 2.0 ** -24 * np.log(V) + EDGE
+    where = torch.arange(1023, V, 1 << 20)
+    z.fill_(NEG)
+    vals = 2.0 * torch.randn((2, where.numel()), generator=torch.Generator().manual_seed(6))
+    z[:, where.to(DEV)] = vals.to(dtype).to(DEV)
+    for s in ({}, {"top_k": torch.full((2,), 100, dtype=torch.int32)}, {"top_p": torch.full((2,), 0.9)}, {"min_p": torch.full((2,), 0.05)}):
+        out = _on_gpu(z, u, 10, s)
+        assert int(out["status"].item()) == 0
+        for t in range(2):
+            ora = R.sample_row(vals[t].to(dtype).float().numpy(), u[t].item(), K=10, **{n: v[t].item() for n, v in s.items()})
+            assert out["mu_topk_ids"][t].tolist() == where[ora["top_ids"]].tolist()
+            if ora["margin"] >= EDGE:
+                assert int(out["sampled_ids"][t]) == int(where[ora["id"]])
+                assert abs(float(out["mu_logp"][t]) - ora["logp"]) <= 2.0 ** -24 * abs(ora["logp"]) + EDGE
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("setting", [{"top_p": 0.6}, {"top_k": 1500}, {"top_k": 12000}, {"top_k": 12000, "top_p": 0.6}, {"top_k": 12000, "top_p": 0.6, "min_p": 0.999}])
+def test_each_way_to_a_cut(dtype, setting):
+    """Rows whose cut lies in the first list; below it, among tokens that a step of the histogram tells apart; among more tokens of one
+    step than the list holds (the cut is bracketed); among as many equal ones.  By mass and by count, rows that share SMs and rows
+    that do not."""
+    V, few = 50257, 4
+    g = torch.Generator().manual_seed(41)
+    at = torch.randperm(V, generator=g)
+    z = torch.full((few, V), -20.0)
+    z[0] = 4.0 * torch.randn(V, generator=g)
+    z[1, at[:14000]] = 2.0 + 3.0 * torch.rand(14000, generator=g)
+    z[2, at[:20000]] = 1.0 + 0.01 * torch.rand(20000, generator=g)
+    z[3, at[:20000]] = 1.0
+    z, u = z.to(dtype), _uniform(few, 41)
+
+    def settings(n):
+        return {k: torch.full((n,), v, dtype=torch.int32 if k == "top_k" else torch.float32) for k, v in setting.items()}
+    out = _on_gpu(z, u, 30, settings(few))
+    assert _check(out, z, u, 30, settings(few)) >= few - 1
+    many = _on_gpu(z.repeat(50, 1), u.repeat(50), 30, settings(50 * few))
+    assert torch.equal(many["sampled_ids"].view(50, few), out["sampled_ids"].expand(50, few))
+    assert torch.equal(many["mu_topk_ids"][-few:], out["mu_topk_ids"])
