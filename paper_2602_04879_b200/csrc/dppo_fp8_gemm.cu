@@ -19,17 +19,22 @@
 //                bulk tensor stores
 // With few tiles and a long K a cluster of S CTAs shares a tile: each sums an S-th part of the K blocks, leaves its sums in its shared
 // memory, and all add up a part of the rows each, CTA after CTA (a fixed order), through distributed shared memory.
-// Every wait is bounded (dppo_pipe.cuh).
+// Every wait on an mbarrier is bounded (dppo_pipe.cuh).  The named barriers come to an end because warps 2 and 3 serve every block of
+// every tile whatever happened before (the rule stands at their loop), the cluster barriers because then every warp's loop ends.
 //
-// What bounds it is the hand-over of the P_kb buffers (MMA done -> sums read -> buffer free), two of which are in flight, and the
+// What bounds the K loop is the hand-over of the P_kb buffers (MMA done -> sums read -> buffer free), two of which are in flight, and the
 // fp32 additions themselves (256 of the 512 cycles that the MMAs of a block take at their nominal rate).  Scales have no barrier of
-// their own: the MMA waits for them along with the operands.
+// their own: the MMA waits for them along with the operands.  Outside the K loop: the promotion warps store a finished tile themselves,
+// and the tensor cores stop once both buffers are full (per busy SM, tiles of 16 K blocks run at 14.2 TFLOP/s, of 1187 at 16.1); tiles
+// run with M fastest, so that an A beyond L2 is read again for each column of tiles (151936 x 2048 x 600: 767 MB read where A and B are
+// 92 MB); a last round of few tiles leaves SMs idle (2048 x 2048: 128 tiles on 148 SMs).
 //
-// Measured on B200 (sustained; e4m3, scales 1 x 128 for A and 128 x 128 for B unless said): 4096 x 151936 x 2048 to bf16 1.21 ms =
-// 2.11 PFLOP/s (a bf16 GEMM peaks at 1.67 here); 151936 x 2048 x 2048 with scales 1 x 128 on both sides 1.02 ms = 1.25 PFLOP/s (two packed
-// instructions for two elements instead of one, and the scales' products); 61 x 151936 x 2048 65 us = 5.0 TB/s, 77 % of a copy's
-// rate; 64 x 2048 x 151936 87 us, 600 us without the split along K.  Single-SM tiles were as fast as pairs of SMs (the hand-over
-// sets the pace, not the operands), and simpler to feed scales to.
+// Measured on B200 (the same call over and over; e4m3, scales 1 x 128 for A and 128 x 128 for B unless said): 4096 x 151936 x 2048 to bf16
+// 1.21 ms = 2.11 PFLOP/s (a bf16 GEMM peaks at 1.67 here; on a GPU warm from other work, inputs changed from call to call, 1.39 ms =
+// 1.84 PFLOP/s); 151936 x 2048 x 2048 with scales 1 x 128 on both sides 1.02-1.04 ms = 1.23-1.25 PFLOP/s; 61 x 151936 x 2048 65 us =
+// 5.0 TB/s, 77 % of a copy's rate; 64 x 2048 x 151936 87 us, 500 us without the split along K; to a C that no tensor map describes,
+// 1796 x 50257 x 1024 to fp32 233 us, 132 us with N = 50256.  Single-SM tiles were as fast as pairs of SMs (the hand-over sets the pace, not
+// the operands), and simpler to feed scales to.
 #include <cooperative_groups.h>
 #include <mutex>
 
@@ -155,9 +160,9 @@ __device__ __forceinline__ void promote_rows(float2* acc, const uint32_t* r, flo
 #pragma unroll
   for (int j = 0; j < 32; ++j) acc[j] = __ffma2_rn(make_float2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1])), s2, acc[j]);
 }
-// Reads a fragment of 16 rows x 64 columns (LAST: of buffer b); acc += s0, s1 (the two rows) * sb (the columns') * fragment.  The thread needs only every fourth pair
-// of the column scales: read by one row per thread, each warp would fetch all 128 of them for every block, and the shared
-// memory's 128 bytes a cycle would be what bounds the kernel.
+// Reads a fragment of 16 rows x 64 columns (LAST: of buffer b); acc += s0, s1 (the two rows) * sb (the columns') * fragment.  The thread
+// needs only every fourth pair of the column scales: read by one row per thread, each warp would fetch all 128 of them for every
+// block, and the shared memory's 128 bytes a cycle would be what bounds the kernel.
 // (The products of the scales are formed before the fragment is waited for.)
 template <bool LAST> __device__ __forceinline__ void read_and_promote(uint32_t taddr, float2* acc, float s0, float s1, const float* sb, uint32_t b) {
   float2 w0[8], w1[8];
@@ -500,17 +505,17 @@ EncodeFn get_encode() {
   });
   return fn;
 }
-// Row-major matrix [rows, cols], boxes of box_cols x box_rows (64 or 128 bytes wide, swizzled alike); out of range reads as 0
-bool make_map(CUtensorMap* map, CUtensorMapDataType type, int es, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_cols, int box_rows) {
+// Row-major matrix [rows, cols], boxes of 128 bytes (the swizzle span) x box_rows; out of range reads as 0.  (Stores clip columns at
+// whole 16-byte pieces only: see n_tma.)
+bool make_map(CUtensorMap* map, CUtensorMapDataType type, int es, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
   EncodeFn enc = get_encode();
   if (!enc) return false;
   cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
   cuuint64_t strides[1] = {(cuuint64_t)ld * es};
-  cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
+  cuuint32_t box[2] = {128u / es, (cuuint32_t)box_rows};
   cuuint32_t estr[2] = {1u, 1u};
-  return enc(map, type, 2, const_cast<void*>(base), dims, strides, box, estr,
-             CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols * es == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return enc(map, type, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <bool B_ROW_SCALES>
@@ -518,7 +523,7 @@ cudaError_t launch(Params p, const void* A, int64_t lda, const void* B, int64_t 
   // Tile width (whole blocks of 128 columns) and split: the time of a K block of a tile hardly depends on the width (the hand-over's
   // latency), so a block is counted as 256 + width, a shared tile's exchange as two blocks (four in clusters of 3, 5, 6 or 7, which
   // take a microsecond or two longer: 30 x 1215 x 2500 12.4 us in sevens, 10.4 in eights), and the cheapest choice is taken.
-  // Measured: 600 x 2048 x 151936 210 us in threes, 292 in pairs; 64 x 2048 x 151936 86 us in eights, 497 alone; 512 x 2048 x 8192 19
+  // Measured: 600 x 2048 x 151936 210 us in threes, 292 in pairs; 64 x 2048 x 151936 87 us in eights, 500 alone; 512 x 2048 x 8192 19
   // and 35 us; 4096 x 151936 x 2048 1.17 ms in tiles of 256, 1.79 ms in tiles of 128; where few tiles leave SMs idle the narrow
   // ones win by a tenth.
   const int64_t tm = (p.M + BM - 1) / BM;
@@ -536,12 +541,12 @@ cudaError_t launch(Params p, const void* A, int64_t lda, const void* B, int64_t 
     }
   }
   CUtensorMap ma, mb, mc;
-  if (!make_map(&ma, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, A, p.M, K, lda, 128, BM)) return cudaErrorInvalidValue;
-  if (!make_map(&mb, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, B, p.N, K, ldb, 128, p.bn)) return cudaErrorInvalidValue;
+  if (!make_map(&ma, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, A, p.M, K, lda, BM)) return cudaErrorInvalidValue;
+  if (!make_map(&mb, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, B, p.N, K, ldb, p.bn)) return cudaErrorInvalidValue;
   mc = ma;
   p.n_tma = p.c_vec ? p.N & ~(p.c_bf16 ? 7 : 3) : 0;
   if (p.n_tma && !make_map(&mc, p.c_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, p.c_bf16 ? 2 : 4, p.C, p.M, p.n_tma,
-                           p.ldc, p.c_bf16 ? 64 : 32, 32))
+                           p.ldc, 32))
     p.n_tma = 0;
   auto kernel = gemm_tn_fp8_kernel<B_ROW_SCALES>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
