@@ -26,8 +26,8 @@
 // fp32 additions themselves (256 of the 512 cycles that the MMAs of a block take at their nominal rate).  Scales have no barrier of
 // their own: the MMA waits for them along with the operands.  Outside the K loop: the promotion warps store a finished tile themselves,
 // and the tensor cores stop once both buffers are full (per busy SM, tiles of 16 K blocks run at 14.2 TFLOP/s, of 1187 at 16.1); tiles
-// run with M fastest, so that an A beyond L2 is read again for each column of tiles (151936 x 2048 x 600: 767 MB read where A and B are
-// 92 MB); a last round of few tiles leaves SMs idle (2048 x 2048: 128 tiles on 148 SMs).
+// run with M fastest, so that an A beyond L2 is read again for each column of tiles (151936 x 2048 x 2048: 2.58 GB read where A and
+// B are 315 MB); a last round of few tiles leaves SMs idle (2048 x 2048: 128 tiles on 148 SMs).
 //
 // Measured on B200 (the same call over and over; e4m3, scales 1 x 128 for A and 128 x 128 for B unless said): 4096 x 151936 x 2048 to bf16
 // 1.21 ms = 2.11 PFLOP/s (a bf16 GEMM peaks at 1.67 here; on a GPU warm from other work, inputs changed from call to call, 1.39 ms =
