@@ -101,8 +101,9 @@ struct Params {
   int accumulate;        // EPI_STORE_F32 (no K split, no row map): the product is added to what C holds (by reductions
                          // performed in L2: the epilogue does not read C)
   int n_tma;             // EPI_STORE_F32 (no row map, not transposed): columns of C that map_c describes, whole 16-byte pieces
-                         // of a row (0: no map; fp32, boxes of 32 x 32, 128-byte swizzle); the epilogue stores (or adds) its blocks through shared memory with bulk tensor
-                         // copies: whole 128-byte lines per row instead of 16 bytes per thread and instruction
+                         // of a row (0: no map; fp32, boxes of 32 x 32, 128-byte swizzle); the epilogue stores (or adds) its
+                         // blocks through shared memory with bulk tensor copies: whole 128-byte lines per row instead of 16
+                         // bytes per thread and instruction
 };
 
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar) {
