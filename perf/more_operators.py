@@ -340,7 +340,7 @@ def run(state):
     if s["op"] == "quantize":
         o = dppo.dppo_int4_quantize(s["w"], s["group"], values=True, status=s["status"])
         return {"values": o["values"], "scale": o["scale"]}
-    y, _ = dppo.dppo_matvec_int4(s["x"], s["q"], s["scale"], s["group"], out_dtype=s["out"])
+    y, _ = dppo.dppo_matvec_int4(s["x"], s["q"], s["scale"], s["group"], out_dtype=s["out"], status=s["status"])
     return {"y": y}
 
 
