@@ -62,6 +62,11 @@ enum { DPPO_BINARY_TV = 0, DPPO_BINARY_KL = 1, DPPO_TOPK_TV = 2, DPPO_TOPK_KL = 
        DPPO_GIVEN_D = 6 };
 /* Element types of the logits / dlogits tensors. */
 enum { DPPO_F32 = 0, DPPO_BF16 = 1 };
+/* KL term of dppo_policy_kl_fwd_bwd: over the vocabulary from the reference policy's logits, KL(pi || rho) or KL(rho || pi), or at the
+ * sampled token from the reference policy's log-probability: k3 = e^x - x - 1, x = log rho(a) - log pi(a). */
+enum { DPPO_KL_PI_REF = 0, DPPO_KL_REF_PI = 1, DPPO_KL_K3 = 2 };
+/* Loss of a pair in dppo_preference_fwd_bwd. */
+enum { DPPO_PREF_SIGMOID = 0, DPPO_PREF_IPO = 1, DPPO_PREF_HINGE = 2 };
 /* 8-bit floating-point formats (dppo_fp8_quantize, dppo_gemm_tn_fp8): 4 exponent and 3 mantissa bits without infinities
  * (largest value 448), or 5 and 2 (57344). */
 enum { DPPO_E4M3 = 0, DPPO_E5M2 = 1 };
@@ -101,7 +106,8 @@ enum {
   DPPO_STATUS_BAD_TOPK_ID = 2,    /* a mu_topk_ids entry outside [0, V)     */
   DPPO_STATUS_NONFINITE_ROW = 4,  /* lse of a row is NaN or infinite         */
   DPPO_STATUS_WAIT_LIMIT = 8,     /* a bounded on-chip wait gave up          */
-  DPPO_STATUS_BAD_SAMPLING = 16   /* dppo_sample: a setting of a row outside its range */
+  DPPO_STATUS_BAD_SAMPLING = 16,  /* dppo_sample: a setting of a row outside its range */
+  DPPO_STATUS_BAD_SEQUENCES = 32  /* dppo_preference_fwd_bwd: cu_seqlens falls or leaves [0, T] */
 };
 
 /* Options; all-zero means defaults. */
@@ -406,6 +412,120 @@ int dppo_gemm_tn_fp8(const void* A, int64_t lda, int a_format, int a_block_rows,
                      int64_t b_scale_row_stride, int64_t b_scale_k_stride,
                      int M, int N, int K, void* C, int c_dtype, int64_t ldc,
                      int32_t* status, const dppo_opts* opts, void* cuda_stream);
+
+/*
+ * Log-probabilities of given tokens: logp_t = z_t[a_t] - lse_t (Sec. 3), e.g. of the reference policy for the two losses below.
+ *
+ *  logits, sampled_ids, token_mask, status: as for dppo_loss_fwd_bwd (any row stride; rows may start at any element; T <= 2^27,
+ *              V <= 2^30).  Here and in the three entry points below logits at or below -3.3895e38 (the lowest bf16) count as -inf.
+ *  logp        [T] out: log pi(a_t); -inf where z_t[a_t] is -inf; 0 for rows that are masked or dropped.
+ *  lse         [T] out, 64 bits (what dppo_token_logp_bwd wants), or NULL: 0 for masked rows, NaN for dropped ones.
+ * Needs no workspace; one kernel launch.
+ */
+int dppo_token_logp(const void* logits, int64_t T, int64_t V, int64_t logits_row_stride, int logits_dtype,
+                    const int32_t* sampled_ids, const uint8_t* token_mask, float* logp, double* lse,
+                    int32_t* status, void* cuda_stream);
+
+/*
+ * Its backward pass: dlogits_tj = dlogp_t (1[j = a_t] - pi_tj), for losses made of log-probabilities.
+ *
+ *  lse         [T] as dppo_token_logp gave it for these logits and ids.      dlogp  [T] derivative by logp_t.
+ *  dlogits     [T, V] out, dtype per dlogits_dtype (DPPO_DLOGITS_SAME or DPPO_DLOGITS_F32); in place or disjoint, as for
+ *              dppo_loss_fwd_bwd.  Rows that are masked, dropped or have dlogp_t = 0 are zero.
+ * Needs no workspace; one kernel launch.
+ */
+int dppo_token_logp_bwd(const void* logits, int64_t T, int64_t V, int64_t logits_row_stride, int logits_dtype,
+                        const int32_t* sampled_ids, const uint8_t* token_mask, const double* lse, const float* dlogp,
+                        int dlogits_dtype, void* dlogits, int64_t dlogits_row_stride, int32_t* status, void* cuda_stream);
+
+/*
+ * Clipped policy loss with a KL term to a reference policy rho, forward and backward (the paper's baselines of App. C.1 clip the ratio;
+ * the KL term is what PPO / GRPO runs against a reference model add to that).  With r_t = pi(a_t) / mu(a_t):
+ *
+ *   loss = s sum_t [ -min(r_t A_t, clip(r_t, 1 - eps_low, 1 + eps_high) A_t) + kl_coef KL_t ]
+ *   M_t = 0 where the clip holds (A_t > 0 and r_t > 1 + eps_high, or A_t < 0 and r_t < 1 - eps_low), 1 otherwise
+ *   dlogits_tj = s ( M_t r_t A_t (pi_tj - 1[j = a_t]) + kl_coef dKL_t / dz_tj )
+ *   KL_t by kl_form: KL(pi || rho), KL(rho || pi), or k3 (see the enum); the KL term is not masked by M_t.
+ *
+ *  logits, sampled_ids, mu_logp, advantages, token_mask, status: as for dppo_loss_fwd_bwd.
+ *  ref_logits     [T, V] of the logits' dtype, own row stride (DPPO_KL_PI_REF, DPPO_KL_REF_PI; ignored otherwise).
+ *  ref_logp       [T] log rho(a_t) (DPPO_KL_K3; ignored otherwise).
+ *  kl_coef        >= 0, finite.      eps_low, eps_high  >= 0; +inf: no clip on that side.
+ *  opts           loss_scale and dlogits_dtype apply.
+ *  loss [1], kl [T], mask [T] (M_t), dlogits [T, V] (in place of logits or disjoint; disjoint from ref_logits), stats [8] or NULL
+ *                 (as for dppo_loss_fwd_bwd, with KL_t for D_t).
+ *  workspace      dppo_workspace_bytes(T, V, 0, 0) bytes, 256-byte aligned.
+ * Rows whose KL or loss term is infinite (pi has mass where rho has none, or the reverse for KL(rho || pi)) are dropped with
+ * DPPO_STATUS_NONFINITE_ROW, as rows with non-finite logits in either tensor are.
+ */
+int dppo_policy_kl_fwd_bwd(const void* logits, int64_t T, int64_t V, int64_t logits_row_stride, int logits_dtype,
+                           const void* ref_logits, int64_t ref_row_stride, const float* ref_logp,
+                           const int32_t* sampled_ids, const float* mu_logp, const float* advantages,
+                           const uint8_t* token_mask, int kl_form, float kl_coef, float eps_low, float eps_high,
+                           const dppo_opts* opts, float* loss, float* kl, uint8_t* mask, void* dlogits,
+                           int64_t dlogits_row_stride, float* stats, int32_t* status,
+                           void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Bytes of device scratch dppo_preference_fwd_bwd needs for T rows and P pairs (256-byte aligned pointer expected). */
+size_t dppo_preference_workspace_bytes(int64_t T, int64_t P);
+
+/*
+ * Loss over pairs of a preferred and a rejected sequence, forward and backward.  Sequence q owns the rows cu_seqlens[q] ..
+ * cu_seqlens[q + 1] - 1; pair p is the sequences 2p (preferred) and 2p + 1 (rejected).  With R_q = beta sum over the sequence's valid rows
+ * of (log pi(a_t) - ref_logp_t), divided by their number where `average` is set, and h = R_2p - R_2p+1 - margin:
+ *
+ *   DPPO_PREF_SIGMOID  -(1 - e) log sigmoid(h) - e log sigmoid(-h),  e = label_smoothing
+ *   DPPO_PREF_IPO      (h / beta - 1 / (2 beta))^2
+ *   DPPO_PREF_HINGE    max(0, 1 - h)
+ *   loss = s * sum over the pairs;  s = opts->loss_scale, or 1 / (number of pairs that count)
+ *
+ *  logits, sampled_ids, token_mask, status: as for dppo_loss_fwd_bwd.  Rows outside the sequences are treated as masked ones: not read,
+ *                 zero gradient.
+ *  ref_logp       [T] the reference policy's log-probabilities (dppo_token_logp); NULL = 0 (a loss without a reference).
+ *  cu_seqlens     [2 P + 1] int64 device words, not falling, within [0, T]; otherwise DPPO_STATUS_BAD_SEQUENCES, loss and gradient zero.
+ *  beta           > 0.    label_smoothing  0 .. 0.5, 0 unless DPPO_PREF_SIGMOID.    margin  finite.    P <= 2^24.
+ *  opts           loss_scale and dlogits_dtype apply.
+ *  loss [1], reward [2 P] (R_q), logp [T], dlogits [T, V] (in place or disjoint).
+ *  workspace      dppo_preference_workspace_bytes(T, P) bytes, 256-byte aligned.
+ * A pair with a sequence without valid rows does not count.  A pair with a dropped row, or whose h is not finite, is dropped as a whole
+ * (rewards 0, zero gradient, a status bit) and does not count either.
+ */
+int dppo_preference_fwd_bwd(const void* logits, int64_t T, int64_t V, int64_t logits_row_stride, int logits_dtype,
+                            const int32_t* sampled_ids, const uint8_t* token_mask, const float* ref_logp,
+                            const int64_t* cu_seqlens, int64_t P, int variant, float beta, float label_smoothing,
+                            float margin, int average, const dppo_opts* opts, float* loss, float* reward, float* logp,
+                            void* dlogits, int64_t dlogits_row_stride, int32_t* status,
+                            void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Rounds a matrix to 4 bits with one bf16 scale per group of 32, 64 or 128 elements of a row (groups at the end of a row are smaller):
+ * the weights of dppo_matvec_int4.
+ *
+ *  x          [rows, cols] row-major, row stride in elements, x_dtype DPPO_F32 or DPPO_BF16.
+ *  q          out, two codes to a byte: columns 2i (low half) and 2i + 1 (high half) at q[row * q_row_stride + i], row stride in bytes,
+ *             >= ceil(cols / 2); bytes behind a row are left alone, the half byte behind an odd last column is 0.
+ *             code = round(x / scale) + 8, ties to even, 1 .. 15; it stands for (code - 8) * scale.
+ *  scale      out, bf16, group g of a row at scale[row * scale_row_stride + g]: max(amax, 2^-100) / 7 rounded once to bf16.
+ *  values     [rows, cols] out in x's dtype: what the codes stand for, rounded once; NULL: not wanted.  May be x itself.
+ *  status     device word: DPPO_STATUS_NONFINITE_ROW if a group holds a NaN or an infinity; its scale and values are NaN.
+ * rows * cols <= 2^38, cols <= 2^30, at most 2^41 columns of rows rounded up to whole groups.  One kernel launch.
+ */
+int dppo_int4_quantize(const void* x, int64_t rows, int64_t cols, int64_t x_row_stride, int x_dtype, int group,
+                       uint8_t* q, int64_t q_row_stride, void* scale, int64_t scale_row_stride,
+                       void* values, int64_t values_row_stride, int32_t* status, void* cuda_stream);
+
+/*
+ * y[M, N] = x[M, K] . w[N, K]^T for a few bf16 rows (a decoding step) and weights in 4 bits:
+ *   y[m, n] = sum_g scale[n, g] sum_{k in group g} x[m, k] (code[n, k] - 8),   each group's sum and their sum in fp32.
+ *
+ *  x [M, K] bf16, q and scale as dppo_int4_quantize lays them out (codes 0 .. 15), y [M, N] DPPO_F32 or DPPO_BF16 (rounded once); row
+ *  strides in elements, of q in bytes.  Any M is right; the kernel is made for M up to 64.  With q and its row stride on
+ *  16-byte boundaries the weights come by bulk copies, otherwise element by element (several times slower).
+ *  y must not overlap the inputs.  K = 0 gives y = 0.  status: device word, DPPO_STATUS_WAIT_LIMIT.  opts: wait_limit_us, test_inject.
+ */
+int dppo_matvec_int4(const void* x, int64_t x_row_stride, const uint8_t* q, int64_t q_row_stride, const void* scale,
+                     int64_t scale_row_stride, int group, int64_t M, int64_t N, int64_t K, void* y, int y_dtype,
+                     int64_t y_row_stride, int32_t* status, const dppo_opts* opts, void* cuda_stream);
 
 /* Name of an error code (static string, never NULL). */
 const char* dppo_error_string(int code);

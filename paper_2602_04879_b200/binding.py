@@ -18,7 +18,9 @@ F32, BF16 = 0, 1
 DLOGITS_SAME, DLOGITS_F32 = 0, 1
 KERNEL_AUTO, KERNEL_GENERIC, KERNEL_RING = 0, 1, 2
 INJECT_NO_COPIES = 1
-STATUS_BAD_SAMPLED_ID, STATUS_BAD_TOPK_ID, STATUS_NONFINITE_ROW, STATUS_WAIT_LIMIT, STATUS_BAD_SAMPLING = 1, 2, 4, 8, 16
+STATUS_BAD_SAMPLED_ID, STATUS_BAD_TOPK_ID, STATUS_NONFINITE_ROW, STATUS_WAIT_LIMIT, STATUS_BAD_SAMPLING, STATUS_BAD_SEQUENCES = 1, 2, 4, 8, 16, 32
+KL_PI_REF, KL_REF_PI, KL_K3 = 0, 1, 2
+PREF_SIGMOID, PREF_IPO, PREF_HINGE = 0, 1, 2
 E4M3, E5M2 = 0, 1
 FP8_FORMATS = {torch.float8_e4m3fn: E4M3, torch.float8_e5m2: E5M2}
 VARIANTS = {"binary_tv": BINARY_TV, "binary_kl": BINARY_KL, "topk_tv": TOPK_TV, "topk_kl": TOPK_KL, "ppo_clip": PPO_CLIP, "minimal_mask": MINIMAL_MASK, "given_d": GIVEN_D}
@@ -102,6 +104,27 @@ def lib():
         L.dppo_gemm_tn_fp8.argtypes = [c_void_p, c_int64, c_int, c_int, c_void_p, c_int64, c_int64,
                                        c_void_p, c_int64, c_int, c_int, c_void_p, c_int64, c_int64,
                                        c_int, c_int, c_int, c_void_p, c_int, c_int64, c_void_p, POINTER(DppoOpts), c_void_p]
+        L.dppo_token_logp.restype = c_int
+        L.dppo_token_logp.argtypes = [c_void_p, c_int64, c_int64, c_int64, c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
+        L.dppo_token_logp_bwd.restype = c_int
+        L.dppo_token_logp_bwd.argtypes = [c_void_p, c_int64, c_int64, c_int64, c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_int64,
+                                          c_void_p, c_void_p]
+        L.dppo_policy_kl_fwd_bwd.restype = c_int
+        L.dppo_policy_kl_fwd_bwd.argtypes = [c_void_p, c_int64, c_int64, c_int64, c_int, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_void_p,
+                                             c_void_p, c_int, c_float, c_float, c_float, POINTER(DppoOpts), c_void_p, c_void_p, c_void_p, c_void_p,
+                                             c_int64, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+        L.dppo_preference_workspace_bytes.restype = c_size_t
+        L.dppo_preference_workspace_bytes.argtypes = [c_int64, c_int64]
+        L.dppo_preference_fwd_bwd.restype = c_int
+        L.dppo_preference_fwd_bwd.argtypes = [c_void_p, c_int64, c_int64, c_int64, c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int,
+                                              c_float, c_float, c_float, c_int, POINTER(DppoOpts), c_void_p, c_void_p, c_void_p, c_void_p, c_int64,
+                                              c_void_p, c_void_p, c_size_t, c_void_p]
+        L.dppo_int4_quantize.restype = c_int
+        L.dppo_int4_quantize.argtypes = [c_void_p, c_int64, c_int64, c_int64, c_int, c_int, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64,
+                                         c_void_p, c_void_p]
+        L.dppo_matvec_int4.restype = c_int
+        L.dppo_matvec_int4.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_int, c_int64, c_int64, c_int64, c_void_p, c_int,
+                                       c_int64, c_void_p, POINTER(DppoOpts), c_void_p]
         _lib = L
     return _lib
 
@@ -496,3 +519,198 @@ def dppo_gemm_tn_fp8(A, a_scale, B, b_scale, a_block_rows=1, b_block_rows=128, o
     if rc != 0:
         raise DppoError(rc, "dppo_gemm_tn_fp8")
     return C, status
+
+
+def _rows_ok(logits, vectors):
+    """The shared checks of the entry points below: logits [T,V] with contiguous rows, and per-row vectors (name, tensor or None, type)."""
+    assert logits.is_cuda and logits.dim() == 2 and (logits.shape[1] <= 1 or logits.stride(1) == 1), "logits"
+    T, dev = logits.shape[0], logits.device
+    for name, t, dt in vectors:
+        assert t is None or (t.dtype == dt and t.shape == (T,) and t.device == dev and t.is_contiguous()), name
+
+
+def _row_stride(t):
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _gradient_out(logits, dlogits, dlogits_f32):
+    dt = torch.float32 if dlogits_f32 else logits.dtype
+    if dlogits is None:
+        return torch.empty(logits.shape, dtype=dt, device=logits.device)
+    assert dlogits.device == logits.device and dlogits.dtype == dt and dlogits.shape == logits.shape, "dlogits"
+    assert dlogits.shape[1] <= 1 or dlogits.stride(1) == 1, "dlogits"
+    return dlogits
+
+
+def _scratch(workspace, nbytes, dev):
+    if workspace is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    assert workspace.device == dev and workspace.dtype == torch.uint8 and workspace.is_contiguous(), "workspace"
+    return workspace
+
+
+def dppo_token_logp(logits, sampled_ids, token_mask=None, status=None, stream=None):
+    """Calls ``dppo_token_logp`` on CUDA tensors: log-probabilities of the tokens ``sampled_ids`` [T] int32 under the rows of
+    ``logits`` [T,V] (fp32 or bf16, any row stride).  Returns dict(logp[T] fp32, lse[T] float64, status[1]); nothing is synchronised.
+    ``stream``: another than the current one; what is allocated here then belongs to it."""
+    if stream is not None:
+        assert stream.device == logits.device, "stream"
+        with torch.cuda.stream(stream):
+            return dppo_token_logp(logits, sampled_ids, token_mask, status)
+    _rows_ok(logits, (("sampled_ids", sampled_ids, torch.int32), ("token_mask", token_mask, torch.uint8)))
+    T, V = logits.shape
+    dev = logits.device
+    logp, lse = torch.empty(T, dtype=torch.float32, device=dev), torch.empty(T, dtype=torch.float64, device=dev)
+    status = _status_word(status, dev)
+    rc = _on(dev, lambda st: lib().dppo_token_logp(logits.data_ptr(), T, V, _row_stride(logits), _dtype_code(logits), sampled_ids.data_ptr(),
+                                                   _adr(token_mask), logp.data_ptr(), lse.data_ptr(), status.data_ptr(), st))
+    if rc != 0:
+        raise DppoError(rc, "dppo_token_logp")
+    return dict(logp=logp, lse=lse, status=status)
+
+
+def dppo_token_logp_bwd(logits, sampled_ids, lse, dlogp, token_mask=None, dlogits_f32=False, dlogits=None, status=None, stream=None):
+    """Calls ``dppo_token_logp_bwd``: the gradient by the logits of a loss whose derivative by the log-probabilities is ``dlogp`` [T] fp32;
+    ``lse`` as ``dppo_token_logp`` returned it.  ``dlogits``: a tensor to write into (the logits themselves: in place).  Returns
+    dict(dlogits[T,V], status[1])."""
+    if stream is not None:
+        assert stream.device == logits.device, "stream"
+        with torch.cuda.stream(stream):
+            return dppo_token_logp_bwd(logits, sampled_ids, lse, dlogp, token_mask, dlogits_f32, dlogits, status)
+    _rows_ok(logits, (("sampled_ids", sampled_ids, torch.int32), ("lse", lse, torch.float64), ("dlogp", dlogp, torch.float32),
+                      ("token_mask", token_mask, torch.uint8)))
+    T, V = logits.shape
+    dev = logits.device
+    dlogits = _gradient_out(logits, dlogits, dlogits_f32)
+    status = _status_word(status, dev)
+    rc = _on(dev, lambda st: lib().dppo_token_logp_bwd(
+        logits.data_ptr(), T, V, _row_stride(logits), _dtype_code(logits), sampled_ids.data_ptr(), _adr(token_mask), lse.data_ptr(), dlogp.data_ptr(),
+        DLOGITS_F32 if dlogits_f32 else DLOGITS_SAME, dlogits.data_ptr(), _row_stride(dlogits), status.data_ptr(), st))
+    if rc != 0:
+        raise DppoError(rc, "dppo_token_logp_bwd")
+    return dict(dlogits=dlogits, status=status)
+
+
+def dppo_policy_kl_fwd_bwd(logits, sampled_ids, mu_logp, advantages, token_mask=None, ref_logits=None, ref_logp=None, kl_form=KL_K3, kl_coef=0.04,
+                           eps_low=0.2, eps_high=0.2, loss_scale=0.0, dlogits_f32=False, dlogits=None, want_stats=False, workspace=None, status=None,
+                           stream=None):
+    """Calls ``dppo_policy_kl_fwd_bwd`` on CUDA tensors: the clipped policy loss plus ``kl_coef`` times the KL term ``kl_form`` (KL_PI_REF,
+    KL_REF_PI: from ``ref_logits`` [T,V]; KL_K3: from ``ref_logp`` [T]).  Returns dict(loss[1], kl[T], mask[T], dlogits[T,V], stats[8] or
+    None, status[1]); nothing is synchronised.  ``dlogits`` may be the logits themselves."""
+    if stream is not None:
+        assert stream.device == logits.device, "stream"
+        with torch.cuda.stream(stream):
+            return dppo_policy_kl_fwd_bwd(logits, sampled_ids, mu_logp, advantages, token_mask, ref_logits, ref_logp, kl_form, kl_coef, eps_low, eps_high,
+                                          loss_scale, dlogits_f32, dlogits, want_stats, workspace, status)
+    _rows_ok(logits, (("sampled_ids", sampled_ids, torch.int32), ("mu_logp", mu_logp, torch.float32), ("advantages", advantages, torch.float32),
+                      ("token_mask", token_mask, torch.uint8), ("ref_logp", ref_logp, torch.float32)))
+    T, V = logits.shape
+    dev = logits.device
+    if ref_logits is not None:
+        assert ref_logits.device == dev and ref_logits.dtype == logits.dtype and ref_logits.shape == (T, V), "ref_logits"
+        assert V <= 1 or ref_logits.stride(1) == 1, "ref_logits"
+    dlogits = _gradient_out(logits, dlogits, dlogits_f32)
+    loss, kl = torch.empty(1, dtype=torch.float32, device=dev), torch.empty(T, dtype=torch.float32, device=dev)
+    mask = torch.empty(T, dtype=torch.uint8, device=dev)
+    stats = torch.empty(8, dtype=torch.float32, device=dev) if want_stats else None
+    status = _status_word(status, dev)
+    workspace = _scratch(workspace, dppo_workspace_bytes(T, V), dev)
+    opts = ctypes.byref(_opts(loss_scale, dlogits_f32))
+    rc = _on(dev, lambda st: lib().dppo_policy_kl_fwd_bwd(
+        logits.data_ptr(), T, V, _row_stride(logits), _dtype_code(logits), _adr(ref_logits), _row_stride(ref_logits) if ref_logits is not None else V,
+        _adr(ref_logp), sampled_ids.data_ptr(), mu_logp.data_ptr(), advantages.data_ptr(), _adr(token_mask), int(kl_form), float(kl_coef), float(eps_low),
+        float(eps_high), opts, loss.data_ptr(), kl.data_ptr(), mask.data_ptr(), dlogits.data_ptr(), _row_stride(dlogits), _adr(stats), status.data_ptr(),
+        workspace.data_ptr(), workspace.numel(), st))
+    if rc != 0:
+        raise DppoError(rc, "dppo_policy_kl_fwd_bwd")
+    return dict(loss=loss, kl=kl, mask=mask, dlogits=dlogits, stats=stats, status=status)
+
+
+def dppo_preference_workspace_bytes(T, P):
+    return int(lib().dppo_preference_workspace_bytes(int(T), int(P)))
+
+
+def dppo_preference_fwd_bwd(logits, sampled_ids, cu_seqlens, ref_logp=None, token_mask=None, variant=PREF_SIGMOID, beta=0.1, label_smoothing=0.0,
+                            margin=0.0, average=False, loss_scale=0.0, dlogits_f32=False, dlogits=None, workspace=None, status=None, stream=None):
+    """Calls ``dppo_preference_fwd_bwd`` on CUDA tensors: the loss over pairs of sequences (2p preferred, 2p+1 rejected), sequence q being the
+    rows ``cu_seqlens[q] .. cu_seqlens[q+1]-1`` (int64 [2P+1] on the device) of ``logits`` [T,V].  ``ref_logp`` [T] fp32: the reference
+    policy's log-probabilities, None = 0.  Returns dict(loss[1], reward[2P], logp[T], dlogits[T,V], status[1]); nothing is synchronised.
+    ``dlogits`` may be the logits themselves."""
+    if stream is not None:
+        assert stream.device == logits.device, "stream"
+        with torch.cuda.stream(stream):
+            return dppo_preference_fwd_bwd(logits, sampled_ids, cu_seqlens, ref_logp, token_mask, variant, beta, label_smoothing, margin, average,
+                                           loss_scale, dlogits_f32, dlogits, workspace, status)
+    _rows_ok(logits, (("sampled_ids", sampled_ids, torch.int32), ("ref_logp", ref_logp, torch.float32), ("token_mask", token_mask, torch.uint8)))
+    T, V = logits.shape
+    dev = logits.device
+    assert cu_seqlens.device == dev and cu_seqlens.dtype == torch.int64 and cu_seqlens.dim() == 1 and cu_seqlens.is_contiguous(), "cu_seqlens"
+    assert cu_seqlens.numel() % 2 == 1, "cu_seqlens: 2 P + 1 entries"
+    P = cu_seqlens.numel() // 2
+    dlogits = _gradient_out(logits, dlogits, dlogits_f32)
+    loss, reward = torch.empty(1, dtype=torch.float32, device=dev), torch.empty(2 * P, dtype=torch.float32, device=dev)
+    logp = torch.empty(T, dtype=torch.float32, device=dev)
+    status = _status_word(status, dev)
+    workspace = _scratch(workspace, dppo_preference_workspace_bytes(T, P), dev)
+    opts = ctypes.byref(_opts(loss_scale, dlogits_f32))
+    rc = _on(dev, lambda st: lib().dppo_preference_fwd_bwd(
+        logits.data_ptr(), T, V, _row_stride(logits), _dtype_code(logits), sampled_ids.data_ptr(), _adr(token_mask), _adr(ref_logp), cu_seqlens.data_ptr(), P,
+        int(variant), float(beta), float(label_smoothing), float(margin), 1 if average else 0, opts, loss.data_ptr(), reward.data_ptr(), logp.data_ptr(),
+        dlogits.data_ptr(), _row_stride(dlogits), status.data_ptr(), workspace.data_ptr(), workspace.numel(), st))
+    if rc != 0:
+        raise DppoError(rc, "dppo_preference_fwd_bwd")
+    return dict(loss=loss, reward=reward, logp=logp, dlogits=dlogits, status=status)
+
+
+INT4_GROUPS = (32, 64, 128)
+
+
+def dppo_int4_quantize(x, group=128, values=False, status=None, stream=None):
+    """Calls ``dppo_int4_quantize`` on a CUDA matrix x [rows,cols] (fp32 or bf16, any row stride).  Returns dict(q, scale, values, status): q
+    uint8 [rows, ceil(cols/2)], two codes to a byte, in rows that start on 16-byte boundaries as ``dppo_matvec_int4`` reads them
+    fastest; scale bf16 [rows, ceil(cols/group)]; with ``values`` the numbers that they stand for, in x's type (None otherwise)."""
+    if stream is not None:
+        assert stream.device == x.device, "stream"
+        with torch.cuda.stream(stream):
+            return dppo_int4_quantize(x, group, values, status)
+    assert x.is_cuda and x.dim() == 2 and (x.shape[1] <= 1 or x.stride(1) == 1), "x"
+    rows, cols = x.shape
+    dev, nbytes = x.device, (cols + 1) // 2
+    G = int(group) if int(group) in INT4_GROUPS else 32            # (the call refuses another)
+    q = torch.empty_strided((rows, nbytes), (max(16, -(-nbytes // 16) * 16), 1), dtype=torch.uint8, device=dev)
+    scale = torch.empty((rows, -(-cols // G)), dtype=torch.bfloat16, device=dev)
+    out = torch.empty((rows, cols), dtype=x.dtype, device=dev) if values else None
+    status = _status_word(status, dev)
+    rc = _on(dev, lambda st: lib().dppo_int4_quantize(x.data_ptr(), rows, cols, _row_stride(x), _dtype_code(x), int(group), q.data_ptr(), q.stride(0),
+                                                      scale.data_ptr(), scale.stride(0) if rows > 1 else scale.shape[1], _adr(out), cols,
+                                                      status.data_ptr(), st))
+    if rc != 0:
+        raise DppoError(rc, "dppo_int4_quantize")
+    return dict(q=q, scale=scale, values=out, status=status)
+
+
+def dppo_matvec_int4(x, q, scale, group=128, out_dtype=torch.float32, y=None, status=None, stream=None, wait_limit_us=0, test_inject=0):
+    """y[M,N] = x[M,K] . w[N,K]^T for bf16 rows x and weights in 4 bits, q uint8 [N, at least ceil(K/2)] and scale bf16 [N, ceil(K/group)] as
+    ``dppo_int4_quantize`` returns them.  Returns (y, status), y fp32 or bf16; nothing is synchronised."""
+    if stream is not None:
+        assert stream.device == x.device, "stream"
+        with torch.cuda.stream(stream):
+            return dppo_matvec_int4(x, q, scale, group, out_dtype, y, status, None, wait_limit_us, test_inject)
+    assert x.is_cuda and x.dtype == torch.bfloat16 and x.dim() == 2 and (x.shape[1] <= 1 or x.stride(1) == 1), "x"
+    M, K = x.shape
+    dev = x.device
+    assert q.device == dev and q.dtype == torch.uint8 and q.dim() == 2 and q.shape[1] >= (K + 1) // 2 and (q.shape[1] <= 1 or q.stride(1) == 1), "q"
+    N = q.shape[0]
+    G = int(group) if int(group) in INT4_GROUPS else 32
+    assert scale.device == dev and scale.dtype == torch.bfloat16 and scale.shape == (N, -(-K // G)) and (scale.shape[1] <= 1 or scale.stride(1) == 1), "scale"
+    if y is None:
+        y = torch.empty((M, N), dtype=out_dtype, device=dev)
+    assert y.device == dev and y.shape == (M, N) and (N <= 1 or y.stride(1) == 1), "y"
+    status = _status_word(status, dev)
+    opts = None if wait_limit_us == 0 and test_inject == 0 else ctypes.byref(_opts(wait_limit_us=wait_limit_us, test_inject=test_inject))
+    rc = _on(dev, lambda st: lib().dppo_matvec_int4(
+        x.data_ptr(), _row_stride(x), q.data_ptr(), q.stride(0) if N > 1 else max(16, -(-q.shape[1] // 16) * 16), scale.data_ptr(),
+        scale.stride(0) if N > 1 else scale.shape[1], int(group), M, N, K, y.data_ptr(), _dtype_code(y), _row_stride(y), status.data_ptr(), opts, st))
+    if rc != 0:
+        raise DppoError(rc, "dppo_matvec_int4")
+    return y, status
