@@ -451,10 +451,11 @@ int dppo_token_logp_bwd(const void* logits, int64_t T, int64_t V, int64_t logits
  *  ref_logits     [T, V] of the logits' dtype, own row stride (DPPO_KL_PI_REF, DPPO_KL_REF_PI; ignored otherwise).
  *  ref_logp       [T] log rho(a_t) (DPPO_KL_K3; ignored otherwise).
  *  kl_coef        >= 0, finite.      eps_low, eps_high  >= 0; +inf: no clip on that side.
- *  opts           loss_scale and dlogits_dtype apply.
+ *  opts           loss_scale, dlogits_dtype, wait_limit_us and test_inject apply.
  *  loss [1], kl [T], mask [T] (M_t), dlogits [T, V] (in place of logits or disjoint; disjoint from ref_logits), stats [8] or NULL
  *                 (as for dppo_loss_fwd_bwd, with KL_t for D_t).
- *  workspace      dppo_workspace_bytes(T, V, 0, 0) bytes, 256-byte aligned.
+ *  workspace      dppo_workspace_bytes(T, V, 0, 0) bytes, 256-byte aligned; needs no initialisation.  Calls that can
+ *                 overlap on the GPU need one each.
  * Rows whose KL or loss term is infinite (pi has mass where rho has none, or the reverse for KL(rho || pi)) are dropped with
  * DPPO_STATUS_NONFINITE_ROW, as rows with non-finite logits in either tensor are.
  */

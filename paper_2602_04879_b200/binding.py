@@ -593,7 +593,7 @@ def dppo_token_logp_bwd(logits, sampled_ids, lse, dlogp, token_mask=None, dlogit
 
 def dppo_policy_kl_fwd_bwd(logits, sampled_ids, mu_logp, advantages, token_mask=None, ref_logits=None, ref_logp=None, kl_form=KL_K3, kl_coef=0.04,
                            eps_low=0.2, eps_high=0.2, loss_scale=0.0, dlogits_f32=False, dlogits=None, want_stats=False, workspace=None, status=None,
-                           stream=None):
+                           stream=None, wait_limit_us=0, test_inject=0):
     """Calls ``dppo_policy_kl_fwd_bwd`` on CUDA tensors: the clipped policy loss plus ``kl_coef`` times the KL term ``kl_form`` (KL_PI_REF,
     KL_REF_PI: from ``ref_logits`` [T,V]; KL_K3: from ``ref_logp`` [T]).  Returns dict(loss[1], kl[T], mask[T], dlogits[T,V], stats[8] or
     None, status[1]); nothing is synchronised.  ``dlogits`` may be the logits themselves."""
@@ -601,7 +601,7 @@ def dppo_policy_kl_fwd_bwd(logits, sampled_ids, mu_logp, advantages, token_mask=
         assert stream.device == logits.device, "stream"
         with torch.cuda.stream(stream):
             return dppo_policy_kl_fwd_bwd(logits, sampled_ids, mu_logp, advantages, token_mask, ref_logits, ref_logp, kl_form, kl_coef, eps_low, eps_high,
-                                          loss_scale, dlogits_f32, dlogits, want_stats, workspace, status)
+                                          loss_scale, dlogits_f32, dlogits, want_stats, workspace, status, None, wait_limit_us, test_inject)
     _rows_ok(logits, (("sampled_ids", sampled_ids, torch.int32), ("mu_logp", mu_logp, torch.float32), ("advantages", advantages, torch.float32),
                       ("token_mask", token_mask, torch.uint8), ("ref_logp", ref_logp, torch.float32)))
     T, V = logits.shape
@@ -615,7 +615,7 @@ def dppo_policy_kl_fwd_bwd(logits, sampled_ids, mu_logp, advantages, token_mask=
     stats = torch.empty(8, dtype=torch.float32, device=dev) if want_stats else None
     status = _status_word(status, dev)
     workspace = _scratch(workspace, dppo_workspace_bytes(T, V), dev)
-    opts = ctypes.byref(_opts(loss_scale, dlogits_f32))
+    opts = ctypes.byref(_opts(loss_scale, dlogits_f32, wait_limit_us=wait_limit_us, test_inject=test_inject))
     rc = _on(dev, lambda st: lib().dppo_policy_kl_fwd_bwd(
         logits.data_ptr(), T, V, _row_stride(logits), _dtype_code(logits), _adr(ref_logits), _row_stride(ref_logits) if ref_logits is not None else V,
         _adr(ref_logp), sampled_ids.data_ptr(), mu_logp.data_ptr(), advantages.data_ptr(), _adr(token_mask), int(kl_form), float(kl_coef), float(eps_low),

@@ -74,28 +74,25 @@ __global__ void __launch_bounds__(kThreads) token_logp_kernel(LogpParams p) {
   if (CL > 1) cluster_arrive();            // (the peers have to run before anything is sent to them)
   const InT* row = reinterpret_cast<const InT*>(p.z) + t * p.ld;
   const uint32_t head = head_of(row);
-  const RowRef<const InT> r(row, head);
-  const int64_t nvec = ((int64_t)head + p.V + N - 1) / N;
-  const int64_t av = ((int64_t)a + head) / N;              // the token's vector, and its place there
-  const int ai = (int)(((int64_t)a + head) % N);
+  const RowRef<const InT, N> r(row, head, p.V);
+  const int step = kThreads * CL;
+  // the token's entry is left out of the sums: 1 - pi(a) keeps its relative accuracy
+  const int own = (int)(((uint32_t)a + head) / N) - (rank * kThreads + tid);       // vectors from this thread's first to the token's
+  const int own_k = own >= 0 && own % step == 0 ? own / step : -1;
   float m = kLowest, s = 0.f;
-  const int64_t step = (int64_t)kThreads * CL;
-  for (int64_t v0 = (int64_t)rank * kThreads + tid; v0 < nvec; v0 += kUnroll * step) {
+  for (int v0 = rank * kThreads + tid, k0 = 0; v0 < r.nvec; v0 += kUnroll * step, k0 += kUnroll) {
     uint4 raw[kUnroll];
     RawMax<InT> mx;
+    load_vecs<kUnroll>(raw, r, v0, step, r.nvec);
+    if (own_k >= k0 && own_k < k0 + kUnroll) {
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) {
-      const int64_t v = v0 + k * step;
-      constexpr uint32_t inf = RawOf<InT>::kNegInf;
-      raw[k] = v < nvec ? load_vec<InT>(r, v * N - head, p.V) : make_uint4(inf, inf, inf, inf);
+      for (int k = 0; k < kUnroll; ++k)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (k0 + k == own_k && i == (int)(((uint32_t)a + head) % N)) set_raw(raw[k], i, from_f32<InT>(-INFINITY));
     }
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) {
-      if (v0 + k * step == av) {                           // left out of the sums: 1 - pi(a) keeps its relative accuracy
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-          if (i == ai) set_raw(raw[k], i, from_f32<InT>(-INFINITY));
-      }
       raw[k] = clamp_raw<InT>(raw[k]);
       mx.add(raw[k]);
     }
@@ -171,12 +168,12 @@ __global__ void __launch_bounds__(kThreads) token_grad_kernel(GradParams p) {
   constexpr int N = Vec<InT>::N;
   for (int64_t item = blockIdx.x; item < p.T * p.pieces; item += gridDim.x) {
     const int64_t at = p.backwards ? p.T * p.pieces - 1 - item : item;
-    const int64_t t = at / p.pieces, v0 = (at - t * p.pieces) * (kUnroll * kThreads) + threadIdx.x;
+    const int64_t t = at / p.pieces;
+    const int v0 = (int)(at - t * p.pieces) * (kUnroll * kThreads) + (int)threadIdx.x;
     const InT* row = reinterpret_cast<const InT*>(p.z) + t * p.ld;
     const uint32_t head = head_of(row);
-    const RowRef<const InT> r(row, head);
-    const RowRef<OutT> d(reinterpret_cast<OutT*>(p.dz) + t * p.ld_out, head);
-    const int64_t nvec = ((int64_t)head + p.V + N - 1) / N;
+    const RowRef<const InT, N> r(row, head, p.V);
+    const RowRef<OutT, N> d(reinterpret_cast<OutT*>(p.dz) + t * p.ld_out, head, p.V);
     const int a = row_token(p.ids, p.token_mask, t, p.V);
     const float c = p.coef[t];
     const double lse = p.lse[t];
@@ -186,22 +183,22 @@ __global__ void __launch_bounds__(kThreads) token_grad_kernel(GradParams p) {
       const float zero[N] = {};
 #pragma unroll
       for (int k = 0; k < kUnroll; ++k)
-        if (v0 + k * kThreads < nvec) store_vec<OutT, N>(d, (v0 + k * kThreads) * N - head, p.V, zero);
+        if (v0 + k * kThreads < r.nvec) store_vec<OutT, N>(d, v0 + k * kThreads, zero);
       continue;
     }
+    const int av = (int)(((uint32_t)a + head) / N);
+    const bool own = av >= v0 && av < v0 + kUnroll * kThreads && (av - v0) % kThreads == 0;
+    const float z_a = own ? to_f32<InT>(row[a]) : 0.f;     // (read before the gradient may overwrite it)
     uint4 raw[kUnroll];
-#pragma unroll
-    for (int k = 0; k < kUnroll; ++k)
-      if (v0 + k * kThreads < nvec) raw[k] = load_vec<InT>(r, (v0 + k * kThreads) * N - head, p.V);
+    load_vecs<kUnroll>(raw, r, v0, kThreads, r.nvec);
     // pi = exp(z - lse): z - (float)lse is exact for the entries that count, what (float)lse lacks goes into the factor
     const float near = (float)lse;
     const float f = (float)(-(double)c * (1.0 + ((double)near - lse)));
     const float2 nr = make_float2(-near, -near), l2 = make_float2(kLog2e, kLog2e), f2 = make_float2(f, f);
-    const int64_t a_img = (int64_t)a + head;
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) {
-      const int64_t v = v0 + k * kThreads;
-      if (v >= nvec) break;
+      const int v = v0 + k * kThreads;
+      if (v >= r.nvec) break;
       float2 z[N / 2];
       to_pairs<InT>(raw[k], z);
       float x[N];
@@ -212,14 +209,9 @@ __global__ void __launch_bounds__(kThreads) token_grad_kernel(GradParams p) {
         x[2 * i] = e.x;
         x[2 * i + 1] = e.y;
       }
-      if (a_img / N == v) {                                // c (1 - pi(a)), without the cancellation
-        const float* zf = reinterpret_cast<const float*>(z);
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-          if (i == (int)(a_img % N)) x[i] = (float)(-(double)c * expm1((double)zf[i] - lse));
-      }
-      store_vec<OutT, N>(d, v * N - head, p.V, x);
+      store_vec<OutT, N>(d, v, x);
     }
+    if (own) d.row[a] = from_f32<OutT>((float)(-(double)c * expm1((double)z_a - lse)));      // c (1 - pi(a)), without the cancellation
   }
 }
 

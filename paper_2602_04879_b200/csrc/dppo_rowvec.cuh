@@ -73,6 +73,24 @@ template <> __device__ __forceinline__ void to_pairs<float>(const uint4& v, floa
   z[0] = make_float2(__uint_as_float(v.x), __uint_as_float(v.y));
   z[1] = make_float2(__uint_as_float(v.z), __uint_as_float(v.w));
 }
+// the entries of a raw vector less m, as pairs of floats (bf16: one instruction an entry, which widens it as well)
+template <typename T> __device__ __forceinline__ void less_pairs(const uint4& v, float m, float2* d);
+__device__ __forceinline__ float2 less_bf16x2(uint32_t w, float nm) {
+  float2 d;
+  asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n add.f32.bf16 %0, l, %3;\n add.f32.bf16 %1, h, %3;\n}\n" : "=f"(d.x), "=f"(d.y) : "r"(w), "f"(nm));
+  return d;
+}
+template <> __device__ __forceinline__ void less_pairs<__nv_bfloat16>(const uint4& v, float m, float2* d) {
+  d[0] = less_bf16x2(v.x, -m);
+  d[1] = less_bf16x2(v.y, -m);
+  d[2] = less_bf16x2(v.z, -m);
+  d[3] = less_bf16x2(v.w, -m);
+}
+template <> __device__ __forceinline__ void less_pairs<float>(const uint4& v, float m, float2* d) {
+  const float2 nm = make_float2(-m, -m);
+  d[0] = __fadd2_rn(make_float2(__uint_as_float(v.x), __uint_as_float(v.y)), nm);
+  d[1] = __fadd2_rn(make_float2(__uint_as_float(v.z), __uint_as_float(v.w)), nm);
+}
 __device__ __forceinline__ float warp_max_nan(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xffffffffu, v, o));
@@ -103,44 +121,73 @@ __device__ __forceinline__ void set_raw(uint4& v, int i, __nv_bfloat16 x) {
 }
 __device__ __forceinline__ void set_raw(uint4& v, int i, float x) { set_word(v, i, __float_as_uint(x)); }
 
-// A row of elements T cut at the vectors of a row with `head` elements in front: `whole` says that those vectors are aligned in this
-// tensor too.
-template <typename T>
-struct RowRef {
-  T* row;
-  bool whole;
-  __device__ __forceinline__ RowRef(T* r, uint32_t head) : row(r), whole(((reinterpret_cast<uintptr_t>(r) - (uintptr_t)head * sizeof(T)) & 15u) == 0) {}
-};
-
 template <typename T>
 __device__ __forceinline__ uint32_t head_of(const T* row) { return (uint32_t)((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(T)); }
 
-// Vector v of the row (elements j0 .. j0 + N - 1, j0 = v N - head; entries outside [0, V) read as -inf).
-template <typename T>
-__device__ __forceinline__ uint4 load_vec(const RowRef<const T>& r, int64_t j0, int64_t V) {
-  constexpr int N = Vec<T>::N;
-  if (r.whole && j0 >= 0 && j0 + N <= V) return ldg128_stream(r.row + j0);
-  uint4 v = make_uint4(RawOf<T>::kNegInf, RawOf<T>::kNegInf, RawOf<T>::kNegInf, RawOf<T>::kNegInf);
+// A row of V elements T cut into vectors of N elements, the first of which starts `head` elements in front of the row.  Vectors lo .. hi - 1
+// lie inside the row and are aligned in this tensor: 16-byte accesses; the others of the nvec go element by element.
+template <typename T, int N>
+struct RowRef {
+  T* row;
+  int V, head, nvec, lo, hi;
+  __device__ __forceinline__ RowRef(T* r, uint32_t h, int64_t v) : row(r), V((int)v), head((int)h) {
+    nvec = (head + V + N - 1) / N;
+    const bool whole = ((reinterpret_cast<uintptr_t>(r) - (uintptr_t)h * sizeof(T)) & 15u) == 0;
+    lo = whole ? (head ? 1 : 0) : 0;
+    hi = whole ? (head + V) / N : 0;
+  }
+  __device__ __forceinline__ bool inside(int v) const { return v >= lo && v < hi; }
+  __device__ __forceinline__ T* at(int v) const { return row + ((int64_t)v * N - head); }
+};
+
+// raw = 16 bytes at p where `yes`, unchanged otherwise: loads of several vectors stay in flight together
+__device__ __forceinline__ void ldg128_if(uint4& raw, const void* p, bool yes) {
+  asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %5, 0;\n @q ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];\n}\n"
+               : "+r"(raw.x), "+r"(raw.y), "+r"(raw.z), "+r"(raw.w) : "l"(p), "r"((int)yes));
+}
+
+// Vectors v0, v0 + step, ... (NV of them) in front of `end`; entries outside the row, and vectors from `end` on, read as -inf.
+template <int NV, typename T, int N>
+__device__ __forceinline__ void load_vecs(uint4* raw, const RowRef<const T, N>& r, int v0, int step, int end) {
+  constexpr uint32_t inf = RawOf<T>::kNegInf;
+  bool edge = false;
 #pragma unroll
-  for (int i = 0; i < N; ++i)
-    if (j0 + i >= 0 && j0 + i < V) set_raw(v, i, r.row[j0 + i]);
-  return v;
+  for (int k = 0; k < NV; ++k) {
+    const int v = v0 + k * step;
+    raw[k] = make_uint4(inf, inf, inf, inf);
+    ldg128_if(raw[k], r.at(v), r.inside(v) && v < end);
+    edge |= v < end && !r.inside(v);
+  }
+  if (edge) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int v = v0 + k * step;
+      if (v < end && !r.inside(v)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int j = v * N - r.head + i;
+          if (j >= 0 && j < r.V) set_raw(raw[k], i, r.row[j]);
+        }
+      }
+    }
+  }
 }
 
 template <typename OutT, int N>
-__device__ __forceinline__ void store_vec(const RowRef<OutT>& r, int64_t j0, int64_t V, const float* x) {
-  if (r.whole && j0 >= 0 && j0 + N <= V) { Store<OutT, N>::run(r.row + j0, 0u, x); return; }
+__device__ __forceinline__ void store_vec(const RowRef<OutT, N>& r, int v, const float* x) {
+  if (r.inside(v)) { Store<OutT, N>::run(r.at(v), 0u, x); return; }
 #pragma unroll
-  for (int i = 0; i < N; ++i)
-    if (j0 + i >= 0 && j0 + i < V) r.row[j0 + i] = from_f32<OutT>(x[i]);
+  for (int i = 0; i < N; ++i) {
+    const int j = v * N - r.head + i;
+    if (j >= 0 && j < r.V) r.row[j] = from_f32<OutT>(x[i]);
+  }
 }
 
 // this CTA's share (part of parts) of a row of zeros
 template <typename OutT, int N>
-__device__ __forceinline__ void zero_row(const RowRef<OutT>& r, uint32_t head, int64_t V, int part, int parts, int threads) {
+__device__ __forceinline__ void zero_row(const RowRef<OutT, N>& r, int part, int parts, int threads) {
   const float zero[N] = {};
-  const int64_t nvec = ((int64_t)head + V + N - 1) / N;
-  for (int64_t v = (int64_t)part * threads + threadIdx.x; v < nvec; v += (int64_t)parts * threads) store_vec<OutT, N>(r, v * N - head, V, zero);
+  for (int v = part * threads + (int)threadIdx.x; v < r.nvec; v += parts * threads) store_vec<OutT, N>(r, v, zero);
 }
 
 }  // namespace dppo
