@@ -146,22 +146,25 @@ struct MatvecParams {
 };
 
 // ---- tensor cores ------------------------------------------------------------------------------------------------------
-// D[n, m] = sum over a group of (code[n, k] - 8) x[m, k] for 128 rows n and NT rows m at a time: the weights are the operand with the many
-// rows.  They come as they are stored by tensor copies (128 rows x 256 codes, 128-byte swizzle) into a ring; a thread per row turns its
+// D[n, m] = sum over a group of (code[n, k] - 8) x[m, k] for up to 128 rows n and NT rows m at a time: the weights are the operand with the many
+// rows.  They come as they are stored by tensor copies (rows x 256 codes, 128-byte swizzle) into a ring; a thread per row turns
 // 128 codes into bf16 pairs in registers and writes them to tensor memory, where tcgen05.mma takes its A operand from; x lies in
-// shared memory for the whole launch (or a segment of K at a time, where it does not fit).  The product of a group is read back, scaled
-// by the row's scale (a thread's own) and added up in fp32 registers while the next codes are converted.
+// shared memory for the whole launch.  The product of a group is read back, scaled by the row's scale (a thread's own) and added up in
+// fp32 registers.  One persistent CTA per SM:
 //   warp 0         tensor copies of the weights
-//   warp 1         allocates tensor memory, issues the MMAs
-//   WG x 4 warps   convert, scale and add up; warpgroup g takes the chunks g, g + WG, ... of 128 codes of a tile
-// At a tile's end the warpgroups exchange their sums through shared memory; each finishes and stores a part of the rows of x.
+//   warps 1, 2     allocate tensor memory (the first), issue the MMAs of every other chunk: a wait for a barrier costs 150 cycles even where nothing is to be
+//                  waited for, and with one warp the tensor cores stood still for two of them a chunk (820 cycles instead of 380)
+//   C x 4 warps    conversion, taking the chunks of 128 codes in turn
+//   E x 4 warps    products: scale, add up, store; each warpgroup NT / E rows of x
+// Where x does not fit, a pair of CTAs (a cluster) shares a tile, each half of K, and they exchange the sums of half of x's rows through
+// distributed shared memory; where that is not enough either, x is loaded again for each part of K.
 //
 // A word of 8 codes c0 .. c7 gives the pairs (c0, c4), (c1, c5), (c2, c6), (c3, c7): a mask and an or put a code into the low mantissa bits of
 // the bf16 number 128, and subtracting 136 leaves code - 8, exactly.  x is laid out in the order that this makes of k.
 namespace mv {
 
-constexpr int ROWS = 128, CHUNK = 128;     // rows of a tile; codes that a thread converts at a time
-constexpr int STAGE_BYTES = ROWS * 128;    // two chunks
+constexpr int LANES = 128, CHUNK = 128;    // rows of a tile at most; codes that a thread converts at a time
+constexpr int STAGE_BYTES = LANES * 128;   // two chunks
 constexpr int XSPAN = 64;                  // k of a swizzled block of x
 
 struct Params {
@@ -173,20 +176,23 @@ struct Params {
   void* y;
   int64_t ldy;
   int y_bf16, x_vec;                       // x_vec: 16-byte loads of x allowed
-  int stages, seg, nseg, groups;           // seg: codes of K that x lies in shared memory for (a multiple of 256), nseg of them
+  int rows, stages, seg, nseg, groups;     // rows of a tile; seg: codes of K that x lies in shared memory for (a multiple of 256), nseg of them to a CTA
+  int pairs;                               // pairs of chunks of a CTA
   int32_t* status;
   unsigned long long wait_ns;
   int inject;
 };
 
-template <int NT> struct Shape {
-  static constexpr int WG = NT == 16 ? 4 : 2;              // what the registers hold: 32 for half of the converted codes, NT for the sums, 16 for a part of a product
-  static constexpr int THREADS = 64 + WG * 128;
-};
-template <int NT, int G> struct Tmem {
-  static constexpr int A = CHUNK / 2, D = CHUNK / G * NT;  // columns of a warpgroup's operand and products
-  static constexpr int COLS = Shape<NT>::WG * (A + D) <= 256 ? 256 : 512;
-  static_assert(Shape<NT>::WG * (A + D) <= 512, "tensor memory");
+template <int NT, int G> struct Shape {
+  static constexpr int E = NT == 64 ? 2 : 1, EN = NT / E;              // warpgroups for the products, rows of x of each
+  static constexpr int A = CHUNK / 2, D = CHUNK / G * NT;              // columns of tensor memory of a chunk: operand, products
+  static constexpr int BUFS = 512 / (A + D) >= 6 ? 6 : 512 / (A + D) / 2 * 2;     // chunks under way
+  // Warpgroups that convert.  Barrier phases are known by their parity, so whoever waits for a buffer's last use has to know that the use before
+  // that is over.  An issuing warp has made it itself, BUFS being even.  A converting warpgroup has seen the end of the MMAs of chunk
+  // i - CONV - BUFS before its chunk i; CONV being even, that chunk and i - 2 BUFS are one issuing warp's, which takes them in order: CONV <= BUFS.
+  static constexpr int CONV = NT == 64 || BUFS < 4 ? 2 : 4;
+  static constexpr int THREADS = 96 + (CONV + E) * 128;
+  static_assert(BUFS >= 2 && BUFS % 2 == 0 && CONV % 2 == 0 && CONV <= BUFS, "barrier phases");
 };
 
 __device__ __forceinline__ uint32_t elect_one() {
@@ -214,7 +220,6 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
                  "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                : "r"(taddr));
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 // the 8 codes of a word as four bf16 pairs (c0, c4), (c1, c5), (c2, c6), (c3, c7), less 8
 __device__ __forceinline__ void convert(uint32_t w, uint32_t* r) {
@@ -228,67 +233,89 @@ __device__ __forceinline__ void convert(uint32_t w, uint32_t* r) {
 
 // x rows m0 .. m0 + NT - 1, codes k0 .. k0 + seg - 1 of K, into shared memory: blocks of 64 codes, NT rows of 128 bytes each, 128-byte
 // swizzle, and within 8 codes the order that convert() makes of them.  Rows and codes that there are not are zero.
-template <int NT>
-__device__ __forceinline__ void load_x(const Params& p, unsigned char* xs, int m0, int k0, int tid, int threads) {
-  const int octets = p.seg / 8;
-  for (int i = tid; i < NT * octets; i += threads) {
-    const int m = i / octets, o = i - m * octets, k = k0 + 8 * o;
-    uint32_t h[8] = {};                                    // the eight entries
-    if (m0 + m < p.M && k < p.K) {
-      const __nv_bfloat16* src = p.x + (int64_t)(m0 + m) * p.ldx + k;
-      if (p.x_vec && k + 8 <= p.K) {
-        const uint4 v = *reinterpret_cast<const uint4*>(src);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+template <int NT, int T>
+__device__ __forceinline__ void load_x(const Params& p, unsigned char* xs, int m0, int k0, int tid) {
+  constexpr int AT_ONCE = 4;               // loads in flight
+  const int octets = p.seg / 8, all = NT * octets;
+  for (int i0 = tid; i0 < all; i0 += AT_ONCE * T) {
+    uint4 v[AT_ONCE];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) h[j] = (w[j >> 1] >> (16 * (j & 1))) & 0xffffu;
-      } else {
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const int i = i0 + u * T, m = i / octets, o = i - m * octets, k = k0 + 8 * o;
+      v[u] = make_uint4(0u, 0u, 0u, 0u);
+      if (i < all && m0 + m < p.M && k < p.K) {
+        const __nv_bfloat16* src = p.x + (int64_t)(m0 + m) * p.ldx + k;
+        if (p.x_vec && k + 8 <= p.K) {
+          v[u] = *reinterpret_cast<const uint4*>(src);
+        } else {
+          uint32_t h[8] = {};
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (k + j < p.K) h[j] = __bfloat16_as_ushort(src[j]);
+          for (int j = 0; j < 8; ++j)
+            if (k + j < p.K) h[j] = __bfloat16_as_ushort(src[j]);
+          v[u] = make_uint4(h[0] | (h[1] << 16), h[2] | (h[3] << 16), h[4] | (h[5] << 16), h[6] | (h[7] << 16));
+        }
       }
     }
-    const int at = (o / 8) * (NT * 128) + m * 128 + ((16 * (o % 8)) ^ ((m & 7) << 4));
-    *reinterpret_cast<uint4*>(xs + at) = make_uint4(h[0] | (h[4] << 16), h[1] | (h[5] << 16), h[2] | (h[6] << 16), h[3] | (h[7] << 16));
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const int i = i0 + u * T, m = i / octets, o = i - m * octets;
+      if (i >= all) break;
+      const int at = (o / 8) * (NT * 128) + m * 128 + ((16 * (o % 8)) ^ ((m & 7) << 4));
+      // (0, 4), (1, 5), (2, 6), (3, 7)
+      *reinterpret_cast<uint4*>(xs + at) = make_uint4(__byte_perm(v[u].x, v[u].z, 0x5410), __byte_perm(v[u].x, v[u].z, 0x7632), __byte_perm(v[u].y, v[u].w, 0x5410),
+                                                      __byte_perm(v[u].y, v[u].w, 0x7632));
+    }
   }
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 
-template <int NT, int G>
-__global__ void __launch_bounds__(Shape<NT>::THREADS, 1) matvec_int4_kernel(const __grid_constant__ CUtensorMap map_q, const Params p) {
-  constexpr int WG = Shape<NT>::WG, NG = CHUNK / G, OWN = NT / WG;      // OWN: rows of x that a warpgroup finishes
-  using TM = Tmem<NT, G>;
+struct Bars {
+  unsigned long long full[12], empty[12];            // stages of weights
+  unsigned long long a_full[6], done[6], d_free[6];  // chunk: operand written; MMAs done (operand free, products there); products read
+  unsigned long long x_free, x_full;                 // x replaced
+  unsigned long long sum_full, sum_free;             // pairs of CTAs: the other's sums are here; read by the other
+  uint32_t tmem;
+  int abort_flag;
+};
+
+template <int NT, int G, int CL>
+__global__ void __launch_bounds__(Shape<NT, G>::THREADS, 1) matvec_int4_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ Params p) {
+  using S = Shape<NT, G>;
+  constexpr int NG = CHUNK / G, BUFS = S::BUFS, CONV = S::CONV, COLS = S::A + S::D, EN = S::EN, OWN = EN / CL;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   unsigned char* xs = smem + p.stages * STAGE_BYTES;
-  float* sums = reinterpret_cast<float*>(xs + (size_t)p.seg * NT * 2);  // [WG - 1][NT][ROWS]
-  unsigned long long* bars = reinterpret_cast<unsigned long long*>(sums + (WG - 1) * NT * ROWS);
-  const uint32_t full0 = smem_u32(bars), empty0 = smem_u32(bars + 16), a0 = smem_u32(bars + 32), d0 = smem_u32(bars + 36);
-  const uint32_t sum_full = smem_u32(bars + 40), sum_free = smem_u32(bars + 41), x_free = smem_u32(bars + 42), x_full = smem_u32(bars + 43);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 44);
-  const WaitCtl wc{reinterpret_cast<volatile int*>(tmem_slot + 1), p.wait_ns};
+  float* sums = reinterpret_cast<float*>(xs + (size_t)p.seg * NT * 2);  // pairs: [E][OWN][LANES], from the other CTA
+  Bars* bars = reinterpret_cast<Bars*>(sums + (CL > 1 ? NT / CL * LANES : 0));
+  const uint32_t full0 = smem_u32(bars->full), empty0 = smem_u32(bars->empty), a0 = smem_u32(bars->a_full), done0 = smem_u32(bars->done), free0 = smem_u32(bars->d_free);
+  const uint32_t x_free = smem_u32(&bars->x_free), x_full = smem_u32(&bars->x_full), sum_full = smem_u32(&bars->sum_full), sum_free = smem_u32(&bars->sum_free);
+  const WaitCtl wc{&bars->abort_flag, p.wait_ns};
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = CL > 1 ? (int)cluster_ctarank() : 0;
   if (tid == 0) {
-    for (int i = 0; i < p.stages; ++i) { mbar_init(full0 + 8 * i, 1); mbar_init(empty0 + 8 * i, 8); }
-    for (int i = 0; i < WG; ++i) { mbar_init(a0 + 8 * i, 4); mbar_init(d0 + 8 * i, 1); }
-    mbar_init(sum_full, WG * 4);
-    mbar_init(sum_free, WG * 4);
-    mbar_init(x_free, WG * 4);
-    mbar_init(x_full, WG * 4);
-    *wc.flag = 0;
+    for (int i = 0; i < 12; ++i) { mbar_init(full0 + 8 * i, 1); mbar_init(empty0 + 8 * i, 8); }
+    for (int i = 0; i < 6; ++i) { mbar_init(a0 + 8 * i, 4); mbar_init(done0 + 8 * i, 1); mbar_init(free0 + 8 * i, 4 * S::E); }
+    mbar_init(x_free, CONV * 4);
+    mbar_init(x_full, CONV * 4);
+    mbar_init(sum_full, 4 * S::E);
+    mbar_init(sum_free, 4 * S::E);
+    bars->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "n"(TM::COLS) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem)), "n"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  if (p.nseg == 1 && p.M <= NT) load_x<NT>(p, xs, 0, 0, tid, Shape<NT>::THREADS);
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  const uint32_t tmem = *tmem_slot;
-  // A tile is 128 rows of the weights times NT rows of x; the blocks of x are the slow index.  Its chunks are counted in pairs (a stage).
-  const int tiles_n = (p.N + ROWS - 1) / ROWS, tiles = tiles_n * ((p.M + NT - 1) / NT), pairs = (p.K + 255) / 256, seg_pairs = p.seg / 256;
+  const uint32_t tmem = bars->tmem;
+  if (CL > 1) cluster_sync_all();          // the other's barriers exist before anything is sent to them
+  // A tile is `rows` rows of the weights times NT rows of x; the blocks of x are the slow index.  A CTA's chunks are counted in pairs (a stage).
+  const int tiles_n = (p.N + p.rows - 1) / p.rows, tiles = tiles_n * ((p.M + NT - 1) / NT), seg_pairs = p.seg / 256;
+  const int pair0 = rank * p.pairs, pairs = max(0, min(p.pairs, (p.K + 255) / 256 - pair0));      // this CTA's part of K
+  const int first = blockIdx.x / CL, grid = gridDim.x / CL;
 
   if (warp == 0) {
     // ------------------------------------------------------------------ weights
@@ -296,182 +323,243 @@ __global__ void __launch_bounds__(Shape<NT>::THREADS, 1) matvec_int4_kernel(cons
       int s = 0;
       uint32_t ph = 0;
       bool ok = true;
-      for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
-        const int n0 = (tile % tiles_n) * ROWS;
+      for (int tile = first; tile < tiles && ok; tile += grid) {
+        const int n0 = (tile % tiles_n) * p.rows;
         for (int c = 0; c < pairs; ++c) {
           if (!mbar_wait_warp(empty0 + 8 * s, ph ^ 1u, wc)) { ok = false; break; }
           if (lane == 0) {
-            mbar_arrive_expect_tx(full0 + 8 * s, STAGE_BYTES);
-            gemm::tma_load_2d(smem_u32(smem) + s * STAGE_BYTES, &map_q, c * 128, n0, full0 + 8 * s);
+            mbar_arrive_expect_tx(full0 + 8 * s, p.rows * 128);
+            gemm::tma_load_2d(smem_u32(smem) + s * STAGE_BYTES, &map_q, (pair0 + c) * 128, n0, full0 + 8 * s);
           }
           if (++s == p.stages) { s = 0; ph ^= 1u; }
         }
       }
     }
-  } else if (warp == 1) {
+  } else if (warp < 3) {
     // ------------------------------------------------------------------ MMAs
-    constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(NT >> 3) << 17) | ((uint32_t)(ROWS >> 4) << 24);
+    constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(NT >> 3) << 17) | ((uint32_t)(LANES >> 4) << 24);
     const uint64_t xdesc = gemm::make_desc_k_sw128(smem_u32(xs));
-    uint32_t use = 0;                                      // chunks of each warpgroup so far (its phase)
-    int g = 0;
+    int b = 0, odd = 0;
+    uint32_t ph = 0;
     bool ok = true;
-    for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
-      for (int c = 0; c < 2 * pairs; ++c) {
-        ok = mbar_wait_warp(a0 + 8 * g, use & 1u, wc);
-        if (!ok) break;
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const int k = (c % (2 * seg_pairs)) * CHUNK;       // within the segment
-        const uint32_t ta = tmem + g * (TM::A + TM::D), td = ta + TM::A;
-        if (elect_one()) {
+    for (int tile = first; tile < tiles && ok; tile += grid) {
+      int k = 0;                                           // within what shared memory holds of x
+      for (int c = 0; c < 2 * pairs; ++c, k = k + CHUNK == p.seg ? 0 : k + CHUNK) {
+        if (odd == warp - 1) {
+          // (the operand first: once it is there, the buffer's products before are the last ones)
+          ok = mbar_wait_warp(a0 + 8 * b, ph, wc) && mbar_wait_warp(free0 + 8 * b, ph ^ 1u, wc);
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t ta = tmem + b * COLS, td = ta + S::A;
+          if (elect_one()) {
 #pragma unroll
-          for (int i = 0; i < CHUNK / 16; ++i) {           // 16 codes an MMA
-            const int at = (k + 16 * i) / XSPAN * (NT * 128) + (16 * i) % XSPAN * 2;
-            mma_ts(td + (16 * i) / G * NT, ta + 8 * i, xdesc + (uint64_t)(at >> 4), idesc, (16 * i) % G != 0);
+            for (int i = 0; i < CHUNK / 16; ++i) {         // 16 codes an MMA
+              const int at = (k + 16 * i) / XSPAN * (NT * 128) + (16 * i) % XSPAN * 2;
+              mma_ts(td + (16 * i) / G * NT, ta + 8 * i, xdesc + (uint64_t)(at >> 4), idesc, (16 * i) % G != 0);
+            }
+            gemm::mma_commit(done0 + 8 * b);
           }
-          gemm::mma_commit(d0 + 8 * g);
+          __syncwarp();
         }
-        __syncwarp();
-        if (++g == WG) { g = 0; ++use; }
+        odd ^= 1;
+        if (++b == BUFS) { b = 0; ph ^= 1u; }
       }
     }
-  } else {
-    // ------------------------------------------------------------------ conversion and sums
-    const int g = (warp - 2) >> 2, q = warp & 3, r = q * 32 + lane;     // warpgroup; a warp's lanes of tensor memory are given by its number
-    const uint32_t ta = tmem + ((uint32_t)(q * 32) << 16) + g * (TM::A + TM::D), td = ta + TM::A;
-    uint32_t n_d = 0, n_tile = 0, n_x = 0;                 // products awaited, tiles finished, segments of x loaded
-    int s0 = 0;                                            // stage of the tile's first pair
-    uint32_t ph0 = 0;
-    int turn = 0;                                          // warpgroup of the tile's first chunk
-    int x_now = p.nseg == 1 && p.M <= NT ? 0 : -1;         // which part of x (block of rows, segment) shared memory holds
+  } else if (warp < 3 + 4 * CONV) {
+    // ------------------------------------------------------------------ conversion
+    const int g = (warp - 3) >> 2, q = warp & 3, r = q * 32 + lane;     // (a warp's lanes of tensor memory are given by its number)
+    const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16);
+    const int mine = first < tiles ? (tiles - first + grid - 1) / grid : 0;      // tiles of this CTA
+    const bool one = p.nseg == 1 && p.M <= NT;             // one part of x for everything
+    const int parts = one ? (mine > 0 && pairs > 0 ? 1 : 0) : mine * p.nseg;
+    int x_now = -1;                        // which part of x (block of rows, part of K) shared memory holds
+    uint32_t n_x = 0;
+    // this warpgroup's next chunk of all the CTA's: its number, its place in the ring (in chunks) and its buffer
+    int i = g, at = g, b = g;
+    uint32_t ph = 0, bph = 0;
+    if (b >= BUFS) { b -= BUFS; bph ^= 1u; }
     bool ok = true;
-    for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
-      const int n = (tile % tiles_n) * ROWS + r, m0 = (tile / tiles_n) * NT;
-      const __nv_bfloat16* srow = p.scale + (int64_t)(n < p.N ? n : 0) * p.lds;
-      float acc[NT];
-#pragma unroll
-      for (int j = 0; j < NT; ++j) acc[j] = 0.f;
-      float sc[NG] = {};                                   // scales of the product under way
-      bool under_way = false;
-      auto take_product = [&]() {
-        if (!under_way) return true;
-        if (!mbar_wait_warp(d0 + 8 * g, n_d & 1u, wc)) return false;
-        ++n_d;
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-#pragma unroll
-        for (int h = 0; h < NG; ++h)
-#pragma unroll
-          for (int j0 = 0; j0 < NT; j0 += 16) {
-            uint32_t v[16];
-            tmem_ld16(td + h * NT + j0, v);
-#pragma unroll
-            for (int j = 0; j < 16; j += 2) {
-              const float2 a = __ffma2_rn(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), make_float2(sc[h], sc[h]), make_float2(acc[j0 + j], acc[j0 + j + 1]));
-              acc[j0 + j] = a.x;
-              acc[j0 + j + 1] = a.y;
-            }
-          }
-        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-        under_way = false;
-        return true;
-      };
-      for (int seg = 0; seg < p.nseg && ok; ++seg) {
-        const int x_want = (tile / tiles_n) * p.nseg + seg;
+    for (int part = 0; part < parts && ok; ++part) {
+      int end = mine * 2 * pairs;
+      if (!one || x_now < 0) {
+        const int t = one ? 0 : part / p.nseg, seg = one ? 0 : part - t * p.nseg, start = t * 2 * pairs + seg * 2 * seg_pairs;
+        if (!one) end = t * 2 * pairs + min(2 * pairs, (seg + 1) * 2 * seg_pairs);
+        if (start >= end) continue;        // (a CTA's last part of K may be empty)
+        const int block = (first + t * grid) / tiles_n, x_want = block * p.nseg + seg;
         if (x_now != x_want) {
-          // once every warpgroup has seen its last product with the part before
-          ok = take_product();
-          if (!ok) break;
+          // once the MMAs with the part before are done: those of the chunk before this part's first, whoever converts it, are the last
+          if (start > 0 && !mbar_wait_warp(done0 + 8 * ((start - 1) % BUFS), (uint32_t)((start - 1) / BUFS) & 1u, wc)) { ok = false; break; }
           __syncwarp();
           if (lane == 0) mbar_arrive(x_free);
-          ok = mbar_wait_warp(x_free, n_x & 1u, wc);
-          if (!ok) break;
-          load_x<NT>(p, xs, m0, seg * p.seg, tid - 64, WG * 128);
+          if (!mbar_wait_warp(x_free, n_x & 1u, wc)) { ok = false; break; }
+          load_x<NT, CONV * 128>(p, xs, block * NT, (pair0 + seg * seg_pairs) * 256, tid - 96);
           __syncwarp();
           if (lane == 0) mbar_arrive(x_full);
-          ok = mbar_wait_warp(x_full, n_x & 1u, wc);
-          if (!ok) break;
+          if (!mbar_wait_warp(x_full, n_x & 1u, wc)) { ok = false; break; }
           ++n_x;
           x_now = x_want;
         }
-        const int c_end = min(2 * pairs, 2 * seg_pairs * (seg + 1));
-        for (int c = 2 * seg_pairs * seg + ((g - turn - 2 * seg_pairs * seg % WG + 2 * WG) % WG); c < c_end; c += WG) {
-          const int pair = s0 + c / 2, s = pair % p.stages;
-          const uint32_t ph = (ph0 + (uint32_t)(pair / p.stages)) & 1u;
-          float nsc[NG];
-#pragma unroll
-          for (int h = 0; h < NG; ++h) {
-            const int gi = c * NG + h;
-            nsc[h] = (n < p.N && gi < p.groups) ? __bfloat162float(__ldg(srow + gi)) : 0.f;
-          }
-          ok = mbar_wait_warp(full0 + 8 * s, ph, wc);
-          if (!ok) break;
-          const uint32_t src = smem_u32(smem) + s * STAGE_BYTES + r * 128;
-          uint4 w[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = lds128(src + ((((c & 1) * 4 + i) ^ (r & 7)) << 4));
-          __syncwarp();
-          if (lane == 0) mbar_arrive(empty0 + 8 * s);
-          uint32_t v[32];
-          convert(w[0].x, v);
-          convert(w[0].y, v + 4);
-          convert(w[0].z, v + 8);
-          convert(w[0].w, v + 12);
-          convert(w[1].x, v + 16);
-          convert(w[1].y, v + 20);
-          convert(w[1].z, v + 24);
-          convert(w[1].w, v + 28);
-          ok = take_product();                             // of the chunk before: its operand may be overwritten now
-          if (!ok) break;
-          tmem_st32(ta, v);
-          convert(w[2].x, v);
-          convert(w[2].y, v + 4);
-          convert(w[2].z, v + 8);
-          convert(w[2].w, v + 12);
-          convert(w[3].x, v + 16);
-          convert(w[3].y, v + 20);
-          convert(w[3].z, v + 24);
-          convert(w[3].w, v + 28);
-          tmem_st32(ta + 32, v);
-          asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) mbar_arrive(a0 + 8 * g);
-#pragma unroll
-          for (int h = 0; h < NG; ++h) sc[h] = nsc[h];
-          under_way = true;
-        }
       }
-      if (!ok || !take_product()) break;
-      s0 += pairs;
-      ph0 += (uint32_t)(s0 / p.stages);
-      s0 %= p.stages;
-      turn = (turn + 2 * pairs) % WG;
-      // the warpgroups' sums: each leaves those of the others' rows of x, and finishes its own
-      if (n_tile > 0 && !mbar_wait_warp(sum_free, (n_tile - 1u) & 1u, wc)) break;
-      const int live = min(NT, p.M - m0);
+      for (; i < end; i += CONV) {
+        const int s = at >> 1;
+        if (!mbar_wait_warp(full0 + 8 * s, ph, wc)) { ok = false; break; }
+        const uint32_t src = smem_u32(smem) + s * STAGE_BYTES + r * 128;
+        uint4 w[4];
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const int owner = j / OWN;
-        if (owner != g && j < live) sums[((g < owner ? g : g - 1) * NT + j) * ROWS + r] = acc[j];
+        for (int j = 0; j < 4; ++j) w[j] = lds128(src + ((((at & 1) * 4 + j) ^ (r & 7)) << 4));
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty0 + 8 * s);
+        uint32_t v[32];
+        auto half = [&](const uint4& x, const uint4& y) {
+          convert(x.x, v); convert(x.y, v + 4); convert(x.z, v + 8); convert(x.w, v + 12);
+          convert(y.x, v + 16); convert(y.y, v + 20); convert(y.z, v + 24); convert(y.w, v + 28);
+        };
+        half(w[0], w[1]);
+        if (!mbar_wait_warp(done0 + 8 * b, bph ^ 1u, wc)) { ok = false; break; }       // the buffer's operand before has been used
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        tmem_st32(lane_base + b * COLS, v);
+        half(w[2], w[3]);
+        tmem_st32(lane_base + b * COLS + 32, v);
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(a0 + 8 * b);
+        at += CONV;
+        if (at >= 2 * p.stages) { at -= 2 * p.stages; ph ^= 1u; }
+        b += CONV;
+        if (b >= BUFS) { b -= BUFS; bph ^= 1u; }
+      }
+    }
+  } else {
+    // ------------------------------------------------------------------ products
+    const int e = (warp - 3 - 4 * CONV) >> 2, q = warp & 3, r = q * 32 + lane;
+    const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16) + S::A + e * EN;
+    int b = 0;
+    uint32_t ph = 0, n_tile = 0;
+    bool ok = true;
+    int tn = first % tiles_n, block = first / tiles_n;     // of the tile under way
+    const int ysize = p.y_bf16 ? 2 : 4;
+    const int64_t ystep = p.ldy * ysize;
+    auto y_at = [&](int n, int m) { return reinterpret_cast<char*>(p.y) + m * ystep + (int64_t)n * ysize; };
+    auto put = [&](char* at, float v) {
+      if (p.y_bf16) *reinterpret_cast<__nv_bfloat16*>(at) = __float2bfloat16_rn(v);
+      else *reinterpret_cast<float*>(at) = v;
+    };
+    // The row's scales, fetched two pairs of chunks ahead (their latency is that of L2 or of memory), the next tile's first along with this
+    // one's last.
+    const int glim = min(max(p.groups - 2 * pair0 * NG, 0), 2 * pairs * NG);      // this CTA's groups
+    auto scales_of = [&](int tile_n, bool there) {
+      const int n = tile_n * p.rows + r;
+      return there && r < p.rows && n < p.N ? reinterpret_cast<const unsigned short*>(p.scale) + (int64_t)n * p.lds + 2 * pair0 * NG : nullptr;
+    };
+    unsigned short sc[2][2 * NG];
+    auto fetch = [&](const unsigned short* row, int c, unsigned short* to) {
+#pragma unroll
+      for (int h = 0; h < 2 * NG; ++h) {
+        to[h] = 0;
+        if (row && c * NG + h < glim) to[h] = __ldg(row + c * NG + h);
+      }
+    };
+    const unsigned short* srow = scales_of(tn, first < tiles);
+    fetch(srow, 0, sc[0]);
+    fetch(srow, 2, sc[1]);
+    // pairs of CTAs: this CTA's rows of x of the tile before wait for the other's sums
+    float keep[CL > 1 ? OWN : 1];
+    char* keep_at = nullptr;
+    int keep_rows = -1;
+    auto complete = [&]() {
+      if (CL == 1 || keep_rows < 0) return true;
+      if (!__all_sync(0xffffffffu, mbar_wait_cluster(sum_full, (n_tile - 1u) & 1u, wc))) return false;
+      const float* theirs = sums + e * OWN * LANES + r;
+      char* at = keep_at;
+#pragma unroll
+      for (int j = 0; j < (CL > 1 ? OWN : 0); ++j) {
+        if (j >= keep_rows) break;
+        const float o = theirs[j * LANES];
+        if (keep_at) put(at, rank == 0 ? keep[j] + o : o + keep[j]);
+        at += ystep;
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(sum_full);
-      if (!mbar_wait_warp(sum_full, n_tile & 1u, wc)) break;
+      if (lane == 0) bar_arrive_cluster(map_to_cta(sum_free, (uint32_t)(rank ^ 1)));
+      keep_rows = -1;
+      return true;
+    };
+    for (int tile = first; tile < tiles && ok; tile += grid) {
+      const int n = tn * p.rows + r, m0 = block * NT + e * EN;
+      const bool live = srow != nullptr;
+      tn += grid;
+      while (tn >= tiles_n) { tn -= tiles_n; ++block; }
+      const unsigned short* srow_next = scales_of(tn, tile + grid < tiles);
+      float2 acc[EN / 2];
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        if (j / OWN == g && j < live) {
-          float v = 0.f;                                   // in the order of the warpgroups, whoever adds
+      for (int j = 0; j < EN / 2; ++j) acc[j] = make_float2(0.f, 0.f);
+      for (int c0 = 0; c0 < 2 * pairs && ok; c0 += 4) {
 #pragma unroll
-          for (int o = 0; o < WG; ++o) v += o == j / OWN ? acc[j] : sums[((o < j / OWN ? o : o - 1) * NT + j) * ROWS + r];
-          if (n < p.N) {
-            if (p.y_bf16) reinterpret_cast<__nv_bfloat16*>(p.y)[(int64_t)(m0 + j) * p.ldy + n] = __float2bfloat16_rn(v);
-            else reinterpret_cast<float*>(p.y)[(int64_t)(m0 + j) * p.ldy + n] = v;
+        for (int u = 0; u < 2; ++u) {
+          const int c = c0 + 2 * u;
+          if (c < 2 * pairs && ok) {                       // two chunks: buffers b and b + 1
+            ok = mbar_wait_warp(done0 + 8 * b, ph, wc) && mbar_wait_warp(done0 + 8 * b + 8, ph, wc);
+            if (ok) {
+              asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+              for (int h = 0; h < NG; ++h) {
+                const float s0 = __uint_as_float((uint32_t)sc[u][h] << 16), s1 = __uint_as_float((uint32_t)sc[u][NG + h] << 16);
+#pragma unroll
+                for (int j0 = 0; j0 < EN; j0 += 16) {
+                  uint32_t v[32];
+                  tmem_ld16(lane_base + b * COLS + h * NT + j0, v);
+                  tmem_ld16(lane_base + (b + 1) * COLS + h * NT + j0, v + 16);
+                  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                  for (int j = 0; j < 8; ++j) {
+                    acc[j0 / 2 + j] = __ffma2_rn(make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), make_float2(s0, s0), acc[j0 / 2 + j]);
+                    acc[j0 / 2 + j] = __ffma2_rn(make_float2(__uint_as_float(v[16 + 2 * j]), __uint_as_float(v[17 + 2 * j])), make_float2(s1, s1), acc[j0 / 2 + j]);
+                  }
+                }
+              }
+              asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+              __syncwarp();
+              if (lane == 0) { mbar_arrive(free0 + 8 * b); mbar_arrive(free0 + 8 * b + 8); }
+              if (c + 4 < 2 * pairs) fetch(srow, c + 4, sc[u]); else fetch(srow_next, 2 * u, sc[u]);
+              b += 2;
+              if (b == BUFS) { b = 0; ph ^= 1u; }
+            }
           }
         }
+        if (ok && c0 == 0) ok = complete();
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(sum_free);
+      if (!ok || !complete()) { ok = false; break; }
+      if (CL == 1) {
+        if (live) {
+          char* at = y_at(n, m0);
+          const int rows = p.M - m0;
+#pragma unroll
+          for (int j = 0; j < EN; ++j) {
+            if (j >= rows) break;
+            put(at, (j & 1) ? acc[j / 2].y : acc[j / 2].x);
+            at += ystep;
+          }
+        }
+      } else {
+        // the other's rows of x go over there, once it has read what went before
+        if (n_tile > 0 && !__all_sync(0xffffffffu, mbar_wait_cluster(sum_free, (n_tile - 1u) & 1u, wc))) { ok = false; break; }
+        const uint32_t dst = map_to_cta(smem_u32(sums + e * OWN * LANES + r), (uint32_t)(rank ^ 1));
+        const int rows = min(p.M - m0 - (rank ^ 1) * OWN, OWN);
+#pragma unroll
+        for (int j = 0; j < OWN; ++j) {
+          const float lo = (j & 1) ? acc[j / 2].y : acc[j / 2].x, hi = (j & 1) ? acc[(OWN + j) / 2].y : acc[(OWN + j) / 2].x;
+          keep[CL > 1 ? j : 0] = rank == 0 ? lo : hi;
+          if (j < rows) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(dst + (uint32_t)(j * LANES * 4)), "f"(rank == 0 ? hi : lo) : "memory");
+        }
+        __syncwarp();
+        if (lane == 0) bar_arrive_cluster(map_to_cta(sum_full, (uint32_t)(rank ^ 1)));
+        keep_rows = max(0, min(p.M - m0 - rank * OWN, OWN));
+        keep_at = live ? y_at(n, m0 + rank * OWN) : nullptr;
+      }
+      srow = srow_next;
       ++n_tile;
     }
+    if (ok) complete();
   }
   __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -482,8 +570,9 @@ __global__ void __launch_bounds__(Shape<NT>::THREADS, 1) matvec_int4_kernel(cons
   }
   if (warp == 1) {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(TM::COLS) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512) : "memory");
   }
+  if (CL > 1) cluster_sync_all();          // the other may still be sending to this CTA's shared memory
 }
 
 using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -500,30 +589,52 @@ EncodeFn get_encode() {
   return fn;
 }
 
-template <int NT, int G>
-cudaError_t launch(Params p, const unsigned char* q, int64_t ldq, int sms, int smem_most, cudaStream_t st) {
+template <int NT, int G, int CL>
+cudaError_t launch_cl(Params p, const unsigned char* q, int64_t ldq, int sms, int smem_most, cudaStream_t st) {
+  using S = Shape<NT, G>;
+  constexpr int FIXED = (CL > 1 ? NT / CL * LANES * 4 : 0) + (int)sizeof(Bars) + 1024;
+  const int room = smem_most - FIXED, total = (p.K + 255) / 256;
+  p.pairs = (total + CL - 1) / CL;
+  // x for all of this CTA's K where at least four stages are left besides it, else as much as leaves that many
+  int most = (room - 4 * STAGE_BYTES) / (NT * 2) / 256;
+  p.nseg = (p.pairs + most - 1) / most;
+  p.seg = (p.pairs + p.nseg - 1) / p.nseg * 256;
+  p.stages = (room - p.seg * NT * 2) / STAGE_BYTES;
+  if (p.stages > 12) p.stages = 12;
+  // rows of a tile: rounds of tiles over the CTAs that are as full as they can be
+  const int64_t ctas = sms / CL, rounds = (p.N + ctas * LANES - 1) / (ctas * LANES);
+  p.rows = (int)((p.N + ctas * rounds - 1) / (ctas * rounds));
   CUtensorMap map;
   const cuuint64_t dims[2] = {(cuuint64_t)((p.K + 1) / 2), (cuuint64_t)p.N}, strides[1] = {(cuuint64_t)ldq};
-  const cuuint32_t box[2] = {128u, (cuuint32_t)ROWS}, ones[2] = {1u, 1u};
+  const cuuint32_t box[2] = {128u, (cuuint32_t)p.rows}, ones[2] = {1u, 1u};
   EncodeFn enc = get_encode();
   if (!enc || enc(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<unsigned char*>(q), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return cudaErrorInvalidValue;
-  constexpr int WG = Shape<NT>::WG, FIXED = (WG - 1) * NT * ROWS * 4 + 512 + 1024;
-  // x for all of K where at least four stages are left besides it, else as much of K as leaves that many
-  const int room = smem_most - FIXED, whole = (p.K + 255) / 256 * 256;
-  p.seg = (room - 4 * STAGE_BYTES) / (NT * 2) / 256 * 256;
-  if (p.seg > whole) p.seg = whole;
-  p.nseg = (whole + p.seg - 1) / p.seg;
-  p.stages = (room - p.seg * NT * 2) / STAGE_BYTES;
-  if (p.stages > 12) p.stages = 12;
   const int smem = p.stages * STAGE_BYTES + p.seg * NT * 2 + FIXED;
-  const int64_t tiles = (int64_t)((p.N + ROWS - 1) / ROWS) * ((p.M + NT - 1) / NT);
-  auto kernel = matvec_int4_kernel<NT, G>;
+  const int64_t tiles = (int64_t)((p.N + p.rows - 1) / p.rows) * ((p.M + NT - 1) / NT);
+  auto kernel = matvec_int4_kernel<NT, G, CL>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  kernel<<<(unsigned)(tiles < sms ? tiles : sms), Shape<NT>::THREADS, smem, st>>>(map, p);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = CL; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.gridDim = dim3((unsigned)((tiles < ctas ? tiles : ctas) * CL), 1, 1);
+  cfg.blockDim = dim3(S::THREADS, 1, 1);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = CL > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, map, p);
+}
+
+template <int NT, int G>
+cudaError_t launch(const Params& p, const unsigned char* q, int64_t ldq, int sms, int smem_most, cudaStream_t st) {
+  // a pair of CTAs where one cannot hold x besides four stages of weights
+  const int64_t x_bytes = (int64_t)((p.K + 255) / 256) * 256 * NT * 2;
+  if (x_bytes + 4 * STAGE_BYTES + (int)sizeof(Bars) + 1024 > smem_most) return launch_cl<NT, G, 2>(p, q, ldq, sms, smem_most, st);
+  return launch_cl<NT, G, 1>(p, q, ldq, sms, smem_most, st);
 }
 
 }  // namespace mv

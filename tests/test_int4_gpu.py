@@ -165,6 +165,20 @@ def test_product(M, N, K, group):
         check_product(y, x, codes, scale, group, out)
 
 
+@pytest.mark.parametrize("M,K,group", [(64, 1024, 32), (61, 1024, 64), (33, 4096, 128), (16, 9000, 32), (7, 700, 128)])
+def test_product_of_many_tiles(M, K, group):
+    """Tens of tiles to an SM, several blocks of rows of x, x in parts and in pairs of SMs: a sample of the columns."""
+    N = 40000
+    x, codes, scale = product_case(M, N, K, group, seed=M + K)
+    q, s, xd = packed(codes), scale.to(DEV), x.to(DEV)
+    cols = torch.arange(0, N, 397)
+    a, st = dppo.dppo_matvec_int4(xd, q, s, group)
+    assert int(st.item()) == 0
+    check_product(a[:, cols.to(DEV)], x, codes[cols], scale[cols], group, F32)
+    for _ in range(3):
+        assert torch.equal(dppo.dppo_matvec_int4(xd, q, s, group)[0], a)
+
+
 def test_product_in_any_layout():
     """Row strides and offsets of every operand; what lies beside y stays."""
     M, N, K, group = 5, 70, 333, 64
