@@ -146,26 +146,35 @@ struct MatvecParams {
 };
 
 // ---- tensor cores ------------------------------------------------------------------------------------------------------
-// D[n, m] = sum over a group of (code[n, k] - 8) x[m, k] for up to 128 rows n and NT rows m at a time: the weights are the operand with the many
-// rows.  They come as they are stored by tensor copies (rows x 256 codes, 128-byte swizzle) into a ring; a thread per row turns
-// 128 codes into bf16 pairs in registers and writes them to tensor memory, where tcgen05.mma takes its A operand from; x lies in
-// shared memory for the whole launch.  The product of a group is read back, scaled by the row's scale (a thread's own) and added up in
-// fp32 registers.  One persistent CTA per SM:
-//   warp 0         tensor copies of the weights
-//   warps 1, 2     allocate tensor memory (the first), issue the MMAs of every other chunk: a wait for a barrier costs 150 cycles even where nothing is to be
-//                  waited for, and with one warp the tensor cores stood still for two of them a chunk (820 cycles instead of 380)
-//   C x 4 warps    conversion, taking the chunks of 128 codes in turn
-//   E x 4 warps    products: scale, add up, store; each warpgroup NT / E rows of x
+// D[n, m] = sum over a group of (code[n, k] - 8) x[m, k] for up to 128 rows n and a few rows m at a time: the weights are the operand with the many
+// rows.  They come as they are stored by tensor copies (rows x 256 codes, 128-byte swizzle) into a ring; a thread per row turns a chunk of
+// its codes into the tensor cores' type in registers and writes them to tensor memory, where tcgen05.mma takes its A operand from; x
+// lies in shared memory for the whole launch.  The product of a group is read back, scaled by the row's scale (a thread's own) and added up
+// in fp32 registers.  One persistent CTA per SM:
+//   warp 0          tensor copies of the weights
+//   warps 1 .. L    issue the MMAs (the first allocates tensor memory)
+//   L x 4 warps     conversion
+//   E x 4 warps     products: scale, add up, store; each warpgroup a part of the rows of x
+// Chunk i belongs to line i % L: a converting warpgroup, an issuing warp and B buffers in tensor memory, which each take their chunks in
+// order.  (Barrier phases are known by their parity, which would not do for a line that could fall two uses of a buffer behind.  With one
+// issuing warp the tensor cores stood still while it found its barriers ready, 150 cycles each.)
 // Where x does not fit, a pair of CTAs (a cluster) shares a tile, each half of K, and they exchange the sums of half of x's rows through
 // distributed shared memory; where that is not enough either, x is loaded again for each part of K.
 //
-// A word of 8 codes c0 .. c7 gives the pairs (c0, c4), (c1, c5), (c2, c6), (c3, c7): a mask and an or put a code into the low mantissa bits of
-// the bf16 number 128, and subtracting 136 leaves code - 8, exactly.  x is laid out in the order that this makes of k.
+// Two ways to the same sums:
+//   bf16   A word of 8 codes c0 .. c7 gives the pairs (c0, c4), (c1, c5), (c2, c6), (c3, c7): a mask and an or put a code into the low mantissa bits of
+//          the bf16 number 128, and subtracting 136 leaves code - 8, exactly.  11 instructions a word, chunks of 128 codes.
+//   int8   (up to 4 rows of x) The codes stay whole numbers: two masks and a shift give a word's 8 bytes.  x is written as three signed 8-bit digits in
+//          units of 2^-22 of (a power of two above) the largest entry of its group, a row of the operand each; the int32 products are exact, and
+//          8 times the sum of the digits is taken off, exactly.  What is lost of x is below 2^-23 of the group's largest entry: less than
+//          fp32 sums lose.  An MMA takes 47 cycles with up to 96 columns, of bf16 (K = 16) as of int8 (K = 32): 374 cycles for 128 rows x 128
+//          codes of bf16, 187 of int8, where HBM delivers them in 356.
+// x is laid out in the order that the conversion makes of k.
 namespace mv {
 
-constexpr int LANES = 128, CHUNK = 128;    // rows of a tile at most; codes that a thread converts at a time
-constexpr int STAGE_BYTES = LANES * 128;   // two chunks
-constexpr int XSPAN = 64;                  // k of a swizzled block of x
+constexpr int LANES = 128;                 // rows of a tile at most
+constexpr int STAGE_BYTES = LANES * 128;   // 256 codes of each row
+constexpr int DIGITS = 3;
 
 struct Params {
   const __nv_bfloat16* x;
@@ -177,22 +186,27 @@ struct Params {
   int64_t ldy;
   int y_bf16, x_vec;                       // x_vec: 16-byte loads of x allowed
   int rows, stages, seg, nseg, groups;     // rows of a tile; seg: codes of K that x lies in shared memory for (a multiple of 256), nseg of them to a CTA
-  int pairs;                               // pairs of chunks of a CTA
+  int pairs;                               // blocks of 256 codes of a CTA
   int32_t* status;
   unsigned long long wait_ns;
   int inject;
 };
 
-template <int NT, int G> struct Shape {
-  static constexpr int E = NT == 64 ? 2 : 1, EN = NT / E;              // warpgroups for the products, rows of x of each
-  static constexpr int A = CHUNK / 2, D = CHUNK / G * NT;              // columns of tensor memory of a chunk: operand, products
-  static constexpr int BUFS = 512 / (A + D) >= 6 ? 6 : 512 / (A + D) / 2 * 2;     // chunks under way
-  // Warpgroups that convert.  Barrier phases are known by their parity, so whoever waits for a buffer's last use has to know that the use before
-  // that is over.  An issuing warp has made it itself, BUFS being even.  A converting warpgroup has seen the end of the MMAs of chunk
-  // i - CONV - BUFS before its chunk i; CONV being even, that chunk and i - 2 BUFS are one issuing warp's, which takes them in order: CONV <= BUFS.
-  static constexpr int CONV = NT == 64 || BUFS < 4 ? 2 : 4;
-  static constexpr int THREADS = 96 + (CONV + E) * 128;
-  static_assert(BUFS >= 2 && BUFS % 2 == 0 && CONV % 2 == 0 && CONV <= BUFS, "barrier phases");
+// NT: columns of an MMA (bf16: rows of x; int8: DIGITS * 4 rows of x, rounded up)
+template <int NT, int G, bool I8> struct Shape {
+  static constexpr int XROWS = I8 ? 4 : NT;                            // rows of x
+  static constexpr int CHUNK = I8 ? 256 : 128, PER = 256 / CHUNK;      // codes that a thread converts at a time; chunks of a stage
+  static constexpr int STEP = I8 ? 32 : 16;                            // codes of an MMA
+  static constexpr int XBYTES = I8 ? NT : 2 * NT;                      // of shared memory for a code
+  static constexpr int XSPAN = I8 ? 128 : 64;                          // codes of a swizzled block of x
+  static constexpr int NG = CHUNK / G;
+  static constexpr int E = XROWS == 64 ? 2 : 1, EN = XROWS / E;        // warpgroups for the products, rows of x of each
+  static constexpr int A = 64, D = NG * NT, COLS = A + D;              // columns of tensor memory of a chunk: operand, products
+  static constexpr int L = !I8 && NT == 16 ? (COLS * 6 <= 512 ? 3 : 4) : 2;
+  static constexpr int B = COLS * 2 * L <= 512 ? 2 : 1;
+  static constexpr int BUFS = L * B;
+  static constexpr int THREADS = 32 + 32 * L + (L + E) * 128;
+  static_assert(BUFS * COLS <= 512, "tensor memory");
 };
 
 __device__ __forceinline__ uint32_t elect_one() {
@@ -201,9 +215,13 @@ __device__ __forceinline__ uint32_t elect_one() {
   return p;
 }
 // A from tensor memory
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
-               ::"r"(d), "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+template <bool I8> __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  if (I8)
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::i8 [%0], [%1], %2, %3, p;\n}\n"
+                 ::"r"(d), "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+  else
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
+                 ::"r"(d), "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
 }
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
   asm volatile(
@@ -222,7 +240,7 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
                : "r"(taddr));
 }
 // the 8 codes of a word as four bf16 pairs (c0, c4), (c1, c5), (c2, c6), (c3, c7), less 8
-__device__ __forceinline__ void convert(uint32_t w, uint32_t* r) {
+__device__ __forceinline__ void convert_bf16(uint32_t w, uint32_t* r) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     uint32_t v;
@@ -230,9 +248,31 @@ __device__ __forceinline__ void convert(uint32_t w, uint32_t* r) {
     asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r[i]) : "r"(v), "r"(0x43084308u));
   }
 }
+// the same as bytes (c0, c2, c4, c6), (c1, c3, c5, c7)
+__device__ __forceinline__ void convert_i8(uint32_t w, uint32_t* r) {
+  r[0] = w & 0x0f0f0f0fu;
+  r[1] = (w >> 4) & 0x0f0f0f0fu;
+}
+// half of a chunk: 32 columns
+template <bool I8> __device__ __forceinline__ void convert_half(const uint4* w, uint32_t* v) {
+#pragma unroll
+  for (int j = 0; j < (I8 ? 4 : 2); ++j) {
+    if (I8) {
+      convert_i8(w[j].x, v + 8 * j);
+      convert_i8(w[j].y, v + 8 * j + 2);
+      convert_i8(w[j].z, v + 8 * j + 4);
+      convert_i8(w[j].w, v + 8 * j + 6);
+    } else {
+      convert_bf16(w[j].x, v + 16 * j);
+      convert_bf16(w[j].y, v + 16 * j + 4);
+      convert_bf16(w[j].z, v + 16 * j + 8);
+      convert_bf16(w[j].w, v + 16 * j + 12);
+    }
+  }
+}
 
-// x rows m0 .. m0 + NT - 1, codes k0 .. k0 + seg - 1 of K, into shared memory: blocks of 64 codes, NT rows of 128 bytes each, 128-byte
-// swizzle, and within 8 codes the order that convert() makes of them.  Rows and codes that there are not are zero.
+// bf16: x rows m0 .. m0 + NT - 1, codes k0 .. k0 + seg - 1 of K, into shared memory: blocks of 64 codes, NT rows of 128 bytes each, 128-byte
+// swizzle, and within 8 codes the order that the conversion makes of them.  Rows and codes that there are not are zero.
 template <int NT, int T>
 __device__ __forceinline__ void load_x(const Params& p, unsigned char* xs, int m0, int k0, int tid) {
   constexpr int AT_ONCE = 4;               // loads in flight
@@ -269,34 +309,76 @@ __device__ __forceinline__ void load_x(const Params& p, unsigned char* xs, int m
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 
+// int8: the same for XROWS rows as digits (row digit * XROWS + m of the operand) in blocks of 128 codes, and for each group and row of x what
+// the products need: 2^22 + 2^23 - 8 times the sum of each digit (see the products), and the group's unit.  A warp per row and group.  An
+// entry that is no number, or infinite, makes the unit NaN.
+template <int NT, int XROWS, int G, int WARPS>
+__device__ __forceinline__ void load_x_digits(const Params& p, unsigned char* xs, int4* table, int m0, int k0, int warp, int lane) {
+  const int groups = p.seg / G;
+  for (int u = warp; u < groups * XROWS; u += WARPS) {
+    const int gi = u / XROWS, m = u - gi * XROWS, kg = gi * G;
+    float v[G / 32];
+    float top = 0.f;
+#pragma unroll
+    for (int j = 0; j < G / 32; ++j) {
+      const int k = k0 + kg + 32 * j + lane;
+      v[j] = m0 + m < p.M && k < p.K ? __bfloat162float(p.x[(int64_t)(m0 + m) * p.ldx + k]) : 0.f;
+      top = max_nan(top, fabsf(v[j]));
+    }
+    top = warp_max_nan(top);
+    const bool bad = !(top <= 3.4028234e38f);
+    // unit 2^(e - 21) for a largest entry in [2^e, 2^(e + 1)); tiny groups in units of 2^-121
+    const int e = max((int)(__float_as_uint(top) >> 23) - 127, -100);
+    const float up = __uint_as_float((uint32_t)(127 + 21 - e) << 23), unit = bad ? NAN : __uint_as_float((uint32_t)(127 + e - 21) << 23);
+    int sum[DIGITS] = {};
+#pragma unroll
+    for (int j = 0; j < G / 32; ++j) {
+      int X = bad ? 0 : __float2int_rn(v[j] * up);
+      const int k = kg + 32 * j + lane, byte = (k & 127 & ~7) + ((k & 1) * 4 + ((k & 7) >> 1));
+#pragma unroll
+      for (int d = 0; d < DIGITS; ++d) {
+        const int digit = d == DIGITS - 1 ? X : ((X + 128) & 255) - 128, row = d * XROWS + m;
+        X = (X - digit) >> 8;
+        sum[d] += digit;
+        xs[k / 128 * (NT * 128) + row * 128 + (byte ^ ((row & 7) << 4))] = (unsigned char)digit;
+      }
+    }
+#pragma unroll
+    for (int d = 0; d < DIGITS; ++d) sum[d] = __reduce_add_sync(0xffffffffu, sum[d]);
+    if (lane == 0) table[gi * XROWS + m] = make_int4(0x4B400000 - 8 * sum[0], 0x4B400000 - 8 * sum[1], 0x4B400000 - 8 * sum[2], (int)__float_as_uint(unit));
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+}
+
 struct Bars {
-  unsigned long long full[12], empty[12];            // stages of weights
-  unsigned long long a_full[6], done[6], d_free[6];  // chunk: operand written; MMAs done (operand free, products there); products read
-  unsigned long long x_free, x_full;                 // x replaced
-  unsigned long long sum_full, sum_free;             // pairs of CTAs: the other's sums are here; read by the other
+  unsigned long long full[12], empty[12];  // stages of weights
+  unsigned long long ready[6], done[6];    // chunk: operand written and the buffer's products before read; MMAs done (operand free, products there)
+  unsigned long long x_free, x_full;       // x replaced
+  unsigned long long sum_full, sum_free;   // pairs of CTAs: the other's sums are here; read by the other
   uint32_t tmem;
   int abort_flag;
 };
 
-template <int NT, int G, int CL>
-__global__ void __launch_bounds__(Shape<NT, G>::THREADS, 1) matvec_int4_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ Params p) {
-  using S = Shape<NT, G>;
-  constexpr int NG = CHUNK / G, BUFS = S::BUFS, CONV = S::CONV, COLS = S::A + S::D, EN = S::EN, OWN = EN / CL;
+template <int NT, int G, int CL, bool I8>
+__global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ Params p) {
+  using S = Shape<NT, G, I8>;
+  constexpr int NG = S::NG, L = S::L, B = S::B, BUFS = S::BUFS, COLS = S::COLS, EN = S::EN, OWN = EN / CL, PER = S::PER, XROWS = S::XROWS;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   unsigned char* xs = smem + p.stages * STAGE_BYTES;
-  float* sums = reinterpret_cast<float*>(xs + (size_t)p.seg * NT * 2);  // pairs: [E][OWN][LANES], from the other CTA
-  Bars* bars = reinterpret_cast<Bars*>(sums + (CL > 1 ? NT / CL * LANES : 0));
-  const uint32_t full0 = smem_u32(bars->full), empty0 = smem_u32(bars->empty), a0 = smem_u32(bars->a_full), done0 = smem_u32(bars->done), free0 = smem_u32(bars->d_free);
+  int4* table = reinterpret_cast<int4*>(xs + (size_t)p.seg * S::XBYTES);                       // int8: [groups of seg][XROWS]
+  float* sums = reinterpret_cast<float*>(table + (I8 ? p.seg / G * XROWS : 0));                // pairs of CTAs: [E][OWN][LANES], from the other
+  Bars* bars = reinterpret_cast<Bars*>(sums + (CL > 1 ? S::E * OWN * LANES : 0));
+  const uint32_t full0 = smem_u32(bars->full), empty0 = smem_u32(bars->empty), ready0 = smem_u32(bars->ready), done0 = smem_u32(bars->done);
   const uint32_t x_free = smem_u32(&bars->x_free), x_full = smem_u32(&bars->x_full), sum_full = smem_u32(&bars->sum_full), sum_free = smem_u32(&bars->sum_free);
   const WaitCtl wc{&bars->abort_flag, p.wait_ns};
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = CL > 1 ? (int)cluster_ctarank() : 0;
   if (tid == 0) {
-    for (int i = 0; i < 12; ++i) { mbar_init(full0 + 8 * i, 1); mbar_init(empty0 + 8 * i, 8); }
-    for (int i = 0; i < 6; ++i) { mbar_init(a0 + 8 * i, 4); mbar_init(done0 + 8 * i, 1); mbar_init(free0 + 8 * i, 4 * S::E); }
-    mbar_init(x_free, CONV * 4);
-    mbar_init(x_full, CONV * 4);
+    for (int i = 0; i < 12; ++i) { mbar_init(full0 + 8 * i, 1); mbar_init(empty0 + 8 * i, 4 * PER); }
+    for (int i = 0; i < 6; ++i) { mbar_init(ready0 + 8 * i, 4 + 4 * S::E); mbar_init(done0 + 8 * i, 1); }
+    mbar_init(x_free, L * 4);
+    mbar_init(x_full, L * 4);
     mbar_init(sum_full, 4 * S::E);
     mbar_init(sum_free, 4 * S::E);
     bars->abort_flag = 0;
@@ -312,10 +394,12 @@ __global__ void __launch_bounds__(Shape<NT, G>::THREADS, 1) matvec_int4_kernel(c
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = bars->tmem;
   if (CL > 1) cluster_sync_all();          // the other's barriers exist before anything is sent to them
-  // A tile is `rows` rows of the weights times NT rows of x; the blocks of x are the slow index.  A CTA's chunks are counted in pairs (a stage).
-  const int tiles_n = (p.N + p.rows - 1) / p.rows, tiles = tiles_n * ((p.M + NT - 1) / NT), seg_pairs = p.seg / 256;
+  // A tile is `rows` rows of the weights times XROWS rows of x; the blocks of x are the slow index.
+  const int tiles_n = (p.N + p.rows - 1) / p.rows, tiles = tiles_n * ((p.M + XROWS - 1) / XROWS);
   const int pair0 = rank * p.pairs, pairs = max(0, min(p.pairs, (p.K + 255) / 256 - pair0));      // this CTA's part of K
   const int first = blockIdx.x / CL, grid = gridDim.x / CL;
+  const int mine = first < tiles ? (tiles - first + grid - 1) / grid : 0;                         // tiles of this CTA
+  const int per_tile = PER * pairs, per_seg = PER * (p.seg / 256), chunks = mine * per_tile;
 
   if (warp == 0) {
     // ------------------------------------------------------------------ weights
@@ -335,64 +419,62 @@ __global__ void __launch_bounds__(Shape<NT, G>::THREADS, 1) matvec_int4_kernel(c
         }
       }
     }
-  } else if (warp < 3) {
+  } else if (warp <= L) {
     // ------------------------------------------------------------------ MMAs
-    constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(NT >> 3) << 17) | ((uint32_t)(LANES >> 4) << 24);
+    const int line = warp - 1;
+    // D = fp32, A and B = bf16; or D = int32, A unsigned and B signed 8-bit; both K-major
+    constexpr uint32_t idesc = (I8 ? (2u << 4) | (1u << 10) : (1u << 4) | (1u << 7) | (1u << 10)) | ((uint32_t)(NT >> 3) << 17) | ((uint32_t)(LANES >> 4) << 24);
     const uint64_t xdesc = gemm::make_desc_k_sw128(smem_u32(xs));
-    int b = 0, odd = 0;
+    int c = line, sub = 0;                 // place in the tile; buffer of the line
     uint32_t ph = 0;
-    bool ok = true;
-    for (int tile = first; tile < tiles && ok; tile += grid) {
-      int k = 0;                                           // within what shared memory holds of x
-      for (int c = 0; c < 2 * pairs; ++c, k = k + CHUNK == p.seg ? 0 : k + CHUNK) {
-        if (odd == warp - 1) {
-          // (the operand first: once it is there, the buffer's products before are the last ones)
-          ok = mbar_wait_warp(a0 + 8 * b, ph, wc) && mbar_wait_warp(free0 + 8 * b, ph ^ 1u, wc);
-          if (!ok) break;
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint32_t ta = tmem + b * COLS, td = ta + S::A;
-          if (elect_one()) {
+    for (int i = line; i < chunks; i += L) {
+      while (c >= per_tile) c -= per_tile;
+      int in = c;                          // place in what shared memory holds of x
+      while (in >= per_seg) in -= per_seg;
+      const uint32_t b = (uint32_t)(line * B + sub), ta = tmem + b * COLS, td = ta + S::A;
+      const uint64_t xd = xdesc + (uint64_t)((uint32_t)(in * (S::CHUNK * S::XBYTES)) >> 4);
+      if (!mbar_wait_warp(ready0 + 8 * b, ph, wc)) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      if (elect_one()) {
 #pragma unroll
-            for (int i = 0; i < CHUNK / 16; ++i) {         // 16 codes an MMA
-              const int at = (k + 16 * i) / XSPAN * (NT * 128) + (16 * i) % XSPAN * 2;
-              mma_ts(td + (16 * i) / G * NT, ta + 8 * i, xdesc + (uint64_t)(at >> 4), idesc, (16 * i) % G != 0);
-            }
-            gemm::mma_commit(done0 + 8 * b);
-          }
-          __syncwarp();
+        for (int j = 0; j < S::CHUNK / S::STEP; ++j) {     // 32 bytes of a row of x an MMA
+          const int at = (S::STEP * j) / S::XSPAN * (NT * 128) + j * 32 % 128;
+          mma_ts<I8>(td + (S::STEP * j) / G * NT, ta + 8 * j, xd + (uint64_t)(at >> 4), idesc, (S::STEP * j) % G != 0);
         }
-        odd ^= 1;
-        if (++b == BUFS) { b = 0; ph ^= 1u; }
+        gemm::mma_commit(done0 + 8 * b);
       }
+      __syncwarp();
+      c += L;
+      if (++sub == B) { sub = 0; ph ^= 1u; }
     }
-  } else if (warp < 3 + 4 * CONV) {
+  } else if (warp < 1 + L + 4 * L) {
     // ------------------------------------------------------------------ conversion
-    const int g = (warp - 3) >> 2, q = warp & 3, r = q * 32 + lane;     // (a warp's lanes of tensor memory are given by its number)
+    const int line = (warp - 1 - L) >> 2, q = warp & 3, r = q * 32 + lane;      // (a warp's lanes of tensor memory are given by its number)
     const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16);
-    const int mine = first < tiles ? (tiles - first + grid - 1) / grid : 0;      // tiles of this CTA
-    const bool one = p.nseg == 1 && p.M <= NT;             // one part of x for everything
-    const int parts = one ? (mine > 0 && pairs > 0 ? 1 : 0) : mine * p.nseg;
+    const bool one = p.nseg == 1 && p.M <= XROWS;          // one part of x for everything
+    const int parts = one ? (chunks > 0 ? 1 : 0) : mine * p.nseg;
     int x_now = -1;                        // which part of x (block of rows, part of K) shared memory holds
     uint32_t n_x = 0;
-    // this warpgroup's next chunk of all the CTA's: its number, its place in the ring (in chunks) and its buffer
-    int i = g, at = g, b = g;
+    int i = line, at = line, sub = 0;      // next chunk: its number, place in the ring (in chunks) and buffer of the line
     uint32_t ph = 0, bph = 0;
-    if (b >= BUFS) { b -= BUFS; bph ^= 1u; }
     bool ok = true;
     for (int part = 0; part < parts && ok; ++part) {
-      int end = mine * 2 * pairs;
+      int end = chunks;
       if (!one || x_now < 0) {
-        const int t = one ? 0 : part / p.nseg, seg = one ? 0 : part - t * p.nseg, start = t * 2 * pairs + seg * 2 * seg_pairs;
-        if (!one) end = t * 2 * pairs + min(2 * pairs, (seg + 1) * 2 * seg_pairs);
+        const int t = one ? 0 : part / p.nseg, seg = one ? 0 : part - t * p.nseg, start = t * per_tile + seg * per_seg;
+        if (!one) end = t * per_tile + min(per_tile, (seg + 1) * per_seg);
         if (start >= end) continue;        // (a CTA's last part of K may be empty)
         const int block = (first + t * grid) / tiles_n, x_want = block * p.nseg + seg;
         if (x_now != x_want) {
-          // once the MMAs with the part before are done: those of the chunk before this part's first, whoever converts it, are the last
-          if (start > 0 && !mbar_wait_warp(done0 + 8 * ((start - 1) % BUFS), (uint32_t)((start - 1) / BUFS) & 1u, wc)) { ok = false; break; }
+          // once the MMAs with the part before are done: this warpgroup's own last chunk, the others see to theirs
+          const int last = i - L, lsub = sub ? sub - 1 : B - 1;
+          if (last >= 0 && !mbar_wait_warp(done0 + 8 * (line * B + lsub), sub ? bph : bph ^ 1u, wc)) { ok = false; break; }
           __syncwarp();
           if (lane == 0) mbar_arrive(x_free);
           if (!mbar_wait_warp(x_free, n_x & 1u, wc)) { ok = false; break; }
-          load_x<NT, CONV * 128>(p, xs, block * NT, (pair0 + seg * seg_pairs) * 256, tid - 96);
+          const int k0 = (pair0 + seg * (p.seg / 256)) * 256;
+          if (I8) load_x_digits<NT, XROWS, G, L * 4>(p, xs, table, block * XROWS, k0, warp - 1 - L, lane);
+          else load_x<NT, L * 128>(p, xs, block * XROWS, k0, tid - 32 - 32 * L);
           __syncwarp();
           if (lane == 0) mbar_arrive(x_full);
           if (!mbar_wait_warp(x_full, n_x & 1u, wc)) { ok = false; break; }
@@ -400,41 +482,39 @@ __global__ void __launch_bounds__(Shape<NT, G>::THREADS, 1) matvec_int4_kernel(c
           x_now = x_want;
         }
       }
-      for (; i < end; i += CONV) {
-        const int s = at >> 1;
+      for (; i < end; i += L) {
+        const int s = at / PER, b = line * B + sub;
         if (!mbar_wait_warp(full0 + 8 * s, ph, wc)) { ok = false; break; }
         const uint32_t src = smem_u32(smem) + s * STAGE_BYTES + r * 128;
-        uint4 w[4];
+        constexpr int PIECES = S::CHUNK / 32;              // of 16 bytes
+        uint4 w[PIECES];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = lds128(src + ((((at & 1) * 4 + j) ^ (r & 7)) << 4));
+        for (int j = 0; j < PIECES; ++j) w[j] = lds128(src + ((((at % PER) * PIECES + j) ^ (r & 7)) << 4));
         __syncwarp();
         if (lane == 0) mbar_arrive(empty0 + 8 * s);
         uint32_t v[32];
-        auto half = [&](const uint4& x, const uint4& y) {
-          convert(x.x, v); convert(x.y, v + 4); convert(x.z, v + 8); convert(x.w, v + 12);
-          convert(y.x, v + 16); convert(y.y, v + 20); convert(y.z, v + 24); convert(y.w, v + 28);
-        };
-        half(w[0], w[1]);
+        convert_half<I8>(w, v);
         if (!mbar_wait_warp(done0 + 8 * b, bph ^ 1u, wc)) { ok = false; break; }       // the buffer's operand before has been used
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         tmem_st32(lane_base + b * COLS, v);
-        half(w[2], w[3]);
+        convert_half<I8>(w + PIECES / 2, v);
         tmem_st32(lane_base + b * COLS + 32, v);
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         __syncwarp();
-        if (lane == 0) mbar_arrive(a0 + 8 * b);
-        at += CONV;
-        if (at >= 2 * p.stages) { at -= 2 * p.stages; ph ^= 1u; }
-        b += CONV;
-        if (b >= BUFS) { b -= BUFS; bph ^= 1u; }
+        if (lane == 0) mbar_arrive(ready0 + 8 * b);
+        at += L;
+        if (at >= PER * p.stages) { at -= PER * p.stages; ph ^= 1u; }
+        if (++sub == B) { sub = 0; bph ^= 1u; }
       }
     }
   } else {
     // ------------------------------------------------------------------ products
-    const int e = (warp - 3 - 4 * CONV) >> 2, q = warp & 3, r = q * 32 + lane;
-    const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16) + S::A + e * EN;
-    int b = 0;
+    const int e = (warp - 1 - L - 4 * L) >> 2, q = warp & 3, r = q * 32 + lane;
+    const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16) + S::A + (I8 ? 0 : e * EN);
+    if (lane == 0)
+      for (int i = 0; i < BUFS; ++i) mbar_arrive(ready0 + 8 * i);      // nothing to be read before a buffer's first use
+    int line = 0, sub = 0;                 // of the next chunk
     uint32_t ph = 0, n_tile = 0;
     bool ok = true;
     int tn = first % tiles_n, block = first / tiles_n;     // of the tile under way
@@ -445,24 +525,24 @@ __global__ void __launch_bounds__(Shape<NT, G>::THREADS, 1) matvec_int4_kernel(c
       if (p.y_bf16) *reinterpret_cast<__nv_bfloat16*>(at) = __float2bfloat16_rn(v);
       else *reinterpret_cast<float*>(at) = v;
     };
-    // The row's scales, fetched two pairs of chunks ahead (their latency is that of L2 or of memory), the next tile's first along with this
-    // one's last.
-    const int glim = min(max(p.groups - 2 * pair0 * NG, 0), 2 * pairs * NG);      // this CTA's groups
+    // The row's scales, fetched AHEAD chunks ahead (their latency is that of L2 or of memory), the next tile's first along with this one's last.
+    constexpr int AHEAD = I8 ? 2 : 4;
+    const int g0 = pair0 * (256 / G), glim = min(max(p.groups - g0, 0), per_tile * NG);           // this CTA's groups
     auto scales_of = [&](int tile_n, bool there) {
       const int n = tile_n * p.rows + r;
-      return there && r < p.rows && n < p.N ? reinterpret_cast<const unsigned short*>(p.scale) + (int64_t)n * p.lds + 2 * pair0 * NG : nullptr;
+      return there && r < p.rows && n < p.N ? reinterpret_cast<const unsigned short*>(p.scale) + (int64_t)n * p.lds + g0 : nullptr;
     };
-    unsigned short sc[2][2 * NG];
+    unsigned short sc[AHEAD][NG];
     auto fetch = [&](const unsigned short* row, int c, unsigned short* to) {
 #pragma unroll
-      for (int h = 0; h < 2 * NG; ++h) {
+      for (int h = 0; h < NG; ++h) {
         to[h] = 0;
         if (row && c * NG + h < glim) to[h] = __ldg(row + c * NG + h);
       }
     };
     const unsigned short* srow = scales_of(tn, first < tiles);
-    fetch(srow, 0, sc[0]);
-    fetch(srow, 2, sc[1]);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) fetch(srow, u, sc[u]);
     // pairs of CTAs: this CTA's rows of x of the tile before wait for the other's sums
     float keep[CL > 1 ? OWN : 1];
     char* keep_at = nullptr;
@@ -471,21 +551,25 @@ __global__ void __launch_bounds__(Shape<NT, G>::THREADS, 1) matvec_int4_kernel(c
       if (CL == 1 || keep_rows < 0) return true;
       if (!__all_sync(0xffffffffu, mbar_wait_cluster(sum_full, (n_tile - 1u) & 1u, wc))) return false;
       const float* theirs = sums + e * OWN * LANES + r;
-      char* at = keep_at;
 #pragma unroll
-      for (int j = 0; j < (CL > 1 ? OWN : 0); ++j) {
-        if (j >= keep_rows) break;
-        const float o = theirs[j * LANES];
-        if (keep_at) put(at, rank == 0 ? keep[j] + o : o + keep[j]);
-        at += ystep;
-      }
+      for (int j = 0; j < (CL > 1 ? OWN : 0); ++j)
+        if (j < keep_rows) keep[j] = rank == 0 ? keep[j] + theirs[j * LANES] : theirs[j * LANES] + keep[j];
       __syncwarp();
-      if (lane == 0) bar_arrive_cluster(map_to_cta(sum_free, (uint32_t)(rank ^ 1)));
+      if (lane == 0) bar_arrive_cluster(map_to_cta(sum_free, (uint32_t)(rank ^ 1)));    // (before the stores: a release waits for them)
+      if (keep_at) {
+        char* at = keep_at;
+#pragma unroll
+        for (int j = 0; j < (CL > 1 ? OWN : 0); ++j) {
+          if (j >= keep_rows) break;
+          put(at, keep[j]);
+          at += ystep;
+        }
+      }
       keep_rows = -1;
       return true;
     };
     for (int tile = first; tile < tiles && ok; tile += grid) {
-      const int n = tn * p.rows + r, m0 = block * NT + e * EN;
+      const int n = tn * p.rows + r, m0 = block * XROWS + e * EN;
       const bool live = srow != nullptr;
       tn += grid;
       while (tn >= tiles_n) { tn -= tiles_n; ++block; }
@@ -493,36 +577,57 @@ __global__ void __launch_bounds__(Shape<NT, G>::THREADS, 1) matvec_int4_kernel(c
       float2 acc[EN / 2];
 #pragma unroll
       for (int j = 0; j < EN / 2; ++j) acc[j] = make_float2(0.f, 0.f);
-      for (int c0 = 0; c0 < 2 * pairs && ok; c0 += 4) {
+      const int4* tab = table;             // int8: of the next chunk
+      int in = 0;
+      for (int c0 = 0; c0 < per_tile && ok; c0 += AHEAD) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int c = c0 + 2 * u;
-          if (c < 2 * pairs && ok) {                       // two chunks: buffers b and b + 1
-            ok = mbar_wait_warp(done0 + 8 * b, ph, wc) && mbar_wait_warp(done0 + 8 * b + 8, ph, wc);
+        for (int u = 0; u < AHEAD; ++u) {
+          const int c = c0 + u;
+          if (c < per_tile && ok) {
+            const uint32_t b = (uint32_t)(line * B + sub), td = lane_base + b * COLS;
+            ok = mbar_wait_warp(done0 + 8 * b, ph, wc);
             if (ok) {
               asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
               for (int h = 0; h < NG; ++h) {
-                const float s0 = __uint_as_float((uint32_t)sc[u][h] << 16), s1 = __uint_as_float((uint32_t)sc[u][NG + h] << 16);
-#pragma unroll
-                for (int j0 = 0; j0 < EN; j0 += 16) {
-                  uint32_t v[32];
-                  tmem_ld16(lane_base + b * COLS + h * NT + j0, v);
-                  tmem_ld16(lane_base + (b + 1) * COLS + h * NT + j0, v + 16);
+                const float s1 = __uint_as_float((uint32_t)sc[u][h] << 16);
+                if (I8) {
+                  uint32_t v[16];
+                  tmem_ld16(td + h * NT, v);
                   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                  float* a = reinterpret_cast<float*>(acc);
 #pragma unroll
-                  for (int j = 0; j < 8; ++j) {
-                    acc[j0 / 2 + j] = __ffma2_rn(make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), make_float2(s0, s0), acc[j0 / 2 + j]);
-                    acc[j0 / 2 + j] = __ffma2_rn(make_float2(__uint_as_float(v[16 + 2 * j]), __uint_as_float(v[17 + 2 * j])), make_float2(s1, s1), acc[j0 / 2 + j]);
+                  for (int m = 0; m < XROWS; ++m) {
+                    if (m0 + m >= p.M) break;
+                    // v - 8 (sum of the digits) is below 2^22 in magnitude: added to the bits of 1.5 2^23 it gives that number plus it
+                    const int4 t = tab[h * XROWS + m];
+                    const float d0 = __int_as_float((int)v[m] + t.x) - 12582912.f, d1 = __int_as_float((int)v[XROWS + m] + t.y) - 12582912.f;
+                    const float d2 = __int_as_float((int)v[2 * XROWS + m] + t.z) - 12582912.f;
+                    a[m] = fmaf(s1 * __int_as_float(t.w), fmaf(d2, 65536.f, fmaf(d1, 256.f, d0)), a[m]);
+                  }
+                } else {
+                  const float2 s2 = make_float2(s1, s1);
+                  constexpr int AT = EN < 32 ? 16 : 32;    // columns read together
+#pragma unroll
+                  for (int j0 = 0; j0 < EN; j0 += AT) {
+                    uint32_t v[AT];
+                    tmem_ld16(td + h * NT + j0, v);
+                    if (AT == 32) tmem_ld16(td + h * NT + j0 + 16, v + AT - 16);
+                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                    for (int j = 0; j < AT / 2; ++j) acc[j0 / 2 + j] = __ffma2_rn(make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), s2, acc[j0 / 2 + j]);
                   }
                 }
               }
               asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
               __syncwarp();
-              if (lane == 0) { mbar_arrive(free0 + 8 * b); mbar_arrive(free0 + 8 * b + 8); }
-              if (c + 4 < 2 * pairs) fetch(srow, c + 4, sc[u]); else fetch(srow_next, 2 * u, sc[u]);
-              b += 2;
-              if (b == BUFS) { b = 0; ph ^= 1u; }
+              if (lane == 0) mbar_arrive(ready0 + 8 * b);
+              if (c + AHEAD < per_tile) fetch(srow, c + AHEAD, sc[u]); else fetch(srow_next, u, sc[u]);
+              if (I8) { tab += NG * XROWS; if (++in == per_seg) { in = 0; tab = table; } }
+              if (++line == L) {
+                line = 0;
+                if (++sub == B) { sub = 0; ph ^= 1u; }
+              }
             }
           }
         }
@@ -547,7 +652,7 @@ __global__ void __launch_bounds__(Shape<NT, G>::THREADS, 1) matvec_int4_kernel(c
         const int rows = min(p.M - m0 - (rank ^ 1) * OWN, OWN);
 #pragma unroll
         for (int j = 0; j < OWN; ++j) {
-          const float lo = (j & 1) ? acc[j / 2].y : acc[j / 2].x, hi = (j & 1) ? acc[(OWN + j) / 2].y : acc[(OWN + j) / 2].x;
+          const float lo = (j & 1) ? acc[j / 2].y : acc[j / 2].x, hi = ((OWN + j) & 1) ? acc[(OWN + j) / 2 % (EN / 2)].y : acc[(OWN + j) / 2 % (EN / 2)].x;
           keep[CL > 1 ? j : 0] = rank == 0 ? lo : hi;
           if (j < rows) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(dst + (uint32_t)(j * LANES * 4)), "f"(rank == 0 ? hi : lo) : "memory");
         }
@@ -589,17 +694,18 @@ EncodeFn get_encode() {
   return fn;
 }
 
-template <int NT, int G, int CL>
+template <int NT, int G, int CL, bool I8>
 cudaError_t launch_cl(Params p, const unsigned char* q, int64_t ldq, int sms, int smem_most, cudaStream_t st) {
-  using S = Shape<NT, G>;
-  constexpr int FIXED = (CL > 1 ? NT / CL * LANES * 4 : 0) + (int)sizeof(Bars) + 1024;
+  using S = Shape<NT, G, I8>;
+  constexpr int FIXED = (CL > 1 ? S::E * S::EN / CL * LANES * 4 : 0) + (int)sizeof(Bars) + 1024;
+  constexpr int X256 = 256 * S::XBYTES + (I8 ? 256 / G * S::XROWS * 16 : 0);               // shared memory for 256 codes of x
   const int room = smem_most - FIXED, total = (p.K + 255) / 256;
   p.pairs = (total + CL - 1) / CL;
   // x for all of this CTA's K where at least four stages are left besides it, else as much as leaves that many
-  int most = (room - 4 * STAGE_BYTES) / (NT * 2) / 256;
+  const int most = (room - 4 * STAGE_BYTES) / X256;
   p.nseg = (p.pairs + most - 1) / most;
   p.seg = (p.pairs + p.nseg - 1) / p.nseg * 256;
-  p.stages = (room - p.seg * NT * 2) / STAGE_BYTES;
+  p.stages = (room - p.seg / 256 * X256) / STAGE_BYTES;
   if (p.stages > 12) p.stages = 12;
   // rows of a tile: rounds of tiles over the CTAs that are as full as they can be
   const int64_t ctas = sms / CL, rounds = (p.N + ctas * LANES - 1) / (ctas * LANES);
@@ -611,9 +717,9 @@ cudaError_t launch_cl(Params p, const unsigned char* q, int64_t ldq, int sms, in
   if (!enc || enc(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<unsigned char*>(q), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return cudaErrorInvalidValue;
-  const int smem = p.stages * STAGE_BYTES + p.seg * NT * 2 + FIXED;
-  const int64_t tiles = (int64_t)((p.N + p.rows - 1) / p.rows) * ((p.M + NT - 1) / NT);
-  auto kernel = matvec_int4_kernel<NT, G, CL>;
+  const int smem = p.stages * STAGE_BYTES + p.seg / 256 * X256 + FIXED;
+  const int64_t tiles = (int64_t)((p.N + p.rows - 1) / p.rows) * ((p.M + S::XROWS - 1) / S::XROWS);
+  auto kernel = matvec_int4_kernel<NT, G, CL, I8>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -629,12 +735,21 @@ cudaError_t launch_cl(Params p, const unsigned char* q, int64_t ldq, int sms, in
   return cudaLaunchKernelEx(&cfg, kernel, map, p);
 }
 
-template <int NT, int G>
+template <int NT, int G, bool I8>
 cudaError_t launch(const Params& p, const unsigned char* q, int64_t ldq, int sms, int smem_most, cudaStream_t st) {
   // a pair of CTAs where one cannot hold x besides four stages of weights
-  const int64_t x_bytes = (int64_t)((p.K + 255) / 256) * 256 * NT * 2;
-  if (x_bytes + 4 * STAGE_BYTES + (int)sizeof(Bars) + 1024 > smem_most) return launch_cl<NT, G, 2>(p, q, ldq, sms, smem_most, st);
-  return launch_cl<NT, G, 1>(p, q, ldq, sms, smem_most, st);
+  using S = Shape<NT, G, I8>;
+  const int64_t x_bytes = (int64_t)((p.K + 255) / 256) * (256 * S::XBYTES + (I8 ? 256 / G * S::XROWS * 16 : 0));
+  if (x_bytes + 4 * STAGE_BYTES + (int)sizeof(Bars) + 1024 > smem_most) return launch_cl<NT, G, 2, I8>(p, q, ldq, sms, smem_most, st);
+  return launch_cl<NT, G, 1, I8>(p, q, ldq, sms, smem_most, st);
+}
+
+template <int NT, bool I8>
+cudaError_t launch_group(const Params& p, int group, const unsigned char* q, int64_t ldq, int sms, int smem_most, cudaStream_t st) {
+  if (group == 128) return launch<NT, 128, I8>(p, q, ldq, sms, smem_most, st);
+  if (group == 64) return launch<NT, 64, I8>(p, q, ldq, sms, smem_most, st);
+  if constexpr (NT < 64) return launch<NT, 32, I8>(p, q, ldq, sms, smem_most, st);
+  return cudaErrorInvalidValue;
 }
 
 }  // namespace mv
@@ -756,7 +871,7 @@ extern "C" int dppo_matvec_int4(const void* x, int64_t x_row_stride, const uint8
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
   // bulk copies of the weights: rows on 16-byte boundaries
   const int64_t pitch = N > 1 ? q_row_stride : ((K + 1) / 2 + 15) / 16 * 16;
-  if (K > 0 && (uintptr_t)q % 16 == 0 && pitch % 16 == 0 && N * ((M + 15) / 16) < ((int64_t)1 << 31)) {
+  if (K > 0 && (uintptr_t)q % 16 == 0 && pitch % 16 == 0 && N * ((M + 3) / 4) * ((K + 127) / 128) < ((int64_t)1 << 31)) {
     mv::Params m = {};
     m.x = p.x; m.ldx = p.ldx; m.scale = p.scale; m.lds = p.lds; m.M = (int)M; m.N = (int)N; m.K = (int)K; m.y = y; m.ldy = p.ldy; m.y_bf16 = p.y_bf16;
     m.x_vec = (uintptr_t)x % 16 == 0 && (M == 1 || x_row_stride % 8 == 0);
@@ -766,15 +881,13 @@ extern "C" int dppo_matvec_int4(const void* x, int64_t x_row_stride, const uint8
     cudaGetDevice(&dev);
     cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev);
-    // rows of x that one pass over the weights serves (the products of 64 rows and groups of 32 would not fit tensor memory)
+    // Rows of x that one pass over the weights serves.  (Of 64 rows and groups of 32 the products would not fit tensor memory.)  Up to four rows as
+    // integers: the int8 MMAs of a tile take half as long, and above that its products take longer than the bf16 ones.
     cudaError_t e;
-    if (M <= 16) {
-      e = group == 128 ? mv::launch<16, 128>(m, q, pitch, sms, most, st) : group == 64 ? mv::launch<16, 64>(m, q, pitch, sms, most, st) : mv::launch<16, 32>(m, q, pitch, sms, most, st);
-    } else if (M <= 32 || group == 32) {
-      e = group == 128 ? mv::launch<32, 128>(m, q, pitch, sms, most, st) : group == 64 ? mv::launch<32, 64>(m, q, pitch, sms, most, st) : mv::launch<32, 32>(m, q, pitch, sms, most, st);
-    } else {
-      e = group == 128 ? mv::launch<64, 128>(m, q, pitch, sms, most, st) : mv::launch<64, 64>(m, q, pitch, sms, most, st);
-    }
+    if (M <= 4) e = mv::launch_group<16, true>(m, group, q, pitch, sms, most, st);
+    else if (M <= 16) e = mv::launch_group<16, false>(m, group, q, pitch, sms, most, st);
+    else if (M <= 32 || group == 32) e = mv::launch_group<32, false>(m, group, q, pitch, sms, most, st);
+    else e = mv::launch_group<64, false>(m, group, q, pitch, sms, most, st);
     return e == cudaSuccess ? DPPO_OK : DPPO_ERR_CUDA;
   }
   const int64_t warps = N * ((M + kGRows - 1) / kGRows), grid = (warps + kGThreads / 32 - 1) / (kGThreads / 32);
