@@ -154,7 +154,7 @@ struct MatvecParams {
 //   warp 0          tensor copies of the weights
 //   warps 1 .. L    issue the MMAs (the first allocates tensor memory)
 //   L x 4 warps     conversion
-//   E x 4 warps     products: scale, add up, store; each warpgroup a part of the rows of x
+//   2 x 4 warps     products: scale, add up, store; each warpgroup all of every other tile, or (64 rows of x) half of x's rows
 // Chunk i belongs to line i % L: a converting warpgroup, an issuing warp and B buffers in tensor memory, which each take their chunks in
 // order.  (Barrier phases are known by their parity, which would not do for a line that could fall two uses of a buffer behind.  With one
 // issuing warp the tensor cores stood still while it found its barriers ready, 150 cycles each.)
@@ -192,7 +192,7 @@ struct Params {
   int inject;
 };
 
-// NT: columns of an MMA (bf16: rows of x; int8: DIGITS * 4 rows of x, rounded up)
+// NT: columns of an MMA (bf16: rows of x; int8: four to a row of x, of which DIGITS count)
 template <int NT, int G, bool I8> struct Shape {
   static constexpr int XROWS = I8 ? 4 : NT;                            // rows of x
   static constexpr int CHUNK = I8 ? 256 : 128, PER = 256 / CHUNK;      // codes that a thread converts at a time; chunks of a stage
@@ -200,12 +200,13 @@ template <int NT, int G, bool I8> struct Shape {
   static constexpr int XBYTES = I8 ? NT : 2 * NT;                      // of shared memory for a code
   static constexpr int XSPAN = I8 ? 128 : 64;                          // codes of a swizzled block of x
   static constexpr int NG = CHUNK / G;
-  static constexpr int E = XROWS == 64 ? 2 : 1, EN = XROWS / E;        // warpgroups for the products, rows of x of each
+  static constexpr int E = XROWS == 64 ? 2 : 1, EN = XROWS / E;        // warpgroups for a tile's products, rows of x of each
+  static constexpr int TURNS = 2 / E;                                  // sets of them, which take the tiles in turn: one stores while the other adds up
   static constexpr int A = 64, D = NG * NT, COLS = A + D;              // columns of tensor memory of a chunk: operand, products
   static constexpr int L = !I8 && NT == 16 ? (COLS * 6 <= 512 ? 3 : 4) : 2;
   static constexpr int B = COLS * 2 * L <= 512 ? 2 : 1;
   static constexpr int BUFS = L * B;
-  static constexpr int THREADS = 32 + 32 * L + (L + E) * 128;
+  static constexpr int THREADS = 32 + 32 * L + (L + E * TURNS) * 128;
   static_assert(BUFS * COLS <= 512, "tensor memory");
 };
 
@@ -238,6 +239,9 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
                  "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_ld4(uint32_t taddr, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];\n" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr));
 }
 // the 8 codes of a word as four bf16 pairs (c0, c4), (c1, c5), (c2, c6), (c3, c7), less 8
 __device__ __forceinline__ void convert_bf16(uint32_t w, uint32_t* r) {
@@ -309,7 +313,7 @@ __device__ __forceinline__ void load_x(const Params& p, unsigned char* xs, int m
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 
-// int8: the same for XROWS rows as digits (row digit * XROWS + m of the operand) in blocks of 128 codes, and for each group and row of x what
+// int8: the same for XROWS rows as digits (row 4 m + digit of the operand) in blocks of 128 codes, and for each group and row of x what
 // the products need: 2^22 + 2^23 - 8 times the sum of each digit (see the products), and the group's unit.  A warp per row and group.  An
 // entry that is no number, or infinite, makes the unit NaN.
 template <int NT, int XROWS, int G, int WARPS>
@@ -337,7 +341,7 @@ __device__ __forceinline__ void load_x_digits(const Params& p, unsigned char* xs
       const int k = kg + 32 * j + lane, byte = (k & 127 & ~7) + ((k & 1) * 4 + ((k & 7) >> 1));
 #pragma unroll
       for (int d = 0; d < DIGITS; ++d) {
-        const int digit = d == DIGITS - 1 ? X : ((X + 128) & 255) - 128, row = d * XROWS + m;
+        const int digit = d == DIGITS - 1 ? X : ((X + 128) & 255) - 128, row = 4 * m + d;
         X = (X - digit) >> 8;
         sum[d] += digit;
         xs[k / 128 * (NT * 128) + row * 128 + (byte ^ ((row & 7) << 4))] = (unsigned char)digit;
@@ -354,7 +358,8 @@ struct Bars {
   unsigned long long full[12], empty[12];  // stages of weights
   unsigned long long ready[6], done[6];    // chunk: operand written and the buffer's products before read; MMAs done (operand free, products there)
   unsigned long long x_free, x_full;       // x replaced
-  unsigned long long sum_full, sum_free;   // pairs of CTAs: the other's sums are here; read by the other
+  unsigned long long turn[2];              // the other set has read its tile's last products
+  unsigned long long sum_full[2], sum_free[2];       // pairs of CTAs, by whose turn it is: the other's sums are here; read by the other
   uint32_t tmem;
   int abort_flag;
 };
@@ -362,15 +367,15 @@ struct Bars {
 template <int NT, int G, int CL, bool I8>
 __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ Params p) {
   using S = Shape<NT, G, I8>;
-  constexpr int NG = S::NG, L = S::L, B = S::B, BUFS = S::BUFS, COLS = S::COLS, EN = S::EN, OWN = EN / CL, PER = S::PER, XROWS = S::XROWS;
+  constexpr int NG = S::NG, L = S::L, B = S::B, BUFS = S::BUFS, COLS = S::COLS, EN = S::EN, OWN = EN / CL, PER = S::PER, XROWS = S::XROWS, TURNS = S::TURNS;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   unsigned char* xs = smem + p.stages * STAGE_BYTES;
   int4* table = reinterpret_cast<int4*>(xs + (size_t)p.seg * S::XBYTES);                       // int8: [groups of seg][XROWS]
-  float* sums = reinterpret_cast<float*>(table + (I8 ? p.seg / G * XROWS : 0));                // pairs of CTAs: [E][OWN][LANES], from the other
-  Bars* bars = reinterpret_cast<Bars*>(sums + (CL > 1 ? S::E * OWN * LANES : 0));
+  float* sums = reinterpret_cast<float*>(table + (I8 ? p.seg / G * XROWS : 0));                // pairs of CTAs: [TURNS][E][OWN][LANES], from the other
+  Bars* bars = reinterpret_cast<Bars*>(sums + (CL > 1 ? TURNS * S::E * OWN * LANES : 0));
   const uint32_t full0 = smem_u32(bars->full), empty0 = smem_u32(bars->empty), ready0 = smem_u32(bars->ready), done0 = smem_u32(bars->done);
-  const uint32_t x_free = smem_u32(&bars->x_free), x_full = smem_u32(&bars->x_full), sum_full = smem_u32(&bars->sum_full), sum_free = smem_u32(&bars->sum_free);
+  const uint32_t x_free = smem_u32(&bars->x_free), x_full = smem_u32(&bars->x_full);
   const WaitCtl wc{&bars->abort_flag, p.wait_ns};
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = CL > 1 ? (int)cluster_ctarank() : 0;
@@ -379,8 +384,7 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
     for (int i = 0; i < 6; ++i) { mbar_init(ready0 + 8 * i, 4 + 4 * S::E); mbar_init(done0 + 8 * i, 1); }
     mbar_init(x_free, L * 4);
     mbar_init(x_full, L * 4);
-    mbar_init(sum_full, 4 * S::E);
-    mbar_init(sum_free, 4 * S::E);
+    for (int i = 0; i < TURNS; ++i) { mbar_init(smem_u32(&bars->turn[i]), 4); mbar_init(smem_u32(&bars->sum_full[i]), 1); mbar_init(smem_u32(&bars->sum_free[i]), 4 * S::E); }
     bars->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -510,14 +514,16 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
     }
   } else {
     // ------------------------------------------------------------------ products
-    const int e = (warp - 1 - L - 4 * L) >> 2, q = warp & 3, r = q * 32 + lane;
+    const int wg = (warp - 1 - L - 4 * L) >> 2, e = S::E > 1 ? wg : 0, turn = S::E > 1 ? 0 : wg, q = warp & 3, r = q * 32 + lane;
     const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16) + S::A + (I8 ? 0 : e * EN);
-    if (lane == 0)
+    const uint32_t sum_full = smem_u32(&bars->sum_full[turn]), sum_free = smem_u32(&bars->sum_free[turn]);
+    float* inbox = sums + (turn * S::E + e) * OWN * LANES + r;
+    if (turn == 0 && lane == 0)
       for (int i = 0; i < BUFS; ++i) mbar_arrive(ready0 + 8 * i);      // nothing to be read before a buffer's first use
-    int line = 0, sub = 0;                 // of the next chunk
-    uint32_t ph = 0, n_tile = 0;
+    const int stride = TURNS * grid;       // between this set's tiles
+    uint32_t n_tile = 0;
     bool ok = true;
-    int tn = first % tiles_n, block = first / tiles_n;     // of the tile under way
+    int tile = first + turn * grid, tn = tile % tiles_n, block = tile / tiles_n;
     const int ysize = p.y_bf16 ? 2 : 4;
     const int64_t ystep = p.ldy * ysize;
     auto y_at = [&](int n, int m) { return reinterpret_cast<char*>(p.y) + m * ystep + (int64_t)n * ysize; };
@@ -540,7 +546,7 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
         if (row && c * NG + h < glim) to[h] = __ldg(row + c * NG + h);
       }
     };
-    const unsigned short* srow = scales_of(tn, first < tiles);
+    const unsigned short* srow = scales_of(tn, tile < tiles);
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) fetch(srow, u, sc[u]);
     // pairs of CTAs: this CTA's rows of x of the tile before wait for the other's sums
@@ -550,12 +556,12 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
     auto complete = [&]() {
       if (CL == 1 || keep_rows < 0) return true;
       if (!__all_sync(0xffffffffu, mbar_wait_cluster(sum_full, (n_tile - 1u) & 1u, wc))) return false;
-      const float* theirs = sums + e * OWN * LANES + r;
 #pragma unroll
-      for (int j = 0; j < (CL > 1 ? OWN : 0); ++j)
-        if (j < keep_rows) keep[j] = rank == 0 ? keep[j] + theirs[j * LANES] : theirs[j * LANES] + keep[j];
+      for (int j = 0; j < (CL > 1 ? OWN : 0); ++j) keep[j] = rank == 0 ? keep[j] + inbox[j * LANES] : inbox[j * LANES] + keep[j];
+      __threadfence_block();
       __syncwarp();
-      if (lane == 0) bar_arrive_cluster(map_to_cta(sum_free, (uint32_t)(rank ^ 1)));    // (before the stores: a release waits for them)
+      // (nothing but what was read is behind this arrival; a release would wait for the stores to y)
+      if (lane == 0) asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(map_to_cta(sum_free, (uint32_t)(rank ^ 1))) : "memory");
       if (keep_at) {
         char* at = keep_at;
 #pragma unroll
@@ -568,15 +574,21 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
       keep_rows = -1;
       return true;
     };
-    for (int tile = first; tile < tiles && ok; tile += grid) {
+    for (int k = turn; tile < tiles && ok; tile += stride, k += TURNS) {       // k: this CTA's tiles
+      // the tile's first chunk: its line, and how often the line's buffers have been used
+      const uint32_t i0 = (uint32_t)k * (uint32_t)per_tile;
+      int line = (int)(i0 % L), sub = (int)(i0 / L % B);
+      uint32_t ph = i0 / (L * B) & 1u;
       const int n = tn * p.rows + r, m0 = block * XROWS + e * EN;
       const bool live = srow != nullptr;
-      tn += grid;
+      tn += stride;
       while (tn >= tiles_n) { tn -= tiles_n; ++block; }
-      const unsigned short* srow_next = scales_of(tn, tile + grid < tiles);
+      const unsigned short* srow_next = scales_of(tn, tile + stride < tiles);
       float2 acc[EN / 2];
 #pragma unroll
       for (int j = 0; j < EN / 2; ++j) acc[j] = make_float2(0.f, 0.f);
+      // Once the tile before has been read, by the other set: all uses of the buffers before this tile's are over then, as the parities want.
+      if (TURNS > 1 && k > 0) ok = mbar_wait_warp(smem_u32(&bars->turn[turn]), (uint32_t)((k - 1) / 2) & 1u, wc);
       const int4* tab = table;             // int8: of the next chunk
       int in = 0;
       for (int c0 = 0; c0 < per_tile && ok; c0 += AHEAD) {
@@ -588,24 +600,42 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
             ok = mbar_wait_warp(done0 + 8 * b, ph, wc);
             if (ok) {
               asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+              if (I8) {
+                float* a = reinterpret_cast<float*>(acc);
+                // v - 8 (sum of the digits) is below 2^22 in magnitude: added to the bits of 1.5 2^23 it gives that number plus it
+                auto add = [&](const uint32_t* v, int m, float s1, const int4& t) {
+                  const float d0 = __int_as_float((int)v[0] + t.x) - 12582912.f, d1 = __int_as_float((int)v[1] + t.y) - 12582912.f;
+                  const float d2 = __int_as_float((int)v[2] + t.z) - 12582912.f;
+                  a[m] = fmaf(s1 * __int_as_float(t.w), fmaf(d2, 65536.f, fmaf(d1, 256.f, d0)), a[m]);
+                };
+                if (p.M == 1) {            // a single row: its digits only
+                  uint32_t v[NG][4];
 #pragma unroll
-              for (int h = 0; h < NG; ++h) {
-                const float s1 = __uint_as_float((uint32_t)sc[u][h] << 16);
-                if (I8) {
-                  uint32_t v[16];
-                  tmem_ld16(td + h * NT, v);
+                  for (int h = 0; h < NG; ++h) tmem_ld4(td + h * NT, v[h]);
                   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-                  float* a = reinterpret_cast<float*>(acc);
 #pragma unroll
-                  for (int m = 0; m < XROWS; ++m) {
-                    if (m0 + m >= p.M) break;
-                    // v - 8 (sum of the digits) is below 2^22 in magnitude: added to the bits of 1.5 2^23 it gives that number plus it
-                    const int4 t = tab[h * XROWS + m];
-                    const float d0 = __int_as_float((int)v[m] + t.x) - 12582912.f, d1 = __int_as_float((int)v[XROWS + m] + t.y) - 12582912.f;
-                    const float d2 = __int_as_float((int)v[2 * XROWS + m] + t.z) - 12582912.f;
-                    a[m] = fmaf(s1 * __int_as_float(t.w), fmaf(d2, 65536.f, fmaf(d1, 256.f, d0)), a[m]);
-                  }
+                  for (int h = 0; h < NG; ++h) add(v[h], 0, __uint_as_float((uint32_t)sc[u][h] << 16), tab[h * XROWS]);
                 } else {
+                  constexpr int AT = NG < 4 ? NG : 4;      // groups read together
+#pragma unroll
+                  for (int h0 = 0; h0 < NG; h0 += AT) {
+                    uint32_t v[AT][16];
+#pragma unroll
+                    for (int h = 0; h < AT; ++h) tmem_ld16(td + (h0 + h) * NT, v[h]);
+                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                    for (int h = 0; h < AT; ++h)
+#pragma unroll
+                      for (int m = 0; m < XROWS; ++m) {
+                        if (m0 + m >= p.M) break;
+                        add(v[h] + 4 * m, m, __uint_as_float((uint32_t)sc[u][h0 + h] << 16), tab[(h0 + h) * XROWS + m]);
+                      }
+                  }
+                }
+              } else {
+#pragma unroll
+                for (int h = 0; h < NG; ++h) {
+                  const float s1 = __uint_as_float((uint32_t)sc[u][h] << 16);
                   const float2 s2 = make_float2(s1, s1);
                   constexpr int AT = EN < 32 ? 16 : 32;    // columns read together
 #pragma unroll
@@ -633,7 +663,12 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
         }
         if (ok && c0 == 0) ok = complete();
       }
-      if (!ok || !complete()) { ok = false; break; }
+      if (!ok) break;
+      if (TURNS > 1) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars->turn[turn ^ 1]));
+      }
+      if (!complete()) { ok = false; break; }
       if (CL == 1) {
         if (live) {
           char* at = y_at(n, m0);
@@ -646,18 +681,18 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
           }
         }
       } else {
-        // the other's rows of x go over there, once it has read what went before
+        // The other's rows of x go over there, once it has read what went before: asynchronous stores, which count on the barrier there themselves
+        // (an arrival that releases ordinary ones takes some 3000 cycles, the stores to y before it among them).
         if (n_tile > 0 && !__all_sync(0xffffffffu, mbar_wait_cluster(sum_free, (n_tile - 1u) & 1u, wc))) { ok = false; break; }
-        const uint32_t dst = map_to_cta(smem_u32(sums + e * OWN * LANES + r), (uint32_t)(rank ^ 1));
-        const int rows = min(p.M - m0 - (rank ^ 1) * OWN, OWN);
+        const uint32_t dst = map_to_cta(smem_u32(inbox), (uint32_t)(rank ^ 1)), bar = map_to_cta(sum_full, (uint32_t)(rank ^ 1));
+        if (e == 0 && q == 0 && lane == 0) mbar_arrive_expect_tx(sum_full, S::E * OWN * LANES * 4);
 #pragma unroll
         for (int j = 0; j < OWN; ++j) {
           const float lo = (j & 1) ? acc[j / 2].y : acc[j / 2].x, hi = ((OWN + j) & 1) ? acc[(OWN + j) / 2 % (EN / 2)].y : acc[(OWN + j) / 2 % (EN / 2)].x;
           keep[CL > 1 ? j : 0] = rank == 0 ? lo : hi;
-          if (j < rows) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(dst + (uint32_t)(j * LANES * 4)), "f"(rank == 0 ? hi : lo) : "memory");
+          asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];"
+                       ::"r"(dst + (uint32_t)(j * LANES * 4)), "r"(__float_as_uint(rank == 0 ? hi : lo)), "r"(bar) : "memory");
         }
-        __syncwarp();
-        if (lane == 0) bar_arrive_cluster(map_to_cta(sum_full, (uint32_t)(rank ^ 1)));
         keep_rows = max(0, min(p.M - m0 - rank * OWN, OWN));
         keep_at = live ? y_at(n, m0 + rank * OWN) : nullptr;
       }
@@ -697,7 +732,7 @@ EncodeFn get_encode() {
 template <int NT, int G, int CL, bool I8>
 cudaError_t launch_cl(Params p, const unsigned char* q, int64_t ldq, int sms, int smem_most, cudaStream_t st) {
   using S = Shape<NT, G, I8>;
-  constexpr int FIXED = (CL > 1 ? S::E * S::EN / CL * LANES * 4 : 0) + (int)sizeof(Bars) + 1024;
+  constexpr int FIXED = (CL > 1 ? S::TURNS * S::E * S::EN / CL * LANES * 4 : 0) + (int)sizeof(Bars) + 1024;
   constexpr int X256 = 256 * S::XBYTES + (I8 ? 256 / G * S::XROWS * 16 : 0);               // shared memory for 256 codes of x
   const int room = smem_most - FIXED, total = (p.K + 255) / 256;
   p.pairs = (total + CL - 1) / CL;
