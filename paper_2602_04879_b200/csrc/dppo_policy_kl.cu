@@ -500,8 +500,8 @@ __global__ void __launch_bounds__(kRingThreads<FORM != DPPO_KL_K3>, 1) policy_kl
             }
             add_vectors<InT, FORM, PER>(w, zv, yv);
           }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(empty + 8u * pos.slot);
+          // (a vote on the sums, which are never negative: the arrival is not to be moved up between the loads and their use)
+          if (!__any_sync(0xffffffffu, w.S < 0.f || (TWO && w.Sy < 0.f)) && lane == 0) mbar_arrive(empty + 8u * pos.slot);
           pos.advance(kSumSlots);
         }
         w = merge_lanes<FORM>(w);
