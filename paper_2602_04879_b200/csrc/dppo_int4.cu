@@ -154,7 +154,7 @@ struct MatvecParams {
 //   warp 0          tensor copies of the weights
 //   warps 1 .. L    issue the MMAs (the first allocates tensor memory)
 //   L x 4 warps     conversion
-//   2 x 4 warps     products: scale, add up, store; each warpgroup all of every other tile, or (64 rows of x) half of x's rows
+//   P x 4 warps     products: scale, add up, store
 // Chunk i belongs to line i % L: a converting warpgroup, an issuing warp and B buffers in tensor memory, which each take their chunks in
 // order.  (Barrier phases are known by their parity, which would not do for a line that could fall two uses of a buffer behind.  With one
 // issuing warp the tensor cores stood still while it found its barriers ready, 150 cycles each.)
@@ -200,13 +200,15 @@ template <int NT, int G, bool I8> struct Shape {
   static constexpr int XBYTES = I8 ? NT : 2 * NT;                      // of shared memory for a code
   static constexpr int XSPAN = I8 ? 128 : 64;                          // codes of a swizzled block of x
   static constexpr int NG = CHUNK / G;
-  static constexpr int E = XROWS == 64 ? 2 : 1, EN = XROWS / E;        // warpgroups for a tile's products, rows of x of each
-  static constexpr int TURNS = 2 / E;                                  // sets of them, which take the tiles in turn: one stores while the other adds up
+  // Warpgroups for the products.  bf16: 16 rows of x each, and of a single one's tiles two take turns, so that one stores while the other adds
+  // up.  int8: two, each half of a chunk's groups, whose sums meet at the tile's end.
+  static constexpr int E = I8 ? 1 : NT / 16, EN = XROWS / E, SPLIT = I8 ? 2 : 1, TURNS = !I8 && E == 1 ? 2 : 1;
+  static constexpr int PRODUCTS = E * SPLIT * TURNS, READERS = E * SPLIT;      // in all; of a chunk
   static constexpr int A = 64, D = NG * NT, COLS = A + D;              // columns of tensor memory of a chunk: operand, products
   static constexpr int L = !I8 && NT == 16 ? (COLS * 6 <= 512 ? 3 : 4) : 2;
   static constexpr int B = COLS * 2 * L <= 512 ? 2 : 1;
   static constexpr int BUFS = L * B;
-  static constexpr int THREADS = 32 + 32 * L + (L + E * TURNS) * 128;
+  static constexpr int THREADS = 32 + 32 * L + (L + PRODUCTS) * 128;
   static_assert(BUFS * COLS <= 512, "tensor memory");
 };
 
@@ -242,6 +244,13 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
 }
 __device__ __forceinline__ void tmem_ld4(uint32_t taddr, uint32_t* r) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];\n" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr));
+}
+// What the loads before brought is there.  (It names their registers: the compiler sees no other reason to use, or to spill, them after it.)
+template <int N> __device__ __forceinline__ void tmem_ld_wait(uint32_t* r) {
+  static_assert(N % 4 == 0, "");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < N; i += 4) asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]));
 }
 // the 8 codes of a word as four bf16 pairs (c0, c4), (c1, c5), (c2, c6), (c3, c7), less 8
 __device__ __forceinline__ void convert_bf16(uint32_t w, uint32_t* r) {
@@ -358,7 +367,7 @@ struct Bars {
   unsigned long long full[12], empty[12];  // stages of weights
   unsigned long long ready[6], done[6];    // chunk: operand written and the buffer's products before read; MMAs done (operand free, products there)
   unsigned long long x_free, x_full;       // x replaced
-  unsigned long long turn[2];              // the other set has read its tile's last products
+  unsigned long long turn[2];              // two sets by turns: the other has read its tile's last products.  Halves: the second's sums are here; read
   unsigned long long sum_full[2], sum_free[2];       // pairs of CTAs, by whose turn it is: the other's sums are here; read by the other
   uint32_t tmem;
   int abort_flag;
@@ -372,7 +381,8 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   unsigned char* xs = smem + p.stages * STAGE_BYTES;
   int4* table = reinterpret_cast<int4*>(xs + (size_t)p.seg * S::XBYTES);                       // int8: [groups of seg][XROWS]
-  float* sums = reinterpret_cast<float*>(table + (I8 ? p.seg / G * XROWS : 0));                // pairs of CTAs: [TURNS][E][OWN][LANES], from the other
+  float* halves = reinterpret_cast<float*>(table + (I8 ? p.seg / G * XROWS : 0));              // int8: [XROWS][LANES], from the second half of the groups
+  float* sums = halves + (I8 ? XROWS * LANES : 0);                                             // pairs of CTAs: [TURNS][E][OWN][LANES], from the other
   Bars* bars = reinterpret_cast<Bars*>(sums + (CL > 1 ? TURNS * S::E * OWN * LANES : 0));
   const uint32_t full0 = smem_u32(bars->full), empty0 = smem_u32(bars->empty), ready0 = smem_u32(bars->ready), done0 = smem_u32(bars->done);
   const uint32_t x_free = smem_u32(&bars->x_free), x_full = smem_u32(&bars->x_full);
@@ -381,10 +391,11 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
   const int rank = CL > 1 ? (int)cluster_ctarank() : 0;
   if (tid == 0) {
     for (int i = 0; i < 12; ++i) { mbar_init(full0 + 8 * i, 1); mbar_init(empty0 + 8 * i, 4 * PER); }
-    for (int i = 0; i < 6; ++i) { mbar_init(ready0 + 8 * i, 4 + 4 * S::E); mbar_init(done0 + 8 * i, 1); }
+    for (int i = 0; i < 6; ++i) { mbar_init(ready0 + 8 * i, 4 + 4 * S::READERS); mbar_init(done0 + 8 * i, 1); }
     mbar_init(x_free, L * 4);
     mbar_init(x_full, L * 4);
-    for (int i = 0; i < TURNS; ++i) { mbar_init(smem_u32(&bars->turn[i]), 4); mbar_init(smem_u32(&bars->sum_full[i]), 1); mbar_init(smem_u32(&bars->sum_free[i]), 4 * S::E); }
+    for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&bars->turn[i]), 4);
+    for (int i = 0; i < TURNS; ++i) { mbar_init(smem_u32(&bars->sum_full[i]), 1); mbar_init(smem_u32(&bars->sum_free[i]), 4 * S::E); }
     bars->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -494,8 +505,6 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
         uint4 w[PIECES];
 #pragma unroll
         for (int j = 0; j < PIECES; ++j) w[j] = lds128(src + ((((at % PER) * PIECES + j) ^ (r & 7)) << 4));
-        __syncwarp();
-        if (lane == 0) mbar_arrive(empty0 + 8 * s);
         uint32_t v[32];
         convert_half<I8>(w, v);
         if (!mbar_wait_warp(done0 + 8 * b, bph ^ 1u, wc)) { ok = false; break; }       // the buffer's operand before has been used
@@ -506,7 +515,9 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         __syncwarp();
-        if (lane == 0) mbar_arrive(ready0 + 8 * b);
+        // The stage is given back here, where its codes have been used: with the arrival right behind the loads, before the wait above, codes of
+        // the stage's next content turned up among these.
+        if (lane == 0) { mbar_arrive(ready0 + 8 * b); mbar_arrive(empty0 + 8 * s); }
         at += L;
         if (at >= PER * p.stages) { at -= PER * p.stages; ph ^= 1u; }
         if (++sub == B) { sub = 0; bph ^= 1u; }
@@ -514,7 +525,7 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
     }
   } else {
     // ------------------------------------------------------------------ products
-    const int wg = (warp - 1 - L - 4 * L) >> 2, e = S::E > 1 ? wg : 0, turn = S::E > 1 ? 0 : wg, q = warp & 3, r = q * 32 + lane;
+    const int wg = (warp - 1 - L - 4 * L) >> 2, e = S::E > 1 ? wg : 0, turn = TURNS > 1 ? wg : 0, half = S::SPLIT > 1 ? wg : 0, q = warp & 3, r = q * 32 + lane;
     const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16) + S::A + (I8 ? 0 : e * EN);
     const uint32_t sum_full = smem_u32(&bars->sum_full[turn]), sum_free = smem_u32(&bars->sum_free[turn]);
     float* inbox = sums + (turn * S::E + e) * OWN * LANES + r;
@@ -538,12 +549,16 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
       const int n = tile_n * p.rows + r;
       return there && r < p.rows && n < p.N ? reinterpret_cast<const unsigned short*>(p.scale) + (int64_t)n * p.lds + g0 : nullptr;
     };
-    unsigned short sc[AHEAD][NG];
-    auto fetch = [&](const unsigned short* row, int c, unsigned short* to) {
+    // (a register each, and the loads by predicate: nothing here may wait for them)
+    constexpr int OWN_G = NG / S::SPLIT;
+    uint32_t sc[AHEAD][OWN_G];
+    auto fetch = [&](const unsigned short* row, int c, uint32_t* to) {
 #pragma unroll
-      for (int h = 0; h < NG; ++h) {
-        to[h] = 0;
-        if (row && c * NG + h < glim) to[h] = __ldg(row + c * NG + h);
+      for (int h = 0; h < OWN_G; ++h) {
+        const int gi = c * NG + half * OWN_G + h;
+        to[h] = 0u;
+        asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %2, 0;\n @q ld.global.nc.u16 %0, [%1];\n}\n"
+                     : "+r"(to[h]) : "l"(row + gi), "r"((int)(row && gi < glim)));
       }
     };
     const unsigned short* srow = scales_of(tn, tile < tiles);
@@ -584,13 +599,14 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
       tn += stride;
       while (tn >= tiles_n) { tn -= tiles_n; ++block; }
       const unsigned short* srow_next = scales_of(tn, tile + stride < tiles);
+      if (srow_next)                       // (a load that comes from memory would hold up the use of those before it)
+        for (int i = 0; i < glim; i += 16) asm volatile("prefetch.global.L2 [%0];" ::"l"(srow_next + i));
       float2 acc[EN / 2];
 #pragma unroll
       for (int j = 0; j < EN / 2; ++j) acc[j] = make_float2(0.f, 0.f);
       // Once the tile before has been read, by the other set: all uses of the buffers before this tile's are over then, as the parities want.
       if (TURNS > 1 && k > 0) ok = mbar_wait_warp(smem_u32(&bars->turn[turn]), (uint32_t)((k - 1) / 2) & 1u, wc);
       const int4* tab = table;             // int8: of the next chunk
-      int in = 0;
       for (int c0 = 0; c0 < per_tile && ok; c0 += AHEAD) {
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
@@ -608,34 +624,35 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
                   const float d2 = __int_as_float((int)v[2] + t.z) - 12582912.f;
                   a[m] = fmaf(s1 * __int_as_float(t.w), fmaf(d2, 65536.f, fmaf(d1, 256.f, d0)), a[m]);
                 };
+                const int h0 = half * OWN_G;
                 if (p.M == 1) {            // a single row: its digits only
-                  uint32_t v[NG][4];
+                  uint32_t v[OWN_G][4];
 #pragma unroll
-                  for (int h = 0; h < NG; ++h) tmem_ld4(td + h * NT, v[h]);
-                  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                  for (int h = 0; h < OWN_G; ++h) tmem_ld4(td + (h0 + h) * NT, v[h]);
+                  tmem_ld_wait<OWN_G * 4>(v[0]);
 #pragma unroll
-                  for (int h = 0; h < NG; ++h) add(v[h], 0, __uint_as_float((uint32_t)sc[u][h] << 16), tab[h * XROWS]);
+                  for (int h = 0; h < OWN_G; ++h) add(v[h], 0, __uint_as_float(sc[u][h] << 16), tab[(h0 + h) * XROWS]);
                 } else {
-                  constexpr int AT = NG < 4 ? NG : 4;      // groups read together
+                  constexpr int AT = OWN_G < 2 ? OWN_G : 2;      // groups read together
 #pragma unroll
-                  for (int h0 = 0; h0 < NG; h0 += AT) {
+                  for (int h1 = 0; h1 < OWN_G; h1 += AT) {
                     uint32_t v[AT][16];
 #pragma unroll
-                    for (int h = 0; h < AT; ++h) tmem_ld16(td + (h0 + h) * NT, v[h]);
-                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                    for (int h = 0; h < AT; ++h) tmem_ld16(td + (h0 + h1 + h) * NT, v[h]);
+                    tmem_ld_wait<AT * 16>(v[0]);
 #pragma unroll
                     for (int h = 0; h < AT; ++h)
 #pragma unroll
                       for (int m = 0; m < XROWS; ++m) {
                         if (m0 + m >= p.M) break;
-                        add(v[h] + 4 * m, m, __uint_as_float((uint32_t)sc[u][h0 + h] << 16), tab[(h0 + h) * XROWS + m]);
+                        add(v[h] + 4 * m, m, __uint_as_float(sc[u][h1 + h] << 16), tab[(h0 + h1 + h) * XROWS + m]);
                       }
                   }
                 }
               } else {
 #pragma unroll
                 for (int h = 0; h < NG; ++h) {
-                  const float s1 = __uint_as_float((uint32_t)sc[u][h] << 16);
+                  const float s1 = __uint_as_float(sc[u][h] << 16);
                   const float2 s2 = make_float2(s1, s1);
                   constexpr int AT = EN < 32 ? 16 : 32;    // columns read together
 #pragma unroll
@@ -643,7 +660,7 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
                     uint32_t v[AT];
                     tmem_ld16(td + h * NT + j0, v);
                     if (AT == 32) tmem_ld16(td + h * NT + j0 + 16, v + AT - 16);
-                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                    tmem_ld_wait<AT>(v);
 #pragma unroll
                     for (int j = 0; j < AT / 2; ++j) acc[j0 / 2 + j] = __ffma2_rn(make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), s2, acc[j0 / 2 + j]);
                   }
@@ -653,7 +670,7 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
               __syncwarp();
               if (lane == 0) mbar_arrive(ready0 + 8 * b);
               if (c + AHEAD < per_tile) fetch(srow, c + AHEAD, sc[u]); else fetch(srow_next, u, sc[u]);
-              if (I8) { tab += NG * XROWS; if (++in == per_seg) { in = 0; tab = table; } }
+              if (I8) tab += NG * XROWS;
               if (++line == L) {
                 line = 0;
                 if (++sub == B) { sub = 0; ph ^= 1u; }
@@ -661,12 +678,34 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
             }
           }
         }
-        if (ok && c0 == 0) ok = complete();
+        if (ok && c0 == 0 && half == 0) ok = complete();
       }
       if (!ok) break;
       if (TURNS > 1) {
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bars->turn[turn ^ 1]));
+      }
+      if (S::SPLIT > 1) {
+        // the halves' sums meet
+        float* a = reinterpret_cast<float*>(acc);
+        const uint32_t here = smem_u32(&bars->turn[0]), read = smem_u32(&bars->turn[1]);
+        if (half == 1) {
+          if (n_tile > 0 && !mbar_wait_warp(read, (n_tile - 1u) & 1u, wc)) { ok = false; break; }
+#pragma unroll
+          for (int m = 0; m < XROWS; ++m)
+            if (m0 + m < p.M) halves[m * LANES + r] = a[m];
+          __syncwarp();
+          if (lane == 0) mbar_arrive(here);
+          srow = srow_next;
+          ++n_tile;
+          continue;
+        }
+        if (!mbar_wait_warp(here, n_tile & 1u, wc)) { ok = false; break; }
+#pragma unroll
+        for (int m = 0; m < XROWS; ++m)
+          if (m0 + m < p.M) a[m] += halves[m * LANES + r];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(read);
       }
       if (!complete()) { ok = false; break; }
       if (CL == 1) {
@@ -699,7 +738,7 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
       srow = srow_next;
       ++n_tile;
     }
-    if (ok) complete();
+    if (ok && half == 0) complete();
   }
   __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -729,15 +768,24 @@ EncodeFn get_encode() {
   return fn;
 }
 
+template <int NT, int G, int CL, bool I8> struct Room {
+  using S = Shape<NT, G, I8>;
+  static constexpr int FIXED = (I8 ? S::XROWS * LANES * 4 : 0) + (CL > 1 ? S::TURNS * S::E * S::EN / CL * LANES * 4 : 0) + (int)sizeof(Bars) + 1024;
+  static constexpr int X256 = 256 * S::XBYTES + (I8 ? 256 / G * S::XROWS * 16 : 0);        // shared memory for 256 codes of x
+};
+// blocks of 256 codes of x that fit besides four stages of weights
+template <int NT, int G, int CL, bool I8> int x_blocks(int smem_most) {
+  return (smem_most - Room<NT, G, CL, I8>::FIXED - 4 * STAGE_BYTES) / Room<NT, G, CL, I8>::X256;
+}
+
 template <int NT, int G, int CL, bool I8>
 cudaError_t launch_cl(Params p, const unsigned char* q, int64_t ldq, int sms, int smem_most, cudaStream_t st) {
   using S = Shape<NT, G, I8>;
-  constexpr int FIXED = (CL > 1 ? S::TURNS * S::E * S::EN / CL * LANES * 4 : 0) + (int)sizeof(Bars) + 1024;
-  constexpr int X256 = 256 * S::XBYTES + (I8 ? 256 / G * S::XROWS * 16 : 0);               // shared memory for 256 codes of x
+  constexpr int FIXED = Room<NT, G, CL, I8>::FIXED, X256 = Room<NT, G, CL, I8>::X256;
   const int room = smem_most - FIXED, total = (p.K + 255) / 256;
   p.pairs = (total + CL - 1) / CL;
   // x for all of this CTA's K where at least four stages are left besides it, else as much as leaves that many
-  const int most = (room - 4 * STAGE_BYTES) / X256;
+  const int most = x_blocks<NT, G, CL, I8>(smem_most);
   p.nseg = (p.pairs + most - 1) / most;
   p.seg = (p.pairs + p.nseg - 1) / p.nseg * 256;
   p.stages = (room - p.seg / 256 * X256) / STAGE_BYTES;
@@ -772,11 +820,14 @@ cudaError_t launch_cl(Params p, const unsigned char* q, int64_t ldq, int sms, in
 
 template <int NT, int G, bool I8>
 cudaError_t launch(const Params& p, const unsigned char* q, int64_t ldq, int sms, int smem_most, cudaStream_t st) {
-  // a pair of CTAs where one cannot hold x besides four stages of weights
-  using S = Shape<NT, G, I8>;
-  const int64_t x_bytes = (int64_t)((p.K + 255) / 256) * (256 * S::XBYTES + (I8 ? 256 / G * S::XROWS * 16 : 0));
-  if (x_bytes + 4 * STAGE_BYTES + (int)sizeof(Bars) + 1024 > smem_most) return launch_cl<NT, G, 2, I8>(p, q, ldq, sms, smem_most, st);
-  return launch_cl<NT, G, 1, I8>(p, q, ldq, sms, smem_most, st);
+  // A pair of CTAs where one cannot hold x besides four stages of weights.  Where a pair cannot either, x comes in parts, and as bf16: the products
+  // read what the digits came with from shared memory, after the MMAs.
+  const int blocks = (p.K + 255) / 256;
+  if (blocks <= x_blocks<NT, G, 1, I8>(smem_most)) return launch_cl<NT, G, 1, I8>(p, q, ldq, sms, smem_most, st);
+  if constexpr (I8) {
+    if ((blocks + 1) / 2 > x_blocks<NT, G, 2, true>(smem_most)) return launch<16, G, false>(p, q, ldq, sms, smem_most, st);
+  }
+  return launch_cl<NT, G, 2, I8>(p, q, ldq, sms, smem_most, st);
 }
 
 template <int NT, bool I8>

@@ -179,6 +179,20 @@ def test_product_of_many_tiles(M, K, group):
         assert torch.equal(dppo.dppo_matvec_int4(xd, q, s, group)[0], a)
 
 
+@pytest.mark.parametrize("M,K,group,N", [(1, 9000, 32, 40000), (3, 9000, 32, 40000), (4, 4096, 32, 40000), (1, 16000, 64, 20000),
+                                         (3, 33000, 32, 9000), (1, 70000, 128, 700), (20, 33000, 64, 5000)])
+def test_product_of_few_rows_and_long_ones_repeats(M, K, group, N):
+    """Rows of the weights that come and go while the products before them are still under way; rows of x too long for shared memory."""
+    x, codes, scale = product_case(M, N, K, group, seed=M + K)
+    q, s, xd = packed(codes), scale.to(DEV), x.to(DEV)
+    cols = torch.arange(0, N, max(1, N // 40))
+    a, st = dppo.dppo_matvec_int4(xd, q, s, group)
+    assert int(st.item()) == 0
+    check_product(a[:, cols.to(DEV)], x, codes[cols], scale[cols], group, F32)
+    for _ in range(25):
+        assert torch.equal(dppo.dppo_matvec_int4(xd, q, s, group)[0], a)
+
+
 def test_product_in_any_layout():
     """Row strides and offsets of every operand; what lies beside y stays."""
     M, N, K, group = 5, 70, 333, 64
