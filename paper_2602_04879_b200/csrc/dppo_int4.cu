@@ -47,68 +47,102 @@ __device__ __forceinline__ int code_of(float x, float scale, float inv) {
   const int c = min(k + up, 7);
   return x < 0.f ? -c : c;
 }
+// Eight numbers to a word of codes, and their values.  fp32: one by one.
+__device__ __forceinline__ uint32_t codes_of(const float2* x, float scale, float inv, float2* val) {
+  uint32_t w = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int c0 = code_of(x[j].x, scale, inv), c1 = code_of(x[j].y, scale, inv);
+    w |= (uint32_t)(c0 + 8) << (8 * j) | (uint32_t)(c1 + 8) << (8 * j + 4);
+    val[j] = make_float2((float)c0 * scale, (float)c1 * scale);
+  }
+  return w;
+}
+// bf16: x / scale is a quotient of two 8-bit mantissas, so it is the middle of two whole numbers or at least 2^-10 away from it (|2 x - (2 k + 1) scale| is
+// a multiple of half of scale's last place at least).  So the product with the reciprocal, off by less than 2^-19, is first rounded to
+// a multiple of 2^-11, which makes a middle exact, and then to a whole number, ties to even; both by adding 1.5 2^23 units.  The second sum's
+// low bits are the code, and a word's codes are the sum of those bits, shifted, less what the rest of the bits come to.
+__device__ __forceinline__ uint32_t codes_of_bf16(const float2* x, float scale, float inv, float2* val) {
+  constexpr float FINE = 6144.f, WHOLE = 12582912.f + 8.f;
+  constexpr uint32_t REST = 0x4B400000u + (0x4B400000u << 4) + (0x4B400000u << 8);
+  const float2 s2 = make_float2(scale, scale), i2 = make_float2(inv, inv), f2 = make_float2(FINE, FINE), nf2 = make_float2(-FINE, -FINE);
+  const float2 w2 = make_float2(WHOLE, WHOLE), nw2 = make_float2(-WHOLE, -WHOLE);
+  uint32_t w = 0u - REST;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 b = __fadd2_rn(__fadd2_rn(__ffma2_rn(x[j], i2, f2), nf2), w2);
+    val[j] = __fmul2_rn(__fadd2_rn(b, nw2), s2);
+    w += (__float_as_uint(b.x) << (8 * j)) + (__float_as_uint(b.y) << (8 * j + 4));
+  }
+  return w;
+}
 
+// A thread has pieces of 8 columns, all of them loaded before the first is used; a group's G / 8 pieces lie in neighbouring lanes.
 template <typename InT, int G>
 __global__ void __launch_bounds__(kQThreads) int4_quantize_kernel(QuantParams p) {
-  constexpr int LANES = G / 8;
+  constexpr int LANES = G / 8, WORDS = sizeof(InT) == 2 ? 1 : 2;           // 16-byte words of a piece
+  constexpr bool BF16 = sizeof(InT) == 2;
   const InT* X = reinterpret_cast<const InT*>(p.x);
   InT* Vv = reinterpret_cast<InT*>(p.values);
-  const int64_t total = p.rows * p.slots;
-  const int64_t first = (int64_t)blockIdx.x * (kQThreads * kQItems) + threadIdx.x;
-  float v[kQItems][8];
-  int64_t row[kQItems], col[kQItems];
+  const uint32_t slots = (uint32_t)p.slots;
+  const int64_t first = (int64_t)blockIdx.x * (kQThreads * kQItems);
+  const int64_t row0 = first / slots;
+  const uint32_t slot0 = (uint32_t)(first - row0 * slots) + threadIdx.x;
+  uint4 raw[kQItems][WORDS];
 #pragma unroll
   for (int k = 0; k < kQItems; ++k) {
-    const int64_t i = first + k * kQThreads;
-    row[k] = -1;
-    col[k] = 0;
+    const uint32_t at = slot0 + k * kQThreads, r = at / slots;
+    const int64_t row = row0 + r;
+    const uint32_t col = (at - r * slots) * 8;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[k][j] = 0.f;
-    if (i < total) {
-      row[k] = total <= 0xffffffffll ? (int64_t)((uint32_t)i / (uint32_t)p.slots) : i / p.slots;
-      col[k] = (i - row[k] * p.slots) * 8;
-      const InT* src = X + row[k] * p.ldx + col[k];
-      if (p.x_whole && col[k] + 8 <= p.cols) {
-        float2 z[4];
-        if (sizeof(InT) == 2) {
-          to_pairs<__nv_bfloat16>(ldg128_stream(src), z);
-        } else {
-          to_pairs<float>(ldg128_stream(src), z);
-          to_pairs<float>(ldg128_stream(src + 4), z + 2);
-        }
+    for (int u = 0; u < WORDS; ++u) raw[k][u] = make_uint4(0u, 0u, 0u, 0u);
+    if (row < p.rows) {
+      const InT* src = X + row * p.ldx + col;
+      if (p.x_whole && col + 8 <= p.cols) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) { v[k][2 * j] = z[j].x; v[k][2 * j + 1] = z[j].y; }
+        for (int u = 0; u < WORDS; ++u) raw[k][u] = ldg128_stream(src + u * 4);
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (col[k] + j < p.cols) v[k][j] = to_f32<InT>(src[j]);
+          if (col + j < p.cols) set_raw(raw[k][BF16 ? 0 : j / 4], BF16 ? j : j % 4, src[j]);
       }
     }
   }
 #pragma unroll
   for (int k = 0; k < kQItems; ++k) {
-    float amax = 0.f;
+    RawMax<InT> most;
+    most.m = {};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) amax = max_nan(amax, fabsf(v[k][j]));
+    for (int u = 0; u < WORDS; ++u) {
+      constexpr uint32_t MAGNITUDE = BF16 ? 0x7fff7fffu : 0x7fffffffu;
+      const uint4& v = raw[k][u];
+      most.add(make_uint4(v.x & MAGNITUDE, v.y & MAGNITUDE, v.z & MAGNITUDE, v.w & MAGNITUDE));
+    }
+    float amax = most.value();
 #pragma unroll
     for (int o = LANES / 2; o > 0; o >>= 1) amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-    if (row[k] < 0 || col[k] >= p.cols) continue;          // (a piece of the last group may lie behind the row)
+    const uint32_t at = slot0 + k * kQThreads, r = at / slots;
+    const int64_t row = row0 + r;
+    const uint32_t col = (at - r * slots) * 8;
+    if (row >= p.rows || col >= p.cols) continue;          // (a piece of the last group may lie behind the row)
     const bool bad = !(amax <= 3.4028234e38f);
-    const float scale = bad ? NAN : group_scale(fmaxf(amax, 7.888609052210118e-31f)), inv = bad ? 0.f : __frcp_rn(scale);
+    float scale = group_scale(fmaxf(amax, 7.888609052210118e-31f)), inv = __frcp_rn(scale);
+    float2 x[4], val[4];
+#pragma unroll
+    for (int u = 0; u < WORDS; ++u) to_pairs<InT>(raw[k][u], x + 2 * u);
+    if (bad) {
+      scale = NAN;
+      inv = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = make_float2(0.f, 0.f);
+    }
     if ((threadIdx.x & (LANES - 1)) == 0) {
-      p.scale[row[k] * p.lds + col[k] / G] = __float2bfloat16_rn(scale);
+      p.scale[row * p.lds + col / G] = __float2bfloat16_rn(scale);
       if (bad) atomicOr(p.status, DPPO_STATUS_NONFINITE_ROW);
     }
-    uint32_t w = 0;
-    float val[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int c = bad ? 0 : code_of(v[k][j], scale, inv);
-      w |= (uint32_t)(c + 8) << (4 * j);
-      val[j] = (float)c * scale;
-    }
-    unsigned char* dst = p.q + row[k] * p.ldq + col[k] / 2;
-    const int n = (int)min((int64_t)8, p.cols - col[k]);
+    uint32_t w = BF16 ? codes_of_bf16(x, scale, inv, val) : codes_of(x, scale, inv, val);
+    unsigned char* dst = p.q + row * p.ldq + col / 2;
+    const int n = min(8, (int)((uint32_t)p.cols - col));
     if (n < 8) w &= (1u << (4 * n)) - 1u;
     if (n == 8 && p.q_whole) {
       *reinterpret_cast<uint32_t*>(dst) = w;
@@ -118,13 +152,14 @@ __global__ void __launch_bounds__(kQThreads) int4_quantize_kernel(QuantParams p)
         if (2 * j < n) dst[j] = (unsigned char)(w >> (8 * j));
     }
     if (Vv) {
-      InT* out = Vv + row[k] * p.ldv + col[k];
+      InT* out = Vv + row * p.ldv + col;
       if (n == 8 && p.v_whole) {
-        Store<InT, 8>::run(out, 0u, val);
+        Store<InT, 8>::run(out, 0u, reinterpret_cast<const float*>(val));
       } else {
+        const float* one = reinterpret_cast<const float*>(val);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (j < n) out[j] = from_f32<InT>(val[j]);
+          if (j < n) out[j] = from_f32<InT>(one[j]);
       }
     }
   }
