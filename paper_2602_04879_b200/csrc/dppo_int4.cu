@@ -24,17 +24,24 @@ struct QuantParams {
   void* values;              // in the type of x, or null
   int64_t ldv;
   int32_t* status;
-  int64_t slots;             // pieces of 8 columns of a row, a whole number of groups
+  int64_t slots;             // pairs of pieces of 8 columns of a row, a whole number of groups
+  int step_rows, step_slots; // kQThreads pairs further on
   int x_whole, q_whole, v_whole;   // 16-byte loads, 4-byte stores, 16-byte stores of values allowed
 };
 
-constexpr int kQThreads = 256, kQItems = 4;
+constexpr int kQThreads = 256, kQItems = 2;
 
-// amax / 7 rounded to bf16 once: the quotient is rounded towards zero with what was lost kept in the last bit
+// amax / 7 rounded to bf16 once, ties to even: the bf16 number below an approximate quotient (it may be one off where the quotient is next to a bf16
+// number, which the choice between it and the next one makes good), and the sign of amax - 7 (the middle above it), which one fma gives exactly
 __device__ __forceinline__ float group_scale(float amax) {
-  float t = __fdiv_rz(amax, 7.f);
-  if (fmaf(t, 7.f, -amax) != 0.f) t = __uint_as_float(__float_as_uint(t) | 1u);
-  return __bfloat162float(__float2bfloat16_rn(t));
+  const uint32_t below = __float_as_uint(amax * 0.14285715f) & 0xffff0000u;
+  const float d = fmaf(-7.f, __uint_as_float(below | 0x8000u), amax);
+  return __uint_as_float(below + (d > 0.f || (d == 0.f && (below & 0x10000u)) ? 0x10000u : 0u));
+}
+__device__ __forceinline__ float about_one_over(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
 }
 
 // round(|x| / scale) to nearest, ties to even: the quotient's floor from an approximate reciprocal (it may be one off next to a whole
@@ -77,91 +84,109 @@ __device__ __forceinline__ uint32_t codes_of_bf16(const float2* x, float scale, 
   return w;
 }
 
-// A thread has pieces of 8 columns, all of them loaded before the first is used; a group's G / 8 pieces lie in neighbouring lanes.
+// A thread has pairs of pieces of 8 columns of a group, G / 2 columns apart, all of them loaded before the first is used; a group's G / 16 pairs lie in
+// neighbouring lanes, whose loads are whole sectors.
 template <typename InT, int G>
 __global__ void __launch_bounds__(kQThreads) int4_quantize_kernel(QuantParams p) {
-  constexpr int LANES = G / 8, WORDS = sizeof(InT) == 2 ? 1 : 2;           // 16-byte words of a piece
   constexpr bool BF16 = sizeof(InT) == 2;
+  constexpr int LANES = G / 16, WORDS = BF16 ? 1 : 2;      // 16-byte words of a piece
   const InT* X = reinterpret_cast<const InT*>(p.x);
   InT* Vv = reinterpret_cast<InT*>(p.values);
-  const uint32_t slots = (uint32_t)p.slots;
+  const uint32_t slots = (uint32_t)p.slots, cols = (uint32_t)p.cols;
   const int64_t first = (int64_t)blockIdx.x * (kQThreads * kQItems);
-  const int64_t row0 = first / slots;
-  const uint32_t slot0 = (uint32_t)(first - row0 * slots) + threadIdx.x;
-  uint4 raw[kQItems][WORDS];
+  int64_t row0 = first / slots;
+  const uint32_t at0 = (uint32_t)(first - row0 * slots) + threadIdx.x, r0 = at0 / slots;
+  row0 += r0;
+  const uint32_t slot0 = at0 - r0 * slots;
+  uint4 raw[kQItems][2][WORDS];
+  {
+    int64_t row = row0;
+    uint32_t slot = slot0;
 #pragma unroll
-  for (int k = 0; k < kQItems; ++k) {
-    const uint32_t at = slot0 + k * kQThreads, r = at / slots;
-    const int64_t row = row0 + r;
-    const uint32_t col = (at - r * slots) * 8;
+    for (int k = 0; k < kQItems; ++k) {
 #pragma unroll
-    for (int u = 0; u < WORDS; ++u) raw[k][u] = make_uint4(0u, 0u, 0u, 0u);
-    if (row < p.rows) {
-      const InT* src = X + row * p.ldx + col;
-      if (p.x_whole && col + 8 <= p.cols) {
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t col = slot / LANES * G + slot % LANES * 8 + h * (G / 2);
 #pragma unroll
-        for (int u = 0; u < WORDS; ++u) raw[k][u] = ldg128_stream(src + u * 4);
-      } else {
+        for (int u = 0; u < WORDS; ++u) raw[k][h][u] = make_uint4(0u, 0u, 0u, 0u);
+        if (row < p.rows) {
+          const InT* src = X + row * p.ldx + col;
+          if (p.x_whole && col + 8 <= cols) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (col + j < p.cols) set_raw(raw[k][BF16 ? 0 : j / 4], BF16 ? j : j % 4, src[j]);
+            for (int u = 0; u < WORDS; ++u) raw[k][h][u] = ldg128_stream(src + u * 4);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (col + j < cols) set_raw(raw[k][h][BF16 ? 0 : j / 4], BF16 ? j : j % 4, src[j]);
+          }
+        }
       }
+      row += p.step_rows;
+      slot += p.step_slots;
+      if (slot >= slots) { slot -= slots; ++row; }
     }
   }
+  int64_t row = row0;
+  uint32_t slot = slot0;
 #pragma unroll
   for (int k = 0; k < kQItems; ++k) {
     RawMax<InT> most;
     most.m = {};
 #pragma unroll
-    for (int u = 0; u < WORDS; ++u) {
-      constexpr uint32_t MAGNITUDE = BF16 ? 0x7fff7fffu : 0x7fffffffu;
-      const uint4& v = raw[k][u];
-      most.add(make_uint4(v.x & MAGNITUDE, v.y & MAGNITUDE, v.z & MAGNITUDE, v.w & MAGNITUDE));
-    }
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int u = 0; u < WORDS; ++u) {
+        constexpr uint32_t MAGNITUDE = BF16 ? 0x7fff7fffu : 0x7fffffffu;
+        const uint4& v = raw[k][h][u];
+        most.add(make_uint4(v.x & MAGNITUDE, v.y & MAGNITUDE, v.z & MAGNITUDE, v.w & MAGNITUDE));
+      }
     float amax = most.value();
 #pragma unroll
     for (int o = LANES / 2; o > 0; o >>= 1) amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-    const uint32_t at = slot0 + k * kQThreads, r = at / slots;
-    const int64_t row = row0 + r;
-    const uint32_t col = (at - r * slots) * 8;
-    if (row >= p.rows || col >= p.cols) continue;          // (a piece of the last group may lie behind the row)
-    const bool bad = !(amax <= 3.4028234e38f);
-    float scale = group_scale(fmaxf(amax, 7.888609052210118e-31f)), inv = __frcp_rn(scale);
-    float2 x[4], val[4];
-#pragma unroll
-    for (int u = 0; u < WORDS; ++u) to_pairs<InT>(raw[k][u], x + 2 * u);
-    if (bad) {
-      scale = NAN;
-      inv = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = make_float2(0.f, 0.f);
-    }
-    if ((threadIdx.x & (LANES - 1)) == 0) {
-      p.scale[row * p.lds + col / G] = __float2bfloat16_rn(scale);
-      if (bad) atomicOr(p.status, DPPO_STATUS_NONFINITE_ROW);
-    }
-    uint32_t w = BF16 ? codes_of_bf16(x, scale, inv, val) : codes_of(x, scale, inv, val);
-    unsigned char* dst = p.q + row * p.ldq + col / 2;
-    const int n = min(8, (int)((uint32_t)p.cols - col));
-    if (n < 8) w &= (1u << (4 * n)) - 1u;
-    if (n == 8 && p.q_whole) {
-      *reinterpret_cast<uint32_t*>(dst) = w;
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (2 * j < n) dst[j] = (unsigned char)(w >> (8 * j));
-    }
-    if (Vv) {
+    const uint32_t group = slot / LANES, col = group * G + slot % LANES * 8;
+    if (row < p.rows) {
+      const bool bad = !(amax <= 3.4028234e38f);
+      const float scale = bad ? NAN : group_scale(fmaxf(amax, 7.888609052210118e-31f)), inv = about_one_over(scale);
+      if (slot % LANES == 0) {
+        p.scale[row * p.lds + group] = __float2bfloat16_rn(scale);
+        if (bad) atomicOr(p.status, DPPO_STATUS_NONFINITE_ROW);
+      }
+      unsigned char* q = p.q + row * p.ldq + col / 2;
       InT* out = Vv + row * p.ldv + col;
-      if (n == 8 && p.v_whole) {
-        Store<InT, 8>::run(out, 0u, reinterpret_cast<const float*>(val));
-      } else {
-        const float* one = reinterpret_cast<const float*>(val);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (j < n) out[j] = from_f32<InT>(one[j]);
+      for (int h = 0; h < 2; ++h) {
+        const int n = min(8, (int)cols - (int)(col + h * (G / 2)));
+        if (n <= 0) break;                 // (a piece of the last group may lie behind the row)
+        float2 x[4], val[4];
+#pragma unroll
+        for (int u = 0; u < WORDS; ++u) to_pairs<InT>(raw[k][h][u], x + 2 * u);
+        uint32_t w = BF16 ? codes_of_bf16(x, scale, inv, val) : codes_of(x, scale, inv, val);
+        if (bad) w = 0x88888888u;
+        if (n < 8) w &= (1u << (4 * n)) - 1u;
+        unsigned char* dst = q + h * (G / 4);
+        if (n == 8 && p.q_whole) {
+          *reinterpret_cast<uint32_t*>(dst) = w;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (2 * j < n) dst[j] = (unsigned char)(w >> (8 * j));
+        }
+        if (Vv) {
+          InT* to = out + h * (G / 2);
+          if (n == 8 && p.v_whole) {
+            Store<InT, 8>::run(to, 0u, reinterpret_cast<const float*>(val));
+          } else {
+            const float* one = reinterpret_cast<const float*>(val);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (j < n) to[j] = from_f32<InT>(one[j]);
+          }
+        }
       }
     }
+    row += p.step_rows;
+    slot += p.step_slots;
+    if (slot >= slots) { slot -= slots; ++row; }
   }
 }
 
@@ -945,7 +970,9 @@ extern "C" int dppo_int4_quantize(const void* x, int64_t rows, int64_t cols, int
   QuantParams p = {};
   p.x = x; p.rows = rows; p.cols = cols; p.ldx = x_row_stride; p.q = q; p.ldq = q_row_stride; p.scale = reinterpret_cast<__nv_bfloat16*>(scale);
   p.lds = scale_row_stride; p.values = values; p.ldv = values_row_stride; p.status = status;
-  p.slots = groups * (group / 8);
+  p.slots = groups * (group / 16);
+  p.step_rows = (int)(kQThreads / p.slots);
+  p.step_slots = (int)(kQThreads % p.slots);
   p.x_whole = (uintptr_t)x % 16 == 0 && (rows == 1 || (x_row_stride * es) % 16 == 0);
   p.q_whole = (uintptr_t)q % 4 == 0 && (rows == 1 || q_row_stride % 4 == 0);
   p.v_whole = values && (uintptr_t)values % 16 == 0 && (rows == 1 || (values_row_stride * es) % 16 == 0);
