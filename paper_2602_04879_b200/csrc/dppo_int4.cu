@@ -588,7 +588,8 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
     const int wg = (warp - 1 - L - 4 * L) >> 2, e = S::E > 1 ? wg : 0, turn = TURNS > 1 ? wg : 0, half = S::SPLIT > 1 ? wg : 0, q = warp & 3, r = q * 32 + lane;
     const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16) + S::A + (I8 ? 0 : e * EN);
     const uint32_t sum_full = smem_u32(&bars->sum_full[turn]), sum_free = smem_u32(&bars->sum_free[turn]);
-    float* inbox = sums + (turn * S::E + e) * OWN * LANES + r;
+    constexpr int PIECE = OWN % 4 == 0 ? 4 : 2;      // rows of x sent together
+    float* inbox = sums + (turn * S::E + e) * OWN * LANES + r * PIECE;       // [OWN / PIECE][LANES][PIECE]
     if (turn == 0 && lane == 0)
       for (int i = 0; i < BUFS; ++i) mbar_arrive(ready0 + 8 * i);      // nothing to be read before a buffer's first use
     const int stride = TURNS * grid;       // between this set's tiles
@@ -630,13 +631,17 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
     int keep_rows = -1;
     auto complete = [&]() {
       if (CL == 1 || keep_rows < 0) return true;
-      if (!__all_sync(0xffffffffu, mbar_wait_cluster(sum_full, (n_tile - 1u) & 1u, wc))) return false;
+      if (!mbar_wait_warp(sum_full, (n_tile - 1u) & 1u, wc)) return false;
 #pragma unroll
-      for (int j = 0; j < (CL > 1 ? OWN : 0); ++j) keep[j] = rank == 0 ? keep[j] + inbox[j * LANES] : inbox[j * LANES] + keep[j];
-      __threadfence_block();
-      __syncwarp();
-      // (nothing but what was read is behind this arrival; a release would wait for the stores to y)
-      if (lane == 0) asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(map_to_cta(sum_free, (uint32_t)(rank ^ 1))) : "memory");
+      for (int j = 0; j < (CL > 1 ? OWN : 0); j += PIECE) {
+        const float* in = inbox + j * LANES;
+#pragma unroll
+        for (int i = 0; i < PIECE; ++i) keep[j + i] += in[i];
+      }
+      // Nothing but what was read is behind this arrival: a release would wait for the stores to y, a fence for loads under way.  The vote's answer does
+      // not matter; it has the arrival wait for what was read.
+      if ((!__any_sync(0xffffffffu, keep[0] + keep[CL > 1 ? OWN - 1 : 0] == 1.f) || p.M > 0) && lane == 0)
+        asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(map_to_cta(sum_free, (uint32_t)(rank ^ 1))) : "memory");
       if (keep_at) {
         char* at = keep_at;
 #pragma unroll
@@ -782,15 +787,26 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
       } else {
         // The other's rows of x go over there, once it has read what went before: asynchronous stores, which count on the barrier there themselves
         // (an arrival that releases ordinary ones takes some 3000 cycles, the stores to y before it among them).
-        if (n_tile > 0 && !__all_sync(0xffffffffu, mbar_wait_cluster(sum_free, (n_tile - 1u) & 1u, wc))) { ok = false; break; }
+        if (n_tile > 0 && !mbar_wait_warp(sum_free, (n_tile - 1u) & 1u, wc)) { ok = false; break; }
         const uint32_t dst = map_to_cta(smem_u32(inbox), (uint32_t)(rank ^ 1)), bar = map_to_cta(sum_full, (uint32_t)(rank ^ 1));
         if (e == 0 && q == 0 && lane == 0) mbar_arrive_expect_tx(sum_full, S::E * OWN * LANES * 4);
+        const float* a = reinterpret_cast<const float*>(acc);
+        float out[OWN];
 #pragma unroll
-        for (int j = 0; j < OWN; ++j) {
-          const float lo = (j & 1) ? acc[j / 2].y : acc[j / 2].x, hi = ((OWN + j) & 1) ? acc[(OWN + j) / 2 % (EN / 2)].y : acc[(OWN + j) / 2 % (EN / 2)].x;
-          keep[CL > 1 ? j : 0] = rank == 0 ? lo : hi;
-          asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];"
-                       ::"r"(dst + (uint32_t)(j * LANES * 4)), "r"(__float_as_uint(rank == 0 ? hi : lo)), "r"(bar) : "memory");
+        for (int j = 0; j < (CL > 1 ? OWN : 0); ++j) {
+          const float lo = a[j], hi = a[(OWN + j) % EN];
+          keep[j] = rank == 0 ? lo : hi;
+          out[j] = rank == 0 ? hi : lo;
+        }
+#pragma unroll
+        for (int j = 0; j < OWN; j += PIECE) {
+          if (PIECE == 4)
+            asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
+                         ::"r"(dst + (uint32_t)(j * LANES * 4)), "r"(__float_as_uint(out[j])), "r"(__float_as_uint(out[j + 1])), "r"(__float_as_uint(out[(j + 2) % OWN])),
+                           "r"(__float_as_uint(out[(j + 3) % OWN])), "r"(bar) : "memory");
+          else
+            asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%1, %2}, [%3];"
+                         ::"r"(dst + (uint32_t)(j * LANES * 4)), "r"(__float_as_uint(out[j])), "r"(__float_as_uint(out[j + 1])), "r"(bar) : "memory");
         }
         keep_rows = max(0, min(p.M - m0 - rank * OWN, OWN));
         keep_at = live ? y_at(n, m0 + rank * OWN) : nullptr;
