@@ -262,7 +262,7 @@ template <int NT, int G, bool I8> struct Shape {
   static constexpr int NG = CHUNK / G;
   // Warpgroups for the products.  bf16: 16 rows of x each, and of a single one's tiles two take turns, so that one stores while the other adds
   // up.  int8: two, each half of a chunk's groups, whose sums meet at the tile's end.
-  static constexpr int E = I8 ? 1 : NT / 16, EN = XROWS / E, SPLIT = I8 ? 2 : 1, TURNS = !I8 && E == 1 ? 2 : 1;
+  static constexpr int E = NT <= 32 ? 1 : NT / 32, EN = XROWS / E, SPLIT = I8 ? 2 : 1, TURNS = I8 ? 1 : 2;
   static constexpr int PRODUCTS = E * SPLIT * TURNS, READERS = E * SPLIT;      // in all; of a chunk
   static constexpr int A = 64, D = NG * NT, COLS = A + D;              // columns of tensor memory of a chunk: operand, products
   static constexpr int L = !I8 && NT == 16 ? (COLS * 6 <= 512 ? 3 : 4) : 2;
@@ -454,7 +454,7 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
     for (int i = 0; i < 6; ++i) { mbar_init(ready0 + 8 * i, 4 + 4 * S::READERS); mbar_init(done0 + 8 * i, 1); }
     mbar_init(x_free, L * 4);
     mbar_init(x_full, L * 4);
-    for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&bars->turn[i]), 4);
+    for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&bars->turn[i]), 4 * S::E);
     for (int i = 0; i < TURNS; ++i) { mbar_init(smem_u32(&bars->sum_full[i]), 1); mbar_init(smem_u32(&bars->sum_free[i]), 4 * S::E); }
     bars->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -585,7 +585,7 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
     }
   } else {
     // ------------------------------------------------------------------ products
-    const int wg = (warp - 1 - L - 4 * L) >> 2, e = S::E > 1 ? wg : 0, turn = TURNS > 1 ? wg : 0, half = S::SPLIT > 1 ? wg : 0, q = warp & 3, r = q * 32 + lane;
+    const int wg = (warp - 1 - L - 4 * L) >> 2, e = TURNS > 1 ? wg % S::E : 0, turn = TURNS > 1 ? wg / S::E : 0, half = S::SPLIT > 1 ? wg : 0, q = warp & 3, r = q * 32 + lane;
     const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16) + S::A + (I8 ? 0 : e * EN);
     const uint32_t sum_full = smem_u32(&bars->sum_full[turn]), sum_free = smem_u32(&bars->sum_free[turn]);
     constexpr int PIECE = OWN % 4 == 0 ? 4 : 2;      // rows of x sent together
@@ -625,35 +625,6 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
     const unsigned short* srow = scales_of(tn, tile < tiles);
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) fetch(srow, u, sc[u]);
-    // pairs of CTAs: this CTA's rows of x of the tile before wait for the other's sums
-    float keep[CL > 1 ? OWN : 1];
-    char* keep_at = nullptr;
-    int keep_rows = -1;
-    auto complete = [&]() {
-      if (CL == 1 || keep_rows < 0) return true;
-      if (!mbar_wait_warp(sum_full, (n_tile - 1u) & 1u, wc)) return false;
-#pragma unroll
-      for (int j = 0; j < (CL > 1 ? OWN : 0); j += PIECE) {
-        const float* in = inbox + j * LANES;
-#pragma unroll
-        for (int i = 0; i < PIECE; ++i) keep[j + i] += in[i];
-      }
-      // Nothing but what was read is behind this arrival: a release would wait for the stores to y, a fence for loads under way.  The vote's answer does
-      // not matter; it has the arrival wait for what was read.
-      if ((!__any_sync(0xffffffffu, keep[0] + keep[CL > 1 ? OWN - 1 : 0] == 1.f) || p.M > 0) && lane == 0)
-        asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(map_to_cta(sum_free, (uint32_t)(rank ^ 1))) : "memory");
-      if (keep_at) {
-        char* at = keep_at;
-#pragma unroll
-        for (int j = 0; j < (CL > 1 ? OWN : 0); ++j) {
-          if (j >= keep_rows) break;
-          put(at, keep[j]);
-          at += ystep;
-        }
-      }
-      keep_rows = -1;
-      return true;
-    };
     for (int k = turn; tile < tiles && ok; tile += stride, k += TURNS) {       // k: this CTA's tiles
       // the tile's first chunk: its line, and how often the line's buffers have been used
       const uint32_t i0 = (uint32_t)k * (uint32_t)per_tile;
@@ -743,7 +714,6 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
             }
           }
         }
-        if (ok && c0 == 0 && half == 0) ok = complete();
       }
       if (!ok) break;
       if (TURNS > 1) {
@@ -772,30 +742,23 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
         __syncwarp();
         if (lane == 0) mbar_arrive(read);
       }
-      if (!complete()) { ok = false; break; }
+      const float* a = reinterpret_cast<const float*>(acc);
+      float sum[OWN];
+      int m_own = m0;
       if (CL == 1) {
-        if (live) {
-          char* at = y_at(n, m0);
-          const int rows = p.M - m0;
 #pragma unroll
-          for (int j = 0; j < EN; ++j) {
-            if (j >= rows) break;
-            put(at, (j & 1) ? acc[j / 2].y : acc[j / 2].x);
-            at += ystep;
-          }
-        }
+        for (int j = 0; j < OWN; ++j) sum[j] = a[j];
       } else {
         // The other's rows of x go over there, once it has read what went before: asynchronous stores, which count on the barrier there themselves
         // (an arrival that releases ordinary ones takes some 3000 cycles, the stores to y before it among them).
         if (n_tile > 0 && !mbar_wait_warp(sum_free, (n_tile - 1u) & 1u, wc)) { ok = false; break; }
         const uint32_t dst = map_to_cta(smem_u32(inbox), (uint32_t)(rank ^ 1)), bar = map_to_cta(sum_full, (uint32_t)(rank ^ 1));
         if (e == 0 && q == 0 && lane == 0) mbar_arrive_expect_tx(sum_full, S::E * OWN * LANES * 4);
-        const float* a = reinterpret_cast<const float*>(acc);
         float out[OWN];
 #pragma unroll
-        for (int j = 0; j < (CL > 1 ? OWN : 0); ++j) {
+        for (int j = 0; j < OWN; ++j) {
           const float lo = a[j], hi = a[(OWN + j) % EN];
-          keep[j] = rank == 0 ? lo : hi;
+          sum[j] = rank == 0 ? lo : hi;
           out[j] = rank == 0 ? hi : lo;
         }
 #pragma unroll
@@ -808,13 +771,30 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
             asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%1, %2}, [%3];"
                          ::"r"(dst + (uint32_t)(j * LANES * 4)), "r"(__float_as_uint(out[j])), "r"(__float_as_uint(out[j + 1])), "r"(bar) : "memory");
         }
-        keep_rows = max(0, min(p.M - m0 - rank * OWN, OWN));
-        keep_at = live ? y_at(n, m0 + rank * OWN) : nullptr;
+        if (!mbar_wait_warp(sum_full, n_tile & 1u, wc)) { ok = false; break; }
+#pragma unroll
+        for (int j = 0; j < OWN; j += PIECE)
+#pragma unroll
+          for (int i = 0; i < PIECE; ++i) sum[j + i] += inbox[j * LANES + i];
+        // Nothing but what was read is behind this arrival: a release would wait for the stores to y, a fence for loads under way.  The vote's answer does
+        // not matter; it has the arrival wait for what was read.
+        if ((!__any_sync(0xffffffffu, sum[0] + sum[OWN - 1] == 1.f) || p.M > 0) && lane == 0)
+          asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(map_to_cta(sum_free, (uint32_t)(rank ^ 1))) : "memory");
+        m_own = m0 + rank * OWN;
+      }
+      if (live) {
+        char* at = y_at(n, m_own);
+        const int rows = p.M - m_own;
+#pragma unroll
+        for (int j = 0; j < OWN; ++j) {
+          if (j >= rows) break;
+          put(at, sum[j]);
+          at += ystep;
+        }
       }
       srow = srow_next;
       ++n_tile;
     }
-    if (ok && half == 0) complete();
   }
   __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
