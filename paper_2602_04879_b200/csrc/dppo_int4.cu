@@ -262,7 +262,7 @@ template <int NT, int G, bool I8> struct Shape {
   static constexpr int NG = CHUNK / G;
   // Warpgroups for the products.  bf16: 16 rows of x each, and of a single one's tiles two take turns, so that one stores while the other adds
   // up.  int8: two, each half of a chunk's groups, whose sums meet at the tile's end.
-  static constexpr int E = NT <= 32 ? 1 : NT / 32, EN = XROWS / E, SPLIT = I8 ? 2 : 1, TURNS = I8 ? 1 : 2;
+  static constexpr int E = NT == 16 ? 1 : 2, EN = XROWS / E, SPLIT = I8 ? 2 : 1, TURNS = I8 || NT == 32 ? 1 : 2;
   static constexpr int PRODUCTS = E * SPLIT * TURNS, READERS = E * SPLIT;      // in all; of a chunk
   static constexpr int A = 64, D = NG * NT, COLS = A + D;              // columns of tensor memory of a chunk: operand, products
   static constexpr int L = !I8 && NT == 16 ? (COLS * 6 <= 512 ? 3 : 4) : 2;
@@ -276,6 +276,15 @@ __device__ __forceinline__ uint32_t elect_one() {
   uint32_t p;
   asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
   return p;
+}
+// Whether a phase is over, asked ahead of the wait for it, so that the answer comes while something else is done.
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ bool mbar_wait_warp(bool over, uint32_t bar, uint32_t parity, const WaitCtl& w) {
+  return __all_sync(0xffffffffu, over) || dppo::mbar_wait_warp(bar, parity, w);
 }
 // A from tensor memory
 template <bool I8> __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
@@ -346,15 +355,15 @@ template <bool I8> __device__ __forceinline__ void convert_half(const uint4* w, 
 
 // bf16: x rows m0 .. m0 + NT - 1, codes k0 .. k0 + seg - 1 of K, into shared memory: blocks of 64 codes, NT rows of 128 bytes each, 128-byte
 // swizzle, and within 8 codes the order that the conversion makes of them.  Rows and codes that there are not are zero.
-template <int NT, int T>
-__device__ __forceinline__ void load_x(const Params& p, unsigned char* xs, int m0, int k0, int tid) {
-  constexpr int AT_ONCE = 4;               // loads in flight
-  const int octets = p.seg / 8, all = NT * octets;
-  for (int i0 = tid; i0 < all; i0 += AT_ONCE * T) {
+template <int NT, int WARPS>
+__device__ __forceinline__ void load_x(const Params& p, unsigned char* xs, int m0, int k0, int warp, int lane) {
+  constexpr int AT_ONCE = 8;               // loads in flight
+  const int blocks = p.seg / 256, all = NT * blocks;       // a warp takes 256 codes of a row, 8 to a lane
+  for (int i0 = warp; i0 < all; i0 += AT_ONCE * WARPS) {
     uint4 v[AT_ONCE];
 #pragma unroll
     for (int u = 0; u < AT_ONCE; ++u) {
-      const int i = i0 + u * T, m = i / octets, o = i - m * octets, k = k0 + 8 * o;
+      const int i = i0 + u * WARPS, m = i / blocks, k = k0 + (i - m * blocks) * 256 + 8 * lane;
       v[u] = make_uint4(0u, 0u, 0u, 0u);
       if (i < all && m0 + m < p.M && k < p.K) {
         const __nv_bfloat16* src = p.x + (int64_t)(m0 + m) * p.ldx + k;
@@ -371,7 +380,7 @@ __device__ __forceinline__ void load_x(const Params& p, unsigned char* xs, int m
     }
 #pragma unroll
     for (int u = 0; u < AT_ONCE; ++u) {
-      const int i = i0 + u * T, m = i / octets, o = i - m * octets;
+      const int i = i0 + u * WARPS, m = i / blocks, o = (i - m * blocks) * 32 + lane;
       if (i >= all) break;
       const int at = (o / 8) * (NT * 128) + m * 128 + ((16 * (o % 8)) ^ ((m & 7) << 4));
       // (0, 4), (1, 5), (2, 6), (3, 7)
@@ -549,7 +558,7 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
           if (!mbar_wait_warp(x_free, n_x & 1u, wc)) { ok = false; break; }
           const int k0 = (pair0 + seg * (p.seg / 256)) * 256;
           if (I8) load_x_digits<NT, XROWS, G, L * 4>(p, xs, table, block * XROWS, k0, warp - 1 - L, lane);
-          else load_x<NT, L * 128>(p, xs, block * XROWS, k0, tid - 32 - 32 * L);
+          else load_x<NT, L * 4>(p, xs, block * XROWS, k0, warp - 1 - L, lane);
           __syncwarp();
           if (lane == 0) mbar_arrive(x_full);
           if (!mbar_wait_warp(x_full, n_x & 1u, wc)) { ok = false; break; }
@@ -557,17 +566,22 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
           x_now = x_want;
         }
       }
+      bool over = false;
       for (; i < end; i += L) {
         const int s = at / PER, b = line * B + sub;
-        if (!mbar_wait_warp(full0 + 8 * s, ph, wc)) { ok = false; break; }
+        if (!mbar_wait_warp(over, full0 + 8 * s, ph, wc)) { ok = false; break; }
         const uint32_t src = smem_u32(smem) + s * STAGE_BYTES + r * 128;
         constexpr int PIECES = S::CHUNK / 32;              // of 16 bytes
         uint4 w[PIECES];
 #pragma unroll
         for (int j = 0; j < PIECES; ++j) w[j] = lds128(src + ((((at % PER) * PIECES + j) ^ (r & 7)) << 4));
+        const bool used = mbar_test(done0 + 8 * b, bph ^ 1u);
+        at += L;
+        if (at >= PER * p.stages) { at -= PER * p.stages; ph ^= 1u; }
+        over = mbar_test(full0 + 8 * (at / PER), ph);
         uint32_t v[32];
         convert_half<I8>(w, v);
-        if (!mbar_wait_warp(done0 + 8 * b, bph ^ 1u, wc)) { ok = false; break; }       // the buffer's operand before has been used
+        if (!mbar_wait_warp(used, done0 + 8 * b, bph ^ 1u, wc)) { ok = false; break; }       // the buffer's operand before has been used
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         tmem_st32(lane_base + b * COLS, v);
         convert_half<I8>(w + PIECES / 2, v);
@@ -578,14 +592,12 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
         // The stage is given back here, where its codes have been used: with the arrival right behind the loads, before the wait above, codes of
         // the stage's next content turned up among these.
         if (lane == 0) { mbar_arrive(ready0 + 8 * b); mbar_arrive(empty0 + 8 * s); }
-        at += L;
-        if (at >= PER * p.stages) { at -= PER * p.stages; ph ^= 1u; }
         if (++sub == B) { sub = 0; bph ^= 1u; }
       }
     }
   } else {
     // ------------------------------------------------------------------ products
-    const int wg = (warp - 1 - L - 4 * L) >> 2, e = TURNS > 1 ? wg % S::E : 0, turn = TURNS > 1 ? wg / S::E : 0, half = S::SPLIT > 1 ? wg : 0, q = warp & 3, r = q * 32 + lane;
+    const int wg = (warp - 1 - L - 4 * L) >> 2, e = wg % S::E, turn = TURNS > 1 ? wg / S::E : 0, half = S::SPLIT > 1 ? wg : 0, q = warp & 3, r = q * 32 + lane;
     const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16) + S::A + (I8 ? 0 : e * EN);
     const uint32_t sum_full = smem_u32(&bars->sum_full[turn]), sum_free = smem_u32(&bars->sum_free[turn]);
     constexpr int PIECE = OWN % 4 == 0 ? 4 : 2;      // rows of x sent together
@@ -643,14 +655,21 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
       // Once the tile before has been read, by the other set: all uses of the buffers before this tile's are over then, as the parities want.
       if (TURNS > 1 && k > 0) ok = mbar_wait_warp(smem_u32(&bars->turn[turn]), (uint32_t)((k - 1) / 2) & 1u, wc);
       const int4* tab = table;             // int8: of the next chunk
+      bool over = false;                   // whether the next chunk's products are there
       for (int c0 = 0; c0 < per_tile && ok; c0 += AHEAD) {
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
           const int c = c0 + u;
           if (c < per_tile && ok) {
             const uint32_t b = (uint32_t)(line * B + sub), td = lane_base + b * COLS;
-            ok = mbar_wait_warp(done0 + 8 * b, ph, wc);
+            ok = mbar_wait_warp(over, done0 + 8 * b, ph, wc);
             if (ok) {
+              if (++line == L) {
+                line = 0;
+                if (++sub == B) { sub = 0; ph ^= 1u; }
+              }
+              // (64 rows: not worth the registers, 85 us against 90 for 61 x 151936 x 2048)
+              over = NT < 64 && c + 1 < per_tile && mbar_test(done0 + 8 * (uint32_t)(line * B + sub), ph);
               asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
               if (I8) {
                 float* a = reinterpret_cast<float*>(acc);
@@ -707,10 +726,6 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
               if (lane == 0) mbar_arrive(ready0 + 8 * b);
               if (c + AHEAD < per_tile) fetch(srow, c + AHEAD, sc[u]); else fetch(srow_next, u, sc[u]);
               if (I8) tab += NG * XROWS;
-              if (++line == L) {
-                line = 0;
-                if (++sub == B) { sub = 0; ph ^= 1u; }
-              }
             }
           }
         }
@@ -846,6 +861,8 @@ cudaError_t launch_cl(Params p, const unsigned char* q, int64_t ldq, int sms, in
   p.seg = (p.pairs + p.nseg - 1) / p.nseg * 256;
   p.stages = (room - p.seg / 256 * X256) / STAGE_BYTES;
   if (p.stages > 12) p.stages = 12;
+  // A stage's contents are all of one line: a line that waits for one has then seen the one before, as the parity of its phases wants.
+  while (p.stages * S::PER % S::L) --p.stages;
   // rows of a tile: rounds of tiles over the CTAs that are as full as they can be
   const int64_t ctas = sms / CL, rounds = (p.N + ctas * LANES - 1) / (ctas * LANES);
   p.rows = (int)((p.N + ctas * rounds - 1) / (ctas * rounds));
