@@ -263,7 +263,7 @@ template <int NT, int G, bool I8> struct Shape {
   // Warpgroups for the products.  bf16: 16 rows of x each, and of a single one's tiles two take turns, so that one stores while the other adds
   // up.  int8: two, each half of a chunk's groups, whose sums meet at the tile's end.
   static constexpr int E = NT == 16 ? 1 : 2, EN = XROWS / E, SPLIT = I8 ? 2 : 1, TURNS = I8 || NT == 32 ? 1 : 2;
-  static constexpr int PRODUCTS = E * SPLIT * TURNS, READERS = E * SPLIT;      // in all; of a chunk
+  static constexpr int PRODUCTS = E * SPLIT * TURNS;                // in all; E of a chunk
   static constexpr int A = 64, D = NG * NT, COLS = A + D;              // columns of tensor memory of a chunk: operand, products
   static constexpr int L = !I8 && NT == 16 ? (COLS * 6 <= 512 ? 3 : 4) : 2;
   static constexpr int B = COLS * 2 * L <= 512 ? 2 : 1;
@@ -460,7 +460,7 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
   const int rank = CL > 1 ? (int)cluster_ctarank() : 0;
   if (tid == 0) {
     for (int i = 0; i < 12; ++i) { mbar_init(full0 + 8 * i, 1); mbar_init(empty0 + 8 * i, 4 * PER); }
-    for (int i = 0; i < 6; ++i) { mbar_init(ready0 + 8 * i, 4 + 4 * S::READERS); mbar_init(done0 + 8 * i, 1); }
+    for (int i = 0; i < 6; ++i) { mbar_init(ready0 + 8 * i, 4 + 4 * S::E); mbar_init(done0 + 8 * i, 1); }
     mbar_init(x_free, L * 4);
     mbar_init(x_full, L * 4);
     for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&bars->turn[i]), 4 * S::E);
@@ -597,13 +597,14 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
     }
   } else {
     // ------------------------------------------------------------------ products
-    const int wg = (warp - 1 - L - 4 * L) >> 2, e = wg % S::E, turn = TURNS > 1 ? wg / S::E : 0, half = S::SPLIT > 1 ? wg : 0, q = warp & 3, r = q * 32 + lane;
+    constexpr int SPLIT = S::SPLIT;
+    const int wg = (warp - 1 - L - 4 * L) >> 2, e = wg % S::E, turn = TURNS > 1 ? wg / S::E : 0, half = SPLIT > 1 ? wg : 0, q = warp & 3, r = q * 32 + lane;
     const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16) + S::A + (I8 ? 0 : e * EN);
     const uint32_t sum_full = smem_u32(&bars->sum_full[turn]), sum_free = smem_u32(&bars->sum_free[turn]);
     constexpr int PIECE = OWN % 4 == 0 ? 4 : 2;      // rows of x sent together
     float* inbox = sums + (turn * S::E + e) * OWN * LANES + r * PIECE;       // [OWN / PIECE][LANES][PIECE]
     if (turn == 0 && lane == 0)
-      for (int i = 0; i < BUFS; ++i) mbar_arrive(ready0 + 8 * i);      // nothing to be read before a buffer's first use
+      for (int i = half * B; i < (SPLIT > 1 ? (half + 1) * B : BUFS); ++i) mbar_arrive(ready0 + 8 * i);      // nothing to be read before a buffer's first use
     const int stride = TURNS * grid;       // between this set's tiles
     uint32_t n_tile = 0;
     bool ok = true;
@@ -623,12 +624,11 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
       return there && r < p.rows && n < p.N ? reinterpret_cast<const unsigned short*>(p.scale) + (int64_t)n * p.lds + g0 : nullptr;
     };
     // (a register each, and the loads by predicate: nothing here may wait for them)
-    constexpr int OWN_G = NG / S::SPLIT;
-    uint32_t sc[AHEAD][OWN_G];
+    uint32_t sc[AHEAD][NG];
     auto fetch = [&](const unsigned short* row, int c, uint32_t* to) {
 #pragma unroll
-      for (int h = 0; h < OWN_G; ++h) {
-        const int gi = c * NG + half * OWN_G + h;
+      for (int h = 0; h < NG; ++h) {
+        const int gi = c * NG + h;
         to[h] = 0u;
         asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %2, 0;\n @q ld.global.nc.u16 %0, [%1];\n}\n"
                      : "+r"(to[h]) : "l"(row + gi), "r"((int)(row && gi < glim)));
@@ -636,12 +636,14 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
     };
     const unsigned short* srow = scales_of(tn, tile < tiles);
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) fetch(srow, u, sc[u]);
+    for (int u = 0; u < AHEAD; ++u) fetch(srow, (SPLIT > 1 ? half : 0) + u * SPLIT, sc[u]);
     for (int k = turn; tile < tiles && ok; tile += stride, k += TURNS) {       // k: this CTA's tiles
       // the tile's first chunk: its line, and how often the line's buffers have been used
       const uint32_t i0 = (uint32_t)k * (uint32_t)per_tile;
-      int line = (int)(i0 % L), sub = (int)(i0 / L % B);
-      uint32_t ph = i0 / (L * B) & 1u;
+      // (halves: the second half of the line's number of chunks from the tile's first on, and the same of the next tile)
+      const int begin = SPLIT > 1 ? half ^ (int)(i0 & 1u) : 0, begin_next = SPLIT > 1 ? half ^ (int)((i0 + (uint32_t)per_tile) & 1u) : 0;
+      int line = SPLIT > 1 ? half : (int)(i0 % L), sub = (int)((i0 + begin) / L % B);
+      uint32_t ph = (i0 + begin) / (L * B) & 1u;
       const int n = tn * p.rows + r, m0 = block * XROWS + e * EN;
       const bool live = srow != nullptr;
       tn += stride;
@@ -654,22 +656,24 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
       for (int j = 0; j < EN / 2; ++j) acc[j] = make_float2(0.f, 0.f);
       // Once the tile before has been read, by the other set: all uses of the buffers before this tile's are over then, as the parities want.
       if (TURNS > 1 && k > 0) ok = mbar_wait_warp(smem_u32(&bars->turn[turn]), (uint32_t)((k - 1) / 2) & 1u, wc);
-      const int4* tab = table;             // int8: of the next chunk
+      const int4* tab = table + begin * (NG * XROWS);        // int8: of the next chunk
       bool over = false;                   // whether the next chunk's products are there
-      for (int c0 = 0; c0 < per_tile && ok; c0 += AHEAD) {
+      for (int c0 = begin; (c0 == begin || c0 < per_tile) && ok; c0 += AHEAD * SPLIT) {
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-          const int c = c0 + u;
-          if (c < per_tile && ok) {
+          const int c = c0 + u * SPLIT;
+          if (c >= per_tile) {
+            if (c0 == begin) fetch(srow_next, begin_next + u * SPLIT, sc[u]);
+          } else if (ok) {
             const uint32_t b = (uint32_t)(line * B + sub), td = lane_base + b * COLS;
             ok = mbar_wait_warp(over, done0 + 8 * b, ph, wc);
             if (ok) {
-              if (++line == L) {
-                line = 0;
+              if (SPLIT > 1 || ++line == L) {
+                if (SPLIT == 1) line = 0;
                 if (++sub == B) { sub = 0; ph ^= 1u; }
               }
               // (64 rows: not worth the registers, 85 us against 90 for 61 x 151936 x 2048)
-              over = NT < 64 && c + 1 < per_tile && mbar_test(done0 + 8 * (uint32_t)(line * B + sub), ph);
+              over = NT < 64 && c + SPLIT < per_tile && mbar_test(done0 + 8 * (uint32_t)(line * B + sub), ph);
               asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
               if (I8) {
                 float* a = reinterpret_cast<float*>(acc);
@@ -679,28 +683,27 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
                   const float d2 = __int_as_float((int)v[2] + t.z) - 12582912.f;
                   a[m] = fmaf(s1 * __int_as_float(t.w), fmaf(d2, 65536.f, fmaf(d1, 256.f, d0)), a[m]);
                 };
-                const int h0 = half * OWN_G;
                 if (p.M == 1) {            // a single row: its digits only
-                  uint32_t v[OWN_G][4];
+                  uint32_t v[NG][4];
 #pragma unroll
-                  for (int h = 0; h < OWN_G; ++h) tmem_ld4(td + (h0 + h) * NT, v[h]);
-                  tmem_ld_wait<OWN_G * 4>(v[0]);
+                  for (int h = 0; h < NG; ++h) tmem_ld4(td + h * NT, v[h]);
+                  tmem_ld_wait<NG * 4>(v[0]);
 #pragma unroll
-                  for (int h = 0; h < OWN_G; ++h) add(v[h], 0, __uint_as_float(sc[u][h] << 16), tab[(h0 + h) * XROWS]);
+                  for (int h = 0; h < NG; ++h) add(v[h], 0, __uint_as_float(sc[u][h] << 16), tab[h * XROWS]);
                 } else {
-                  constexpr int AT = OWN_G < 2 ? OWN_G : 2;      // groups read together
+                  constexpr int AT = NG < 2 ? NG : 2;      // groups read together
 #pragma unroll
-                  for (int h1 = 0; h1 < OWN_G; h1 += AT) {
+                  for (int h1 = 0; h1 < NG; h1 += AT) {
                     uint32_t v[AT][16];
 #pragma unroll
-                    for (int h = 0; h < AT; ++h) tmem_ld16(td + (h0 + h1 + h) * NT, v[h]);
+                    for (int h = 0; h < AT; ++h) tmem_ld16(td + (h1 + h) * NT, v[h]);
                     tmem_ld_wait<AT * 16>(v[0]);
 #pragma unroll
                     for (int h = 0; h < AT; ++h)
 #pragma unroll
                       for (int m = 0; m < XROWS; ++m) {
                         if (m0 + m >= p.M) break;
-                        add(v[h] + 4 * m, m, __uint_as_float(sc[u][h1 + h] << 16), tab[(h0 + h1 + h) * XROWS + m]);
+                        add(v[h] + 4 * m, m, __uint_as_float(sc[u][h1 + h] << 16), tab[(h1 + h) * XROWS + m]);
                       }
                   }
                 }
@@ -724,8 +727,8 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
               asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
               __syncwarp();
               if (lane == 0) mbar_arrive(ready0 + 8 * b);
-              if (c + AHEAD < per_tile) fetch(srow, c + AHEAD, sc[u]); else fetch(srow_next, u, sc[u]);
-              if (I8) tab += NG * XROWS;
+              if (c + AHEAD * SPLIT < per_tile) fetch(srow, c + AHEAD * SPLIT, sc[u]); else fetch(srow_next, begin_next + u * SPLIT, sc[u]);
+              if (I8) tab += SPLIT * NG * XROWS;
             }
           }
         }
@@ -735,7 +738,7 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bars->turn[turn ^ 1]));
       }
-      if (S::SPLIT > 1) {
+      if (SPLIT > 1) {
         // the halves' sums meet
         float* a = reinterpret_cast<float*>(acc);
         const uint32_t here = smem_u32(&bars->turn[0]), read = smem_u32(&bars->turn[1]);
