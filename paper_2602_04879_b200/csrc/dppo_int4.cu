@@ -262,7 +262,7 @@ template <int NT, int G, bool I8> struct Shape {
   static constexpr int NG = CHUNK / G;
   // Warpgroups for the products.  bf16: 16 rows of x each, and of a single one's tiles two take turns, so that one stores while the other adds
   // up.  int8: two, each half of a chunk's groups, whose sums meet at the tile's end.
-  static constexpr int E = NT == 16 ? 1 : 2, EN = XROWS / E, SPLIT = I8 ? 2 : 1, TURNS = I8 || NT == 32 ? 1 : 2;
+  static constexpr int E = I8 || NT == 16 ? 1 : 2, EN = XROWS / E, SPLIT = I8 ? 2 : 1, TURNS = I8 || NT == 32 ? 1 : 2;
   static constexpr int PRODUCTS = E * SPLIT * TURNS;                // in all; E of a chunk
   static constexpr int A = 64, D = NG * NT, COLS = A + D;              // columns of tensor memory of a chunk: operand, products
   static constexpr int L = !I8 && NT == 16 ? (COLS * 6 <= 512 ? 3 : 4) : 2;
@@ -396,38 +396,48 @@ __device__ __forceinline__ void load_x(const Params& p, unsigned char* xs, int m
 // entry that is no number, or infinite, makes the unit NaN.
 template <int NT, int XROWS, int G, int WARPS>
 __device__ __forceinline__ void load_x_digits(const Params& p, unsigned char* xs, int4* table, int m0, int k0, int warp, int lane) {
-  const int groups = p.seg / G;
-  for (int u = warp; u < groups * XROWS; u += WARPS) {
-    const int gi = u / XROWS, m = u - gi * XROWS, kg = gi * G;
-    float v[G / 32];
-    float top = 0.f;
+  constexpr int AT_ONCE = 4;
+  const int rows = min(XROWS, p.M - m0), all = p.seg / G * rows;           // (columns of rows that there are not are never read)
+  for (int u0 = warp; u0 < all; u0 += AT_ONCE * WARPS) {
+    float v[AT_ONCE][G / 32];
 #pragma unroll
-    for (int j = 0; j < G / 32; ++j) {
-      const int k = k0 + kg + 32 * j + lane;
-      v[j] = m0 + m < p.M && k < p.K ? __bfloat162float(p.x[(int64_t)(m0 + m) * p.ldx + k]) : 0.f;
-      top = max_nan(top, fabsf(v[j]));
-    }
-    top = warp_max_nan(top);
-    const bool bad = !(top <= 3.4028234e38f);
-    // unit 2^(e - 21) for a largest entry in [2^e, 2^(e + 1)); tiny groups in units of 2^-121
-    const int e = max((int)(__float_as_uint(top) >> 23) - 127, -100);
-    const float up = __uint_as_float((uint32_t)(127 + 21 - e) << 23), unit = bad ? NAN : __uint_as_float((uint32_t)(127 + e - 21) << 23);
-    int sum[DIGITS] = {};
+    for (int a = 0; a < AT_ONCE; ++a) {
+      const int u = u0 + a * WARPS, gi = u / rows, m = u - gi * rows;
 #pragma unroll
-    for (int j = 0; j < G / 32; ++j) {
-      int X = bad ? 0 : __float2int_rn(v[j] * up);
-      const int k = kg + 32 * j + lane, byte = (k & 127 & ~7) + ((k & 1) * 4 + ((k & 7) >> 1));
-#pragma unroll
-      for (int d = 0; d < DIGITS; ++d) {
-        const int digit = d == DIGITS - 1 ? X : ((X + 128) & 255) - 128, row = 4 * m + d;
-        X = (X - digit) >> 8;
-        sum[d] += digit;
-        xs[k / 128 * (NT * 128) + row * 128 + (byte ^ ((row & 7) << 4))] = (unsigned char)digit;
+      for (int j = 0; j < G / 32; ++j) {
+        const int k = k0 + gi * G + 32 * j + lane;
+        v[a][j] = u < all && k < p.K ? __bfloat162float(p.x[(int64_t)(m0 + m) * p.ldx + k]) : 0.f;
       }
     }
 #pragma unroll
-    for (int d = 0; d < DIGITS; ++d) sum[d] = __reduce_add_sync(0xffffffffu, sum[d]);
-    if (lane == 0) table[gi * XROWS + m] = make_int4(0x4B400000 - 8 * sum[0], 0x4B400000 - 8 * sum[1], 0x4B400000 - 8 * sum[2], (int)__float_as_uint(unit));
+    for (int a = 0; a < AT_ONCE; ++a) {
+      const int u = u0 + a * WARPS, gi = u / rows, m = u - gi * rows, kg = gi * G;
+      if (u >= all) break;
+      float top = 0.f;
+#pragma unroll
+      for (int j = 0; j < G / 32; ++j) top = max_nan(top, fabsf(v[a][j]));
+      top = warp_max_nan(top);
+      const bool bad = !(top <= 3.4028234e38f);
+      // unit 2^(e - 21) for a largest entry in [2^e, 2^(e + 1)); tiny groups in units of 2^-121
+      const int e = max((int)(__float_as_uint(top) >> 23) - 127, -100);
+      const float up = __uint_as_float((uint32_t)(127 + 21 - e) << 23), unit = bad ? NAN : __uint_as_float((uint32_t)(127 + e - 21) << 23);
+      int sum[DIGITS] = {};
+#pragma unroll
+      for (int j = 0; j < G / 32; ++j) {
+        int X = bad ? 0 : __float2int_rn(v[a][j] * up);
+        const int k = kg + 32 * j + lane, byte = (k & 127 & ~7) + ((k & 1) * 4 + ((k & 7) >> 1));
+#pragma unroll
+        for (int d = 0; d < DIGITS; ++d) {
+          const int digit = d == DIGITS - 1 ? X : ((X + 128) & 255) - 128, row = 4 * m + d;
+          X = (X - digit) >> 8;
+          sum[d] += digit;
+          xs[k / 128 * (NT * 128) + row * 128 + (byte ^ ((row & 7) << 4))] = (unsigned char)digit;
+        }
+      }
+#pragma unroll
+      for (int d = 0; d < DIGITS; ++d) sum[d] = __reduce_add_sync(0xffffffffu, sum[d]);
+      if (lane == 0) table[gi * XROWS + m] = make_int4(0x4B400000 - 8 * sum[0], 0x4B400000 - 8 * sum[1], 0x4B400000 - 8 * sum[2], (int)__float_as_uint(unit));
+    }
   }
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
@@ -906,12 +916,15 @@ cudaError_t launch(const Params& p, const unsigned char* q, int64_t ldq, int sms
   return launch_cl<NT, G, 2, I8>(p, q, ldq, sms, smem_most, st);
 }
 
-template <int NT, bool I8>
-cudaError_t launch_group(const Params& p, int group, const unsigned char* q, int64_t ldq, int sms, int smem_most, cudaStream_t st) {
-  if (group == 128) return launch<NT, 128, I8>(p, q, ldq, sms, smem_most, st);
-  if (group == 64) return launch<NT, 64, I8>(p, q, ldq, sms, smem_most, st);
-  if constexpr (NT < 64) return launch<NT, 32, I8>(p, q, ldq, sms, smem_most, st);
-  return cudaErrorInvalidValue;
+// Rows of x that one pass over the weights serves.  (Of 64 rows and groups of 32 the products would not fit tensor memory.)  Up to four rows as integers: a
+// tile's int8 MMAs take half as long and its conversion a third of the instructions; above that the products take more than is saved (8 rows
+// 69 us against 54, 16 rows 135 against 55, at 151936 x 2048).
+template <int G>
+cudaError_t launch_rows(const Params& p, const unsigned char* q, int64_t ldq, int sms, int smem_most, cudaStream_t st) {
+  if (p.M <= 4) return launch<16, G, true>(p, q, ldq, sms, smem_most, st);
+  if (p.M <= 16) return launch<16, G, false>(p, q, ldq, sms, smem_most, st);
+  if constexpr (G >= 64) if (p.M > 32) return launch<64, G, false>(p, q, ldq, sms, smem_most, st);
+  return launch<32, G, false>(p, q, ldq, sms, smem_most, st);
 }
 
 }  // namespace mv
@@ -1045,13 +1058,8 @@ extern "C" int dppo_matvec_int4(const void* x, int64_t x_row_stride, const uint8
     cudaGetDevice(&dev);
     cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev);
-    // Rows of x that one pass over the weights serves.  (Of 64 rows and groups of 32 the products would not fit tensor memory.)  Up to four rows as
-    // integers: the int8 MMAs of a tile take half as long, and above that its products take longer than the bf16 ones.
-    cudaError_t e;
-    if (M <= 4) e = mv::launch_group<16, true>(m, group, q, pitch, sms, most, st);
-    else if (M <= 16) e = mv::launch_group<16, false>(m, group, q, pitch, sms, most, st);
-    else if (M <= 32 || group == 32) e = mv::launch_group<32, false>(m, group, q, pitch, sms, most, st);
-    else e = mv::launch_group<64, false>(m, group, q, pitch, sms, most, st);
+    const cudaError_t e = group == 128 ? mv::launch_rows<128>(m, q, pitch, sms, most, st)
+                                       : (group == 64 ? mv::launch_rows<64>(m, q, pitch, sms, most, st) : mv::launch_rows<32>(m, q, pitch, sms, most, st));
     return e == cudaSuccess ? DPPO_OK : DPPO_ERR_CUDA;
   }
   const int64_t warps = N * ((M + kGRows - 1) / kGRows), grid = (warps + kGThreads / 32 - 1) / (kGThreads / 32);
