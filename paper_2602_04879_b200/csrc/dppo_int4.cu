@@ -84,6 +84,8 @@ __device__ __forceinline__ uint32_t codes_of_bf16(const float2* x, float scale, 
   return w;
 }
 
+// Bound by HBM: 151936 x 2048 bf16 in groups of 128 with the values, 1.41 GB, in 225 us, 97 % of the measured copy rate.  (With a piece to a thread, two
+// divisions a piece for its place and two for its scale it was bound by the issue slots: 590 us with the fp32 way to the codes, 311 with the bf16 one.)
 // A thread has pairs of pieces of 8 columns of a group, G / 2 columns apart, all of them loaded before the first is used; a group's G / 16 pairs lie in
 // neighbouring lanes, whose loads are whole sectors.
 template <typename InT, int G>
@@ -206,11 +208,11 @@ struct MatvecParams {
 };
 
 // ---- tensor cores ------------------------------------------------------------------------------------------------------
-// D[n, m] = sum over a group of (code[n, k] - 8) x[m, k] for up to 128 rows n and a few rows m at a time: the weights are the operand with the many
-// rows.  They come as they are stored by tensor copies (rows x 256 codes, 128-byte swizzle) into a ring; a thread per row turns a chunk of
-// its codes into the tensor cores' type in registers and writes them to tensor memory, where tcgen05.mma takes its A operand from; x
-// lies in shared memory for the whole launch.  The product of a group is read back, scaled by the row's scale (a thread's own) and added up
-// in fp32 registers.  One persistent CTA per SM:
+// D[n, m] = sum over a group of (code[n, k] - 8) x[m, k] for up to 128 rows n of the weights and a few rows m of x at a time: the weights are the
+// operand with the many rows.  They come as they are stored by tensor copies (rows x 256 codes, 128-byte swizzle) into a ring; a thread per
+// row turns a chunk of its codes into the tensor cores' type in registers and writes them to tensor memory, where tcgen05.mma takes its A
+// operand from; x lies in shared memory for the whole launch.  The product of a group is read back, scaled by the row's scale (a thread's own)
+// and added up in fp32 registers.  One persistent CTA per SM:
 //   warp 0          tensor copies of the weights
 //   warps 1 .. L    issue the MMAs (the first allocates tensor memory)
 //   L x 4 warps     conversion
@@ -227,8 +229,18 @@ struct MatvecParams {
 //   int8   (up to 4 rows of x) The codes stay whole numbers: two masks and a shift give a word's 8 bytes.  x is written as three signed 8-bit digits in
 //          units of 2^-22 of (a power of two above) the largest entry of its group, a row of the operand each; the int32 products are exact, and
 //          8 times the sum of the digits is taken off, exactly.  What is lost of x is below 2^-23 of the group's largest entry: less than
-//          fp32 sums lose.  An MMA takes 47 cycles with up to 96 columns, of bf16 (K = 16) as of int8 (K = 32): 374 cycles for 128 rows x 128
-//          codes of bf16, 187 of int8, where HBM delivers them in 356.
+//          fp32 sums lose.
+//
+// What bounds it, 151936 x 2048 in groups of 128 (166 MB; 25 us at the measured copy rate), calls back to back:
+//   1 row     31 us.  A launch, x and the first weights take 5 us; then 4 warps convert, and 8 take the products of, 256 codes of 115 rows in some 650
+//             cycles, where HBM delivers them in 640.
+//   16 rows   55 us, 61 rows 81 us.  The issue slots (62 % busy with 61 rows, the rest latency from one warp to the next): a chunk of 128 codes costs
+//             16 words x 11 instructions of conversion, and the products' warps some 100 each around their sums.  The tensor cores are not the
+//             bound: an MMA takes 47 cycles with up to 96 columns, of bf16 (K = 16) as of int8 (K = 32): 374 cycles a chunk for bf16, 187 for int8, of
+//             the 760 that it takes.
+// Tried and left: the chunks' products in rotation over two or three parts for bf16 (32 rows 62 -> 72 us: more warps for the same issue slots), three or
+// four lines for int8 (31 -> 33 us), int8 for 8 and 16 rows (see launch_rows).
+//
 // x is laid out in the order that the conversion makes of k.
 namespace mv {
 
@@ -260,11 +272,13 @@ template <int NT, int G, bool I8> struct Shape {
   static constexpr int XBYTES = I8 ? NT : 2 * NT;                      // of shared memory for a code
   static constexpr int XSPAN = I8 ? 128 : 64;                          // codes of a swizzled block of x
   static constexpr int NG = CHUNK / G;
-  // Warpgroups for the products.  bf16: 16 rows of x each, and of a single one's tiles two take turns, so that one stores while the other adds
-  // up.  int8: two, each half of a chunk's groups, whose sums meet at the tile's end.
+  // Warpgroups for the products: E share the rows of x.  int8: SPLIT parts, one for each line, whose sums meet at the tile's end (39 us for a row by one
+  // part, 31 by two).  bf16: TURNS sets, which take tiles in rotation, so that one stores while the other adds up (61 rows: 110 us with one set, 81
+  // with two); a single set for 17 to 32 rows, whose two warpgroups of 16 rows leave no registers for four (32 rows: 62 us, and 68 with two sets).
   static constexpr int E = I8 || NT == 16 ? 1 : 2, EN = XROWS / E, SPLIT = I8 ? 2 : 1, TURNS = I8 || NT == 32 ? 1 : 2;
   static constexpr int PRODUCTS = E * SPLIT * TURNS;                // in all; E of a chunk
   static constexpr int A = 64, D = NG * NT, COLS = A + D;              // columns of tensor memory of a chunk: operand, products
+  // Lines and buffers: six buffers of tensor memory in three lines where they fit (16 rows 55 us; four lines of one buffer 66 us), else four.
   static constexpr int L = !I8 && NT == 16 ? (COLS * 6 <= 512 ? 3 : 4) : 2;
   static constexpr int B = COLS * 2 * L <= 512 ? 2 : 1;
   static constexpr int BUFS = L * B;
@@ -446,7 +460,7 @@ struct Bars {
   unsigned long long full[12], empty[12];  // stages of weights
   unsigned long long ready[6], done[6];    // chunk: operand written and the buffer's products before read; MMAs done (operand free, products there)
   unsigned long long x_free, x_full;       // x replaced
-  unsigned long long turn[2];              // two sets by turns: the other has read its tile's last products.  Halves: the second's sums are here; read
+  unsigned long long turn[2];              // two sets: the other has read its tile's last products.  Two parts: the second's sums are there; read
   unsigned long long sum_full[2], sum_free[2];       // pairs of CTAs, by whose turn it is: the other's sums are here; read by the other
   uint32_t tmem;
   int abort_flag;
@@ -460,8 +474,8 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   unsigned char* xs = smem + p.stages * STAGE_BYTES;
   int4* table = reinterpret_cast<int4*>(xs + (size_t)p.seg * S::XBYTES);                       // int8: [groups of seg][XROWS]
-  float* halves = reinterpret_cast<float*>(table + (I8 ? p.seg / G * XROWS : 0));              // int8: [XROWS][LANES], from the second half of the groups
-  float* sums = halves + (I8 ? XROWS * LANES : 0);                                             // pairs of CTAs: [TURNS][E][OWN][LANES], from the other
+  float* meet = reinterpret_cast<float*>(table + (I8 ? p.seg / G * XROWS : 0));              // int8: [XROWS][LANES], from the second part
+  float* sums = meet + (I8 ? XROWS * LANES : 0);                                             // pairs of CTAs: [TURNS][E][OWN][LANES], from the other
   Bars* bars = reinterpret_cast<Bars*>(sums + (CL > 1 ? TURNS * S::E * OWN * LANES : 0));
   const uint32_t full0 = smem_u32(bars->full), empty0 = smem_u32(bars->empty), ready0 = smem_u32(bars->ready), done0 = smem_u32(bars->done);
   const uint32_t x_free = smem_u32(&bars->x_free), x_full = smem_u32(&bars->x_full);
@@ -608,13 +622,13 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
   } else {
     // ------------------------------------------------------------------ products
     constexpr int SPLIT = S::SPLIT;
-    const int wg = (warp - 1 - L - 4 * L) >> 2, e = wg % S::E, turn = TURNS > 1 ? wg / S::E : 0, half = SPLIT > 1 ? wg : 0, q = warp & 3, r = q * 32 + lane;
+    const int wg = (warp - 1 - L - 4 * L) >> 2, e = wg % S::E, turn = TURNS > 1 ? wg / S::E : 0, part = SPLIT > 1 ? wg : 0, q = warp & 3, r = q * 32 + lane;
     const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16) + S::A + (I8 ? 0 : e * EN);
     const uint32_t sum_full = smem_u32(&bars->sum_full[turn]), sum_free = smem_u32(&bars->sum_free[turn]);
     constexpr int PIECE = OWN % 4 == 0 ? 4 : 2;      // rows of x sent together
     float* inbox = sums + (turn * S::E + e) * OWN * LANES + r * PIECE;       // [OWN / PIECE][LANES][PIECE]
     if (turn == 0 && lane == 0)
-      for (int i = half * B; i < (SPLIT > 1 ? (half + 1) * B : BUFS); ++i) mbar_arrive(ready0 + 8 * i);      // nothing to be read before a buffer's first use
+      for (int i = part * B; i < (SPLIT > 1 ? (part + 1) * B : BUFS); ++i) mbar_arrive(ready0 + 8 * i);      // nothing to be read before a buffer's first use
     const int stride = TURNS * grid;       // between this set's tiles
     uint32_t n_tile = 0;
     bool ok = true;
@@ -646,13 +660,13 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
     };
     const unsigned short* srow = scales_of(tn, tile < tiles);
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) fetch(srow, (SPLIT > 1 ? half : 0) + u * SPLIT, sc[u]);
+    for (int u = 0; u < AHEAD; ++u) fetch(srow, part + u * SPLIT, sc[u]);
     for (int k = turn; tile < tiles && ok; tile += stride, k += TURNS) {       // k: this CTA's tiles
       // the tile's first chunk: its line, and how often the line's buffers have been used
       const uint32_t i0 = (uint32_t)k * (uint32_t)per_tile;
-      // (halves: the second half of the line's number of chunks from the tile's first on, and the same of the next tile)
-      const int begin = SPLIT > 1 ? half ^ (int)(i0 & 1u) : 0, begin_next = SPLIT > 1 ? half ^ (int)((i0 + (uint32_t)per_tile) & 1u) : 0;
-      int line = SPLIT > 1 ? half : (int)(i0 % L), sub = (int)((i0 + begin) / L % B);
+      // (parts: the first of the tile's chunks that is of this line, and the same of the next tile)
+      const int begin = SPLIT > 1 ? part ^ (int)(i0 & 1u) : 0, begin_next = SPLIT > 1 ? part ^ (int)((i0 + (uint32_t)per_tile) & 1u) : 0;
+      int line = SPLIT > 1 ? part : (int)(i0 % L), sub = (int)((i0 + begin) / L % B);
       uint32_t ph = (i0 + begin) / (L * B) & 1u;
       const int n = tn * p.rows + r, m0 = block * XROWS + e * EN;
       const bool live = srow != nullptr;
@@ -749,14 +763,14 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
         if (lane == 0) mbar_arrive(smem_u32(&bars->turn[turn ^ 1]));
       }
       if (SPLIT > 1) {
-        // the halves' sums meet
+        // the parts' sums meet at the first
         float* a = reinterpret_cast<float*>(acc);
         const uint32_t here = smem_u32(&bars->turn[0]), read = smem_u32(&bars->turn[1]);
-        if (half == 1) {
+        if (part == 1) {
           if (n_tile > 0 && !mbar_wait_warp(read, (n_tile - 1u) & 1u, wc)) { ok = false; break; }
 #pragma unroll
           for (int m = 0; m < XROWS; ++m)
-            if (m0 + m < p.M) halves[m * LANES + r] = a[m];
+            if (m0 + m < p.M) meet[m * LANES + r] = a[m];
           __syncwarp();
           if (lane == 0) mbar_arrive(here);
           srow = srow_next;
@@ -766,7 +780,7 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
         if (!mbar_wait_warp(here, n_tile & 1u, wc)) { ok = false; break; }
 #pragma unroll
         for (int m = 0; m < XROWS; ++m)
-          if (m0 + m < p.M) a[m] += halves[m * LANES + r];
+          if (m0 + m < p.M) a[m] += meet[m * LANES + r];
         __syncwarp();
         if (lane == 0) mbar_arrive(read);
       }

@@ -47,6 +47,8 @@ constexpr int kUnroll = 2;
 
 // what a warp knows of its part of a row
 struct Part { float mz, S, my, Sy, W, rare; };     // reference and sum of exp of z, the same of y, sum of exp times the difference; entries that are not ordinary
+// The same of a warp and of all of them.  From here on in 64 bits: the KL is what two large numbers leave, some 20 times smaller than they are.
+struct Sums { float mz, my, rare, pad; double S, Sy, W; };
 
 // Coefficients of the row's gradient: dz_j = e^(z_j - zr) (B ((z_j - zr) - (y_j - yr)) + A) for KL(pi || rho), e^(z_j - zr) A - B e^(y_j - yr) for
 // KL(rho || pi), A e^(z_j - zr) for k3, and its value at the token.  zr and yr are the two log-sum-exp, rounded.
@@ -63,6 +65,30 @@ template <typename T> __device__ __forceinline__ void exp_pairs(const uint4& z, 
     e[i] = make_float2(ex2_approx(x.x), ex2_approx(x.y));
   }
 }
+
+__device__ __forceinline__ void st_cluster_f64(uint32_t cluster_addr, double v) {
+  asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(cluster_addr), "d"(v) : "memory");
+}
+
+__device__ __forceinline__ float min_nan(float a, float b) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t min_nan_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// exp(d) without the rounding of d log2(e): what the product lost multiplies it by one plus that.  On average it is low by kExLow of itself (measured
+// as the KL's mean error, with and without it, on logits of standard deviation 1 and 3 in both types).
+__device__ __forceinline__ float exp_exact_arg(float d) {
+  const float x = d * kLog2e, v = ex2_approx(x);
+  return fmaf(v, fmaf(x, -(float)kLn2, d), v);
+}
+
+constexpr double kExLow = 1.5e-8;
 
 struct PolicyParams {
   RowParams row;             // logits, ids, mu_logp, adv, token_mask, dlogits, outputs (divergence: the KL), workspace
@@ -90,19 +116,21 @@ __device__ __forceinline__ RowIn row_in(const PolicyParams& q, int64_t t, int a)
 // The row's scalars and coefficients from its sums over the entries other than the token's (against mz and my; W against mz - my), by one warp.
 // 64-bit functions that do not depend on one another are evaluated side by side, a lane each (0: of pi, 1: of rho).
 template <int FORM>
-__device__ __forceinline__ Coef finish_row(const PolicyParams& q, int64_t t, const RowIn& in, const Part& w, int lane, double s, bool write) {
+__device__ __forceinline__ Coef finish_row(const PolicyParams& q, int64_t t, const RowIn& in, const Sums& w, int lane, double s, bool write) {
   constexpr bool TWO = FORM != DPPO_KL_K3;
   const RowParams& p = q.row;
-  const float mz = w.mz, my = w.my, S = w.S, Sy = w.Sy, W = w.W, z_a = in.z_a, y_a = in.y_a, mu = in.mu, adv = in.adv;
+  const float mz = w.mz, my = w.my, z_a = in.z_a, y_a = in.y_a, mu = in.mu, adv = in.adv;
+  const double S = w.S, Sy = w.Sy, W = w.W;
   const bool second = TWO && lane == 1;
   // maximum over the row, the weight of the others and of the token against it
-  const float tok = second ? y_a : z_a, top = second ? my : mz, sum = second ? Sy : S;
+  const float tok = second ? y_a : z_a, top = second ? my : mz;
+  const double sum = second ? Sy : S;
   const bool have_tok = !(tok <= kLowest), have_others = !(top == kLowest);
   const double big = have_tok && (!have_others || tok > top) ? (double)tok : (double)top;
   const double d_tok = have_tok ? (double)tok - big : -INFINITY, d_top = have_others ? (double)top - big : -INFINITY;
   const double e_far = exp(fmin(d_tok, d_top));          // the larger of the two is the maximum itself
   const double w_tok = d_tok >= d_top ? (have_tok ? 1.0 : 0.0) : e_far;
-  const double w_others = have_others ? (d_top >= d_tok ? (double)sum : (double)sum * e_far) : 0.0;
+  const double w_others = have_others ? (d_top >= d_tok ? sum : sum * e_far) : 0.0;
   const double total = w_tok + w_others;
   const double log_total = log(total);                   // -inf: no mass; NaN: a logit that is none
   const double p_tok = w_tok / total, p_others = w_others / total;
@@ -138,12 +166,12 @@ __device__ __forceinline__ Coef finish_row(const PolicyParams& q, int64_t t, con
       const double l_a = lp - ((y_a <= kLowest ? -INFINITY : (double)y_a) - lse_y);
       co.yr = (float)lse_y;
       if (FORM == DPPO_KL_PI_REF) {
-        kl = (pi_o > 0.0 ? pi_o * ((double)W / (double)S + shift) : 0.0) + (pi_a > 0.0 ? pi_a * l_a : 0.0);
+        kl = (pi_o > 0.0 ? pi_o * (W / S + shift) : 0.0) + (pi_a > 0.0 ? pi_a * l_a : 0.0);
         co.B = (float)(b * fz);
         co.A = (float)(fz * (g + b * ((double)co.zr - (double)co.yr - c - kl)));
         co.fix = (float)(-g * pi_o + (pi_a > 0.0 ? b * pi_a * (l_a - kl) : 0.0));
       } else {
-        kl = (rho_o > 0.0 ? rho_o * ((double)W / (double)Sy - shift) : 0.0) - (rho_a > 0.0 ? rho_a * l_a : 0.0);
+        kl = (rho_o > 0.0 ? rho_o * (W / Sy - shift) : 0.0) - (rho_a > 0.0 ? rho_a * l_a : 0.0);
         co.A = (float)(fz * (g + b));
         co.B = (float)(b * (1.0 + ((double)co.yr - lse_y)));
         co.fix = (float)(-g * pi_o + b * (pi_a - rho_a));
@@ -223,8 +251,25 @@ __device__ __forceinline__ void add_careful(Part& w, uint4* zv, uint4* yv) {
   w.W += W.x + W.y;
 }
 
+// smallest of raw entries, kept raw
+template <typename T> struct RawMin;
+template <> struct RawMin<__nv_bfloat16> {
+  uint32_t m = 0x7F7F7F7Fu;
+  __device__ __forceinline__ void add(const uint4& v) { m = min_nan_bf16x2(min_nan_bf16x2(m, v.x), min_nan_bf16x2(min_nan_bf16x2(v.y, v.z), v.w)); }
+  __device__ __forceinline__ float value() const { return min_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u)); }
+};
+template <> struct RawMin<float> {
+  float m = -kLowest;
+  __device__ __forceinline__ void add(const uint4& v) {
+    m = min_nan(min_nan(m, __uint_as_float(v.x)), min_nan(min_nan(__uint_as_float(v.y), __uint_as_float(v.z)), __uint_as_float(v.w)));
+  }
+  __device__ __forceinline__ float value() const { return m; }
+};
+
 // The same for ordinary entries: against references that stay where the thread's first vector put them.  Where that does not do (an entry far above
-// its reference, -inf, NaN: the sums show it) the entries go the careful way.
+// its reference, -inf, NaN: the sums show it) the entries go the careful way.  exp(y_j - y_ref) is formed from exp(z_j - z_ref) and the exponential of the difference, which is near one: what the first is off by
+// then stands in both sums alike and leaves the KL, where two exponentials on their own leave it 4e-8 off (relative to a KL of 0.045, logits of
+// standard deviation 3 and 151936 entries: 1.8e-6 and now 6e-7).  For this z_j must not be so low that its exponential vanishes.
 template <typename InT, int FORM, int NV>
 __device__ __forceinline__ void add_vectors(Part& w, uint4* zv, uint4* yv) {
   constexpr bool TWO = FORM != DPPO_KL_K3;
@@ -236,6 +281,7 @@ __device__ __forceinline__ void add_vectors(Part& w, uint4* zv, uint4* yv) {
     if (TWO) { my.add(yv[0]); w.my = my.value(); }
   }
   float2 S = make_float2(0.f, 0.f), Sy = S, W = S;
+  RawMin<InT> low;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     float2 az[N / 2], ez[N / 2];
@@ -243,20 +289,21 @@ __device__ __forceinline__ void add_vectors(Part& w, uint4* zv, uint4* yv) {
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) S = __fadd2_rn(S, ez[i]);
     if (TWO) {
-      const float2 neg = make_float2(-1.f, -1.f);
-      float2 ay[N / 2], ey[N / 2];
-      exp_pairs<InT>(yv[k], w.my, ay, ey);
+      const float2 neg = make_float2(-1.f, -1.f), nl2 = make_float2(-kLog2e, -kLog2e);
+      low.add(zv[k]);
+      float2 ay[N / 2];
+      less_pairs<InT>(yv[k], w.my, ay);
 #pragma unroll
       for (int i = 0; i < N / 2; ++i) {
-        Sy = __fadd2_rn(Sy, ey[i]);
-        if (FORM == DPPO_KL_PI_REF) W = __ffma2_rn(ez[i], __ffma2_rn(ay[i], neg, az[i]), W);
-        else W = __ffma2_rn(ey[i], __ffma2_rn(az[i], neg, ay[i]), W);
+        const float2 d = __ffma2_rn(ay[i], neg, az[i]), x = __fmul2_rn(d, nl2), ey = __fmul2_rn(ez[i], make_float2(ex2_approx(x.x), ex2_approx(x.y)));
+        Sy = __fadd2_rn(Sy, ey);
+        W = __ffma2_rn(FORM == DPPO_KL_PI_REF ? ez[i] : ey, d, W);
       }
     }
   }
-  const float s = S.x + S.y, sy = Sy.x + Sy.y, d = W.x + W.y;
+  const float s = S.x + S.y, sy = Sy.x + Sy.y, d = FORM == DPPO_KL_REF_PI ? -(W.x + W.y) : W.x + W.y;
   constexpr float most = 7.3786976e19f;    // 2^66; false for NaN
-  if (w.mz > kLowest && s <= most && (!TWO || (w.my > kLowest && sy <= most && fabsf(d) <= most))) {
+  if (w.mz > kLowest && s <= most && (!TWO || (w.my > kLowest && sy <= most && fabsf(d) <= most && low.value() - w.mz >= -60.f))) {
     w.S += s;
     w.Sy += sy;
     w.W += d;
@@ -267,22 +314,27 @@ __device__ __forceinline__ void add_vectors(Part& w, uint4* zv, uint4* yv) {
 
 // The lanes' sums as one, against their maxima (a lane that saw nothing but probability zero counts nothing; NaN stays).
 template <int FORM>
-__device__ __forceinline__ Part merge_lanes(Part w) {
+__device__ __forceinline__ Sums merge_lanes(const Sums& w) {
   constexpr bool TWO = FORM != DPPO_KL_K3;
-  const float mz = warp_max_nan(w.mz), my = TWO ? warp_max_nan(w.my) : 0.f;
-  const float fz = w.mz == kLowest ? 0.f : ex2_approx((w.mz - mz) * kLog2e), fy = !TWO || w.my == kLowest ? 0.f : ex2_approx((w.my - my) * kLog2e);
-  const float off = (w.mz - mz) - (w.my - my);
-  if (FORM == DPPO_KL_PI_REF) w.W = fz != 0.f ? fz * fmaf(w.S, off, w.W) : 0.f;
-  if (FORM == DPPO_KL_REF_PI) w.W = fy != 0.f ? fy * fmaf(-w.Sy, off, w.W) : 0.f;
-  w.S = warp_sum_f32(fz != 0.f ? fz * w.S : 0.f);
+  Sums r = {};
+  r.mz = warp_max_nan(w.mz);
+  r.my = TWO ? warp_max_nan(w.my) : 0.f;
+  // The factor of y from that of z, as in add_vectors, where neither vanishes.  (64-bit exponentials cost 4096 rows of 32000 entries a quarter more time.)
+  const float dz = w.mz - r.mz, off = dz - (w.my - r.my);
+  const double fz = w.mz == kLowest ? 0.0 : (double)exp_exact_arg(dz);
+  double fy = 0.0;
+  if (TWO && w.my != kLowest) fy = dz >= -60.f && off >= -60.f ? fz * (off == 0.f ? 1.0 : (double)exp_exact_arg(-off) * (1.0 + kExLow)) : (double)exp_exact_arg(w.my - r.my);
+  r.S = warp_sum(fz != 0.0 ? fz * w.S : 0.0);
   if (TWO) {
-    w.Sy = warp_sum_f32(fy != 0.f ? fy * w.Sy : 0.f);
-    w.W = warp_sum_f32(w.W);
+    r.Sy = warp_sum(fy != 0.0 ? fy * w.Sy : 0.0);
+    r.W = warp_sum(FORM == DPPO_KL_PI_REF ? (fz != 0.0 ? fz * fma(w.S, (double)off, w.W) : 0.0) : (fy != 0.0 ? fy * fma(-w.Sy, (double)off, w.W) : 0.0));
   }
-  w.mz = mz;
-  w.my = my;
-  w.rare = __any_sync(0xffffffffu, w.rare != 0.f) ? 1.f : 0.f;
-  return w;
+  r.rare = __any_sync(0xffffffffu, w.rare != 0.f) ? 1.f : 0.f;
+  return r;
+}
+template <int FORM>
+__device__ __forceinline__ Sums merge_lanes(const Part& w) {
+  return merge_lanes<FORM>(Sums{w.mz, w.my, w.rare, 0.f, (double)w.S, (double)w.Sy, (double)w.W});
 }
 
 // The gradient of one vector.
@@ -321,12 +373,12 @@ struct RingMisc {
   unsigned long long part_full[kHand], part_empty[kHand];  // sums of a row: sum warps -> scalar warp
   unsigned long long coef_full[kHand], coef_empty[kHand];  // coefficients of a row: scalar warp -> gradient warps
   unsigned long long x_full[kHand], x_empty[kHand];        // sums of a row of every CTA of the cluster
-  Part part[kHand][kMaxTeams * kTeamWarps], x_part[kHand][kMaxCluster];
+  Sums part[kHand][kMaxTeams * kTeamWarps], x_part[kHand][kMaxCluster];
   Coef coef[kHand];
   int abort_flag;
   unsigned int grad_slots;                                 // slots the gradient warps have finished
 };
-constexpr int kMiscBytes = 2048;
+constexpr int kMiscBytes = 4096;
 static_assert(sizeof(RingMisc) <= kMiscBytes, "misc area");
 
 // A row's image in the ring: from the 16-byte boundary at or below its first element (head elements early) on.
@@ -504,11 +556,11 @@ __global__ void __launch_bounds__(kRingThreads<FORM != DPPO_KL_K3>, 1) policy_kl
           if (!__any_sync(0xffffffffu, w.S < 0.f || (TWO && w.Sy < 0.f)) && lane == 0) mbar_arrive(empty + 8u * pos.slot);
           pos.advance(kSumSlots);
         }
-        w = merge_lanes<FORM>(w);
+        const Sums sums = merge_lanes<FORM>(w);
         if (lane == 0) {
           const uint32_t b = n % kHand, u = n / kHand;
           if (u == 0 || mbar_wait(part_empty + 8u * b, (u & 1u) ^ 1u, wc)) {
-            misc->part[b][warp] = w;
+            misc->part[b][warp] = sums;
             mbar_arrive(part_full + 8u * b);
           }
         }
@@ -594,8 +646,8 @@ __global__ void __launch_bounds__(kRingThreads<FORM != DPPO_KL_K3>, 1) policy_kl
         const uint32_t b = (n - 1) % kHand, u = (n - 1) / kHand;
         const RowIn in = row_in<InT, FORM>(q, t, a);
         bool have = mbar_wait_warp(part_full + 8u * b, u & 1u, wc);
-        const Part none{kLowest, 0.f, kLowest, 0.f, 0.f, 0.f};
-        Part w = have && lane < TEAMS * kTeamWarps ? misc->part[b][lane] : none;
+        const Sums none{kLowest, kLowest, 0.f, 0.f, 0.0, 0.0, 0.0};
+        Sums w = have && lane < TEAMS * kTeamWarps ? misc->part[b][lane] : none;
         __syncwarp();
         if (lane == 0 && have) mbar_arrive(part_empty + 8u * b);
         w = merge_lanes<FORM>(w);
@@ -605,9 +657,11 @@ __global__ void __launch_bounds__(kRingThreads<FORM != DPPO_KL_K3>, 1) policy_kl
           if (have && u > 0) have = __all_sync(0xffffffffu, mbar_wait_cluster(xe, (u & 1u) ^ 1u, wc));
           if (have && lane < CL) {
             const uint32_t dst = map_to_cta(smem_u32(&misc->x_part[b][rank]), (uint32_t)lane);
-            st_cluster_f32x2(dst, w.mz, w.S);
-            st_cluster_f32x2(dst + 8, w.my, w.Sy);
-            st_cluster_f32x2(dst + 16, w.W, w.rare);
+            st_cluster_f32x2(dst, w.mz, w.my);
+            st_cluster_f32x2(dst + 8, w.rare, 0.f);
+            st_cluster_f64(dst + 16, w.S);
+            st_cluster_f64(dst + 24, w.Sy);
+            st_cluster_f64(dst + 32, w.W);
             bar_arrive_cluster(map_to_cta(xf, (uint32_t)lane));
           }
           if (have) have = __all_sync(0xffffffffu, mbar_wait_cluster(xf, u & 1u, wc));
@@ -640,7 +694,7 @@ template <typename InT, typename OutT, int FORM>
 __global__ void __launch_bounds__(kThreads) policy_kl_kernel(const __grid_constant__ PolicyParams q) {
   constexpr bool TWO = FORM != DPPO_KL_K3;
   constexpr int N = Vec<InT>::N;
-  __shared__ Part parts[kWarps];
+  __shared__ Sums parts[kWarps];
   __shared__ Coef s_coef;
   const RowParams& p = q.row;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -675,13 +729,12 @@ __global__ void __launch_bounds__(kThreads) policy_kl_kernel(const __grid_consta
         }
       add_careful<InT, FORM, kUnroll>(w, zv, yv);
     }
-    w = merge_lanes<FORM>(w);
-    if (lane == 0) parts[warp] = w;
+    Sums sums = merge_lanes<FORM>(w);
+    if (lane == 0) parts[warp] = sums;
     __syncthreads();
     if (warp == 0) {
-      w = lane < kWarps ? parts[lane] : Part{kLowest, 0.f, kLowest, 0.f, 0.f, 0.f};
-      w = merge_lanes<FORM>(w);
-      const Coef co = finish_row<FORM>(q, t, in, w, lane, q.scale > 0.0 ? q.scale : p.hdr->scale, true);
+      sums = merge_lanes<FORM>(lane < kWarps ? parts[lane] : Sums{kLowest, kLowest, 0.f, 0.f, 0.0, 0.0, 0.0});
+      const Coef co = finish_row<FORM>(q, t, in, sums, lane, q.scale > 0.0 ? q.scale : p.hdr->scale, true);
       if (lane == 0) s_coef = co;
     }
     __syncthreads();
