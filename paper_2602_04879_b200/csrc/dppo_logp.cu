@@ -9,6 +9,10 @@
 // Pairs of sequences: the coefficient c_t of a row needs the sums over all rows of its pair, so the logits are read twice (forward, a
 // single CTA for the pairs, backward).  The backward pass walks the rows from the last to the first: those it starts with were
 // read last and still lie in L2.
+//
+// All of it is bound by HBM: forward 8192 x 151936 bf16 388 us, 97 % of the measured copy rate; 16 pairs, 6000 x 151936 bf16, 845 us for three passes over
+// 1.82 GB.  A CTA per row and four vectors in flight a thread: eight are slower (445 us for the 8192 rows; fewer CTAs an SM), and so are 2, 4 or 8 CTAs
+// to a row where there are rows enough (422, 486, 661 us); for one row they are the faster ones (18.5, 12.4, 9.5 and 8.2 us).
 #include "dppo_rowvec.cuh"
 
 namespace dppo {
