@@ -522,7 +522,8 @@ int dppo_int4_quantize(const void* x, int64_t rows, int64_t cols, int64_t x_row_
  *  x [M, K] bf16, q and scale as dppo_int4_quantize lays them out (codes 0 .. 15), y [M, N] DPPO_F32 or DPPO_BF16 (rounded once); row
  *  strides in elements, of q in bytes.  Any M is right; the kernel is made for M up to 64.  With q and its row stride on
  *  16-byte boundaries the weights come by bulk copies, otherwise element by element (several times slower).
- *  y must not overlap the inputs.  K = 0 gives y = 0.  status: device word, DPPO_STATUS_WAIT_LIMIT.  opts: wait_limit_us, test_inject.
+ *  y must not overlap the inputs.  K = 0 gives y = 0.  A row of x with an infinity or a NaN has no finite results (NaN throughout for M <= 4).
+ *  status: device word, DPPO_STATUS_WAIT_LIMIT.  opts: wait_limit_us, test_inject.
  */
 int dppo_matvec_int4(const void* x, int64_t x_row_stride, const uint8_t* q, int64_t q_row_stride, const void* scale,
                      int64_t scale_row_stride, int group, int64_t M, int64_t N, int64_t K, void* y, int y_dtype,

@@ -903,7 +903,8 @@ cudaError_t launch_cl(Params p, const unsigned char* q, int64_t ldq, int sms, in
   const int smem = p.stages * STAGE_BYTES + p.seg / 256 * X256 + FIXED;
   const int64_t tiles = (int64_t)((p.N + p.rows - 1) / p.rows) * ((p.M + S::XROWS - 1) / S::XROWS);
   auto kernel = matvec_int4_kernel<NT, G, CL, I8>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  // (the most there is, whatever this call takes: another thread may be between this and its launch)
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_most);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[1];

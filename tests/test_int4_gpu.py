@@ -5,6 +5,8 @@ one fma gives exactly.  Values are code times scale (12 bits, exact in fp32) rou
 (12 bits); they are added up in fp32, in any order, a rounding (2^-24, or 2^-23 where a tensor core truncates) for each of at most K
 additions of the group sums, the scaling and the sum over the groups: (K + 3) 2^-23 of the sum of the terms' magnitudes, and half a step of
 the output type (2^-24, 2^-8)."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -269,6 +271,35 @@ def test_product_captured_and_on_another_stream():
     assert not busy.query()
     torch.cuda.synchronize()
     assert torch.equal(z, want) and torch.equal(w["q"], wq)
+
+
+def test_product_from_several_threads():
+    """Calls that take unlike amounts of shared memory, from threads with a stream each."""
+    cases = []
+    for K in (512, 2048, 4096, 700):
+        x, codes, scale = product_case(16, 900, K, 64, seed=K)
+        q, s, xd = packed(codes), scale.to(DEV), x.to(DEV)
+        cases.append((xd, q, s, dppo.dppo_matvec_int4(xd, q, s, 64)[0]))
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(i):
+        xd, q, s, want = cases[i]
+        st = torch.cuda.Stream(DEV)
+        try:
+            with torch.cuda.stream(st):
+                for _ in range(200):
+                    if not torch.equal(dppo.dppo_matvec_int4(xd, q, s, 64)[0], want):
+                        wrong.append((i, "result"))
+        except Exception as e:             # noqa: BLE001 (reported below)
+            wrong.append((i, repr(e)))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(cases))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong, wrong[:3]
 
 
 def test_rollout_in_4_bits_and_its_update_end_to_end():
