@@ -307,7 +307,7 @@ __device__ __forceinline__ void add_vectors(Part& w, uint4* zv, uint4* yv) {
   }
   const float s = S.x + S.y, sy = Sy.x + Sy.y, d = FORM == DPPO_KL_REF_PI ? -(W.x + W.y) : W.x + W.y;
   constexpr float most = 7.3786976e19f;    // 2^66; false for NaN
-  if (w.mz > kLowest && s <= most && (!TWO || (w.my > kLowest && sy <= most && fabsf(d) <= most && low.value() - w.mz >= -60.f))) {
+  if (w.mz > kLowest && s <= most && (!TWO || (w.my > kLowest && sy <= most && fabsf(d) <= most && low.value() - w.mz >= -80.f))) {
     w.S += s;
     w.Sy += sy;
     w.W += d;
@@ -327,7 +327,7 @@ __device__ __forceinline__ Sums merge_lanes(const Sums& w) {
   const float dz = w.mz - r.mz, off = dz - (w.my - r.my);
   const double fz = w.mz == kLowest ? 0.0 : (double)exp_exact_arg(dz);
   double fy = 0.0;
-  if (TWO && w.my != kLowest) fy = dz >= -60.f && off >= -60.f ? fz * (off == 0.f ? 1.0 : (double)exp_exact_arg(-off) * (1.0 + kExLow)) : (double)exp_exact_arg(w.my - r.my);
+  if (TWO && w.my != kLowest) fy = dz >= -80.f && off >= -80.f ? fz * (off == 0.f ? 1.0 : (double)exp_exact_arg(-off) * (1.0 + kExLow)) : (double)exp_exact_arg(w.my - r.my);
   r.S = warp_sum(fz != 0.0 ? fz * w.S : 0.0);
   if (TWO) {
     r.Sy = warp_sum(fy != 0.0 ? fy * w.Sy : 0.0);

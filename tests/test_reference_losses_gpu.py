@@ -295,6 +295,27 @@ def test_policy_kl_of_policies_that_differ_by_a_constant_or_not_at_all():
             assert np.abs(host(o["dlogits"])).max() <= 0.25 * (6 * eps(5000) + 4 * U * 100)
 
 
+@pytest.mark.parametrize("form", ["pi_ref", "ref_pi"])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("apart", ["wide", "halves", "one entry"])
+def test_policy_of_policies_that_live_on_different_entries(apart, dtype, form):
+    """Entries whose probability vanishes under one policy and counts under the other: their exponentials cannot come from one another."""
+    T, V = 4, 20488
+    c = policy_case(T, V, dtype, seed=31, masked=False)
+    z, y = c["z"].float(), c["y"].float()
+    if apart == "wide":
+        g = torch.Generator().manual_seed(32)
+        z, y = z + 30 * torch.randn(z.shape, generator=g), y + 30 * torch.randn(y.shape, generator=g)
+    elif apart == "halves":
+        z[:, ::2] -= 150
+        y[:, 1::2] -= 90
+    else:
+        y[:, 4321] += 120
+        z[:, 4322] -= 120
+    c["z"], c["y"] = z.to(dtype), y.to(dtype)
+    check_policy(c, run_policy(c, form), form)
+
+
 def test_policy_masked_vocabulary_infinities_and_dropped_rows():
     for dtype in (BF, F32):
         c = policy_case(8, 3001, dtype, seed=19, masked=False)
