@@ -238,7 +238,7 @@ struct MatvecParams {
 //             16 words x 11 instructions of conversion, and the products' warps some 100 each around their sums.  The tensor cores are not the
 //             bound: an MMA takes 47 cycles with up to 96 columns, of bf16 (K = 16) as of int8 (K = 32): 374 cycles a chunk for bf16, 187 for int8, of
 //             the 760 that it takes.
-// Tried and left: the chunks' products in rotation over two or three parts for bf16 (32 rows 62 -> 72 us: more warps for the same issue slots), three or
+// Tried and left: the chunks' products in rotation over two or three parts for bf16 (32 rows 64 -> 72 us: more warps for the same issue slots), three or
 // four lines for int8 (31 -> 33 us), int8 for 8 and 16 rows (see launch_rows).
 //
 // x is laid out in the order that the conversion makes of k.
@@ -259,6 +259,7 @@ struct Params {
   int y_bf16, x_vec;                       // x_vec: 16-byte loads of x allowed
   int rows, stages, seg, nseg, groups;     // rows of a tile; seg: codes of K that x lies in shared memory for (a multiple of 256), nseg of them to a CTA
   int pairs;                               // blocks of 256 codes of a CTA
+  int scales_together;                     // a chunk's scales lie on a boundary of their size
   int32_t* status;
   unsigned long long wait_ns;
   int inject;
@@ -274,7 +275,7 @@ template <int NT, int G, bool I8> struct Shape {
   static constexpr int NG = CHUNK / G;
   // Warpgroups for the products: E share the rows of x.  int8: SPLIT parts, one for each line, whose sums meet at the tile's end (39 us for a row by one
   // part, 31 by two).  bf16: TURNS sets, which take tiles in rotation, so that one stores while the other adds up (61 rows: 110 us with one set, 81
-  // with two); a single set for 17 to 32 rows, whose two warpgroups of 16 rows leave no registers for four (32 rows: 62 us, and 68 with two sets).
+  // with two); a single set for 17 to 32 rows, whose two warpgroups of 16 rows leave no registers for four (32 rows: 64 us, and 68 with two sets).
   static constexpr int E = I8 || NT == 16 ? 1 : 2, EN = XROWS / E, SPLIT = I8 ? 2 : 1, TURNS = I8 || NT == 32 ? 1 : 2;
   static constexpr int PRODUCTS = E * SPLIT * TURNS;                // in all; E of a chunk
   static constexpr int A = 64, D = NG * NT, COLS = A + D;              // columns of tensor memory of a chunk: operand, products
@@ -649,7 +650,27 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
     };
     // (a register each, and the loads by predicate: nothing here may wait for them)
     uint32_t sc[AHEAD][NG];
+    // int8, four or eight groups to a chunk: all at once where they lie so (two to a register then; groups of 32, one row: 64 -> 56 us).
+    constexpr bool MANY = I8 && NG >= 4;
+    const bool together = MANY && p.scales_together;
     auto fetch = [&](const unsigned short* row, int c, uint32_t* to) {
+      if constexpr (MANY) {
+        if (together) {
+          const unsigned short* src = row + c * NG;
+          const int there = row ? min(max(glim - c * NG, 0), NG) : 0;
+#pragma unroll
+          for (int h = 0; h < NG; ++h) to[h] = 0u;
+          if (there == NG) {
+            if (NG == 8) asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(to[0]), "=r"(to[1 % NG]), "=r"(to[2 % NG]), "=r"(to[3 % NG]) : "l"(src));
+            else asm volatile("ld.global.nc.v2.u32 {%0, %1}, [%2];" : "=r"(to[0]), "=r"(to[1 % NG]) : "l"(src));
+          } else {
+#pragma unroll
+            for (int h = 0; h < NG; ++h)
+              if (h < there) to[h / 2] |= (uint32_t)src[h] << (16 * (h & 1));
+          }
+          return;
+        }
+      }
 #pragma unroll
       for (int h = 0; h < NG; ++h) {
         const int gi = c * NG + h;
@@ -657,6 +678,9 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
         asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %2, 0;\n @q ld.global.nc.u16 %0, [%1];\n}\n"
                      : "+r"(to[h]) : "l"(row + gi), "r"((int)(row && gi < glim)));
       }
+    };
+    auto scale_of = [&](const uint32_t* from, int h) {
+      return __uint_as_float(together ? (h & 1 ? from[h / 2] & 0xffff0000u : from[h / 2] << 16) : from[h] << 16);
     };
     const unsigned short* srow = scales_of(tn, tile < tiles);
 #pragma unroll
@@ -713,7 +737,7 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
                   for (int h = 0; h < NG; ++h) tmem_ld4(td + h * NT, v[h]);
                   tmem_ld_wait<NG * 4>(v[0]);
 #pragma unroll
-                  for (int h = 0; h < NG; ++h) add(v[h], 0, __uint_as_float(sc[u][h] << 16), tab[h * XROWS]);
+                  for (int h = 0; h < NG; ++h) add(v[h], 0, scale_of(sc[u], h), tab[h * XROWS]);
                 } else {
                   constexpr int AT = NG < 2 ? NG : 2;      // groups read together
 #pragma unroll
@@ -727,14 +751,14 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
 #pragma unroll
                       for (int m = 0; m < XROWS; ++m) {
                         if (m0 + m >= p.M) break;
-                        add(v[h] + 4 * m, m, __uint_as_float(sc[u][h1 + h] << 16), tab[(h1 + h) * XROWS + m]);
+                        add(v[h] + 4 * m, m, scale_of(sc[u], h1 + h), tab[(h1 + h) * XROWS + m]);
                       }
                   }
                 }
               } else {
 #pragma unroll
                 for (int h = 0; h < NG; ++h) {
-                  const float s1 = __uint_as_float(sc[u][h] << 16);
+                  const float s1 = scale_of(sc[u], h);
                   const float2 s2 = make_float2(s1, s1);
                   constexpr int AT = EN < 32 ? 16 : 32;    // columns read together
 #pragma unroll
@@ -882,6 +906,7 @@ cudaError_t launch_cl(Params p, const unsigned char* q, int64_t ldq, int sms, in
   constexpr int FIXED = Room<NT, G, CL, I8>::FIXED, X256 = Room<NT, G, CL, I8>::X256;
   const int room = smem_most - FIXED, total = (p.K + 255) / 256;
   p.pairs = (total + CL - 1) / CL;
+  p.scales_together = (uintptr_t)p.scale % (2 * S::NG) == 0 && (p.N == 1 || p.lds % S::NG == 0);
   // x for all of this CTA's K where at least four stages are left besides it, else as much as leaves that many
   const int most = x_blocks<NT, G, CL, I8>(smem_most);
   p.nseg = (p.pairs + most - 1) / most;

@@ -215,6 +215,22 @@ def test_product_in_any_layout():
             assert (yb[~inside] == 7.0).all()
 
 
+@pytest.mark.parametrize("M,group,K", [(3, 32, 1000), (1, 64, 1500), (4, 32, 2048), (2, 64, 255), (20, 32, 700)])
+def test_product_with_scales_in_padded_rows(M, group, K):
+    """Rows of scales on the boundaries at which a chunk's are fetched together, with a last chunk that is not whole, and off them; what lies
+    between the rows is not used."""
+    N, groups = 300, -(-K // group)
+    x, codes, scale = product_case(M, N, K, group, seed=K)
+    q, xd = packed(codes), x.to(DEV)
+    up = -(-groups // 8) * 8
+    for so, lds in ((0, up), (0, up + 8), (8, up + 16), (0, up + 4), (4, up + 4), (1, up), (0, groups + 1), (2, up + 2)):
+        sb = torch.full((so + N * lds,), float("nan"), dtype=BF, device=DEV)
+        sv = torch.as_strided(sb, (N, groups), (lds, 1), so).copy_(scale)
+        y, st = dppo.dppo_matvec_int4(xd, q, sv, group)
+        assert int(st.item()) == 0
+        check_product(y, x, codes, scale, group, F32)
+
+
 @pytest.mark.parametrize("M", [1, 61])
 def test_product_special_values(M):
     """Infinities and NaN in x stay in their row, in a scale in their column; K = 0; all-zero rows."""
