@@ -592,8 +592,9 @@ __global__ void __launch_bounds__(kRingThreads<FORM != DPPO_KL_K3>, 1) policy_kl
         const uint32_t b = n % kHand, u = n / kHand;
         const bool have = mbar_wait_warp(coef_full + 8u * b, u & 1u, wc);
         Coef co = misc->coef[b];
-        __syncwarp();
-        if (lane == 0 && have) mbar_arrive(coef_empty + 8u * b);
+        // (a vote on what was read, whatever its answer: the arrival is not to be moved up before the loads)
+        if ((!__any_sync(0xffffffffu, co.zr + co.yr + co.A + co.B + co.fix == 1.f && co.mode == kCareful) || p.V > 0) && lane == 0 && have)
+          mbar_arrive(coef_empty + 8u * b);
         if (!have) co.mode = kZeros;
         ++n;
         const int av = (a + head) / N;
@@ -652,9 +653,8 @@ __global__ void __launch_bounds__(kRingThreads<FORM != DPPO_KL_K3>, 1) policy_kl
         bool have = mbar_wait_warp(part_full + 8u * b, u & 1u, wc);
         const Sums none{kLowest, kLowest, 0.f, 0.f, 0.0, 0.0, 0.0};
         Sums w = have && lane < TEAMS * kTeamWarps ? misc->part[b][lane] : none;
-        __syncwarp();
-        if (lane == 0 && have) mbar_arrive(part_empty + 8u * b);
         w = merge_lanes<FORM>(w);
+        if (lane == 0 && have) mbar_arrive(part_empty + 8u * b);           // (behind the exchange between the lanes: all have what they read)
         if (CL > 1) {
           // the CTAs of the cluster exchange their sums: lane r sends to CTA r once every CTA has read the buffer's last content
           const uint32_t xf = smem_u32(&misc->x_full[b]), xe = smem_u32(&misc->x_empty[b]);
@@ -670,9 +670,8 @@ __global__ void __launch_bounds__(kRingThreads<FORM != DPPO_KL_K3>, 1) policy_kl
           }
           if (have) have = __all_sync(0xffffffffu, mbar_wait_cluster(xf, u & 1u, wc));
           w = have && lane < CL ? misc->x_part[b][lane] : none;
-          __syncwarp();
-          if (have && lane < CL) bar_arrive_cluster(map_to_cta(xe, (uint32_t)lane));
           w = merge_lanes<FORM>(w);
+          if (have && lane < CL) bar_arrive_cluster(map_to_cta(xe, (uint32_t)lane));
         }
         if (have) {
           const Coef co = finish_row<FORM>(q, t, in, w, lane, s, rank == 0);
