@@ -805,8 +805,7 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
 #pragma unroll
         for (int m = 0; m < XROWS; ++m)
           if (m0 + m < p.M) a[m] += meet[m * LANES + r];
-        __syncwarp();
-        if (lane == 0) mbar_arrive(read);
+        if ((!__any_sync(0xffffffffu, a[0] + a[1] + a[2] + a[3 % EN] == 1.f) || p.M > 0) && lane == 0) mbar_arrive(read);   // (once they have been read, see below)
       }
       const float* a = reinterpret_cast<const float*>(acc);
       float sum[OWN];
