@@ -842,8 +842,11 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
 #pragma unroll
           for (int i = 0; i < PIECE; ++i) sum[j + i] += inbox[j * LANES + i];
         // Nothing but what was read is behind this arrival: a release would wait for the stores to y, a fence for loads under way.  The vote's answer does
-        // not matter; it has the arrival wait for what was read.
-        if ((!__any_sync(0xffffffffu, sum[0] + sum[OWN - 1] == 1.f) || p.M > 0) && lane == 0)
+        // not matter; it has the arrival wait for what was read, of which every vector is in it.
+        float all = 0.f;
+#pragma unroll
+        for (int j = 0; j < OWN; ++j) all += sum[j];
+        if ((!__any_sync(0xffffffffu, all == 1.f) || p.M > 0) && lane == 0)
           asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(map_to_cta(sum_free, (uint32_t)(rank ^ 1))) : "memory");
         m_own = m0 + rank * OWN;
       }
