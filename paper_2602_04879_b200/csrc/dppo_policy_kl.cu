@@ -253,6 +253,9 @@ __device__ __forceinline__ void add_careful(Part& w, uint4* zv, uint4* yv) {
   w.S += S.x + S.y;
   w.Sy += Sy.x + Sy.y;
   w.W += W.x + W.y;
+  // A reference that is still the lowest: all its entries have probability zero.  (Against one another their exponentials are 1.)
+  if (w.mz == kLowest) { w.S = 0.f; if (FORM == DPPO_KL_PI_REF) w.W = 0.f; }
+  if (TWO && w.my == kLowest) { w.Sy = 0.f; if (FORM == DPPO_KL_REF_PI) w.W = 0.f; }
 }
 
 // smallest of raw entries, kept raw
@@ -278,7 +281,7 @@ template <typename InT, int FORM, int NV>
 __device__ __forceinline__ void add_vectors(Part& w, uint4* zv, uint4* yv) {
   constexpr bool TWO = FORM != DPPO_KL_K3;
   constexpr int N = Vec<InT>::N;
-  if (w.mz == kLowest) {
+  if (w.mz == kLowest && (!TWO || w.my == kLowest)) {      // (nothing but probability zero so far, in either: no sums to move)
     RawMax<InT> mz, my;
     mz.add(zv[0]);
     w.mz = mz.value();
@@ -327,7 +330,7 @@ __device__ __forceinline__ Sums merge_lanes(const Sums& w) {
   const float dz = w.mz - r.mz, off = dz - (w.my - r.my);
   const double fz = w.mz == kLowest ? 0.0 : (double)exp_exact_arg(dz);
   double fy = 0.0;
-  if (TWO && w.my != kLowest) fy = dz >= -80.f && off >= -80.f ? fz * (off == 0.f ? 1.0 : (double)exp_exact_arg(-off) * (1.0 + kExLow)) : (double)exp_exact_arg(w.my - r.my);
+  if (TWO && w.my != kLowest) fy = fz != 0.0 && dz >= -80.f && off >= -80.f ? fz * (off == 0.f ? 1.0 : (double)exp_exact_arg(-off) * (1.0 + kExLow)) : (double)exp_exact_arg(w.my - r.my);
   r.S = warp_sum(fz != 0.0 ? fz * w.S : 0.0);
   if (TWO) {
     r.Sy = warp_sum(fy != 0.0 ? fy * w.Sy : 0.0);
