@@ -86,10 +86,11 @@ __device__ __forceinline__ uint32_t min_nan_bf16x2(uint32_t a, uint32_t b) {
 }
 
 // exp(d) without the rounding of d log2(e): what the product lost multiplies it by one plus that.  On average it is low by kExLow of itself (measured
-// as the KL's mean error, with and without it, on logits of standard deviation 1 and 3 in both types).
+// as the KL's mean error, with and without it, on logits of standard deviation 1 and 3 in both types).  Zero where it vanishes: the product may have
+// overflowed there, and what it lost is then no number.
 __device__ __forceinline__ float exp_exact_arg(float d) {
   const float x = d * kLog2e, v = ex2_approx(x);
-  return fmaf(v, fmaf(x, -(float)kLn2, d), v);
+  return v == 0.f ? 0.f : fmaf(v, fmaf(x, -(float)kLn2, d), v);
 }
 
 constexpr double kExLow = 1.5e-8;
@@ -224,10 +225,11 @@ __device__ __forceinline__ void add_careful(Part& w, uint4* zv, uint4* yv) {
   const float bz = max_nan(w.mz, mz.value()), by = TWO ? max_nan(w.my, my.value()) : 0.f;
   if (!(bz == w.mz) || (TWO && !(by == w.my))) {
     const float fz = ex2_approx((w.mz - bz) * kLog2e), fy = TWO ? ex2_approx((w.my - by) * kLog2e) : 0.f;
-    if (FORM == DPPO_KL_PI_REF) w.W = (w.mz > kLowest) ? fz * fmaf(w.S, (w.mz - bz) - (w.my - by), w.W) : 0.f;
-    if (FORM == DPPO_KL_REF_PI) w.W = (w.my > kLowest) ? fy * fmaf(w.Sy, (w.my - by) - (w.mz - bz), w.W) : 0.f;
+    // (where a sum vanishes against the new maximum its differences do too, however large they are)
     w.S *= fz;
     w.Sy *= fy;
+    if (FORM == DPPO_KL_PI_REF) w.W = fz != 0.f && w.S != 0.f ? fmaf(w.S, (w.mz - bz) - (w.my - by), fz * w.W) : 0.f;
+    if (FORM == DPPO_KL_REF_PI) w.W = fy != 0.f && w.Sy != 0.f ? fmaf(w.Sy, (w.my - by) - (w.mz - bz), fy * w.W) : 0.f;
     w.mz = bz;
     w.my = by;
   }

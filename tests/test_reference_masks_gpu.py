@@ -53,7 +53,7 @@ def with_mask(c, live, value, in_z, in_y):
 
 
 SIZES = [(3, 151936, BF), (3, 60000, F32), (150, 20488, BF), (150, 9000, F32)]
-VALUES = [float("-inf"), "lowest", -1e9]
+VALUES = [float("-inf"), "lowest", -3e38, -1e38, -1e9]
 
 
 @pytest.mark.parametrize("kind", ["front", "back", "few", "blocks"])
@@ -90,7 +90,7 @@ def test_vocabulary_masked_in_the_policy_alone(T, V, dtype, kind):
 @pytest.mark.parametrize("T,V,dtype", SIZES)
 def test_vocabulary_masked_in_the_reference_alone(T, V, dtype):
     case, live = masked_case("blocks", T, V, dtype, seed=V + T + 20)
-    for value in (float("-inf"),):
+    for value in (float("-inf"), -3e38):
         c, zh, yh = with_mask(case, live, value, False, True)
         o = run_policy(c, "pi_ref", mask=False)
         assert int(o["status"].item()) == binding.STATUS_NONFINITE_ROW
@@ -107,7 +107,7 @@ def test_masked_vocabulary_in_rows_off_16_byte_boundaries(dtype, alone):
     T, V = 5, 20001
     for kind in ("front", "few"):
         case, live = masked_case(kind, T, V, dtype, seed=77)
-        for value in (float("-inf"), -1e9):
+        for value in (float("-inf"), -3e38, -1e38):
             c, zh, yh = with_mask(case, live, value, True, not alone)
             z, _ = placed(c["z"], V + 2, 1)
             for form in ("pi_ref", "k3") if alone else FORMS:
