@@ -429,7 +429,8 @@ int dppo_token_logp(const void* logits, int64_t T, int64_t V, int64_t logits_row
 /*
  * Its backward pass: dlogits_tj = dlogp_t (1[j = a_t] - pi_tj), for losses made of log-probabilities.
  *
- *  lse         [T] as dppo_token_logp gave it for these logits and ids.      dlogp  [T] derivative by logp_t.
+ *  lse         [T] as dppo_token_logp gave it for these logits and ids (64 bits of it: pi is off by 2^-53 |lse| of itself).
+ *  dlogp       [T] derivative by logp_t.
  *  dlogits     [T, V] out, dtype per dlogits_dtype (DPPO_DLOGITS_SAME or DPPO_DLOGITS_F32); in place or disjoint, as for
  *              dppo_loss_fwd_bwd.  Rows that are masked, dropped or have dlogp_t = 0 are zero.
  * Needs no workspace; one kernel launch.

@@ -204,7 +204,8 @@ __global__ void __launch_bounds__(kThreads) token_grad_kernel(GradParams p) {
     load_vecs<kUnroll>(raw, r, v0, kThreads, r.nvec);
     // pi = exp(z - lse): z - (float)lse is exact for the entries that count, what (float)lse lacks goes into the factor
     const float near = (float)lse;
-    const float f = (float)(-(double)c * (1.0 + ((double)near - lse)));
+    const double over = (double)near - lse;
+    const float f = (float)(-(double)c * (fabs(over) < kNearZero ? exp_series(over) : (double)ex2_approx((float)over * kLog2e)));
     const float2 nr = make_float2(-near, -near), l2 = make_float2(kLog2e, kLog2e), f2 = make_float2(f, f);
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) {

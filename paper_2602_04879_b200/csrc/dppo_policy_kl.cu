@@ -86,11 +86,12 @@ __device__ __forceinline__ uint32_t min_nan_bf16x2(uint32_t a, uint32_t b) {
 }
 
 // exp(d) without the rounding of d log2(e): what the product lost multiplies it by one plus that.  On average it is low by kExLow of itself (measured
-// as the KL's mean error, with and without it, on logits of standard deviation 1 and 3 in both types).  Zero where it vanishes: the product may have
-// overflowed there, and what it lost is then no number.
+// as the KL's mean error, with and without it, on logits of standard deviation 1 and 3 in both types).  (Far down the
+// product would overflow, and what it lost be no number.)
 __device__ __forceinline__ float exp_exact_arg(float d) {
+  d = max_nan(d, -200.f);
   const float x = d * kLog2e, v = ex2_approx(x);
-  return v == 0.f ? 0.f : fmaf(v, fmaf(x, -(float)kLn2, d), v);
+  return fmaf(v, fmaf(x, -(float)kLn2, d), v);
 }
 
 constexpr double kExLow = 1.5e-8;
@@ -139,46 +140,48 @@ __device__ __forceinline__ Coef finish_row(const PolicyParams& q, int64_t t, con
   const double total = w_tok + w_others;
   const double log_total = log(total);                   // -inf: no mass; NaN: a logit that is none
   const double p_tok = w_tok / total, p_others = w_others / total;
-  const double lse_l = big + log_total;
-  const bool fine = isfinite(lse_l) && (!have_tok || isfinite(tok));
+  const float lse_l = (float)(big + log_total);
+  const bool fine = isfinite(big + log_total) && (!have_tok || isfinite(tok));
+  // Log-probabilities, and what the rounded log-sum-exp is above the exact one, from differences with the maximum: logits may be far from zero.
+  const double lp_l = d_tok - log_total, above_l = ((double)lse_l - big) - log_total;
   auto of = [&](double v, int l) { return __shfl_sync(0xffffffffu, v, l); };
-  const double lse = of(lse_l, 0), lse_y = TWO ? of(lse_l, 1) : 0.0, pi_a = of(p_tok, 0), pi_o = of(p_others, 0);
+  const double above = of(above_l, 0), above_y = TWO ? of(above_l, 1) : 0.0, pi_a = of(p_tok, 0), pi_o = of(p_others, 0);
   const double rho_a = TWO ? of(p_tok, 1) : 0.0, rho_o = TWO ? of(p_others, 1) : 0.0;
   bool ok = __shfl_sync(0xffffffffu, (int)fine, 0) && (!TWO || __shfl_sync(0xffffffffu, (int)fine, 1));
-  double kl = 0.0, g = 0.0, r = 0.0, row_loss = 0.0;
+  double kl = 0.0, g = 0.0, r = 0.0, row_loss = 0.0, mu_a = 0.0;
   int M = 0;
   Coef co = {};
   if (ok) {
-    const double lp = z_a <= kLowest ? -INFINITY : (double)z_a - lse, b = s * (double)q.beta;
+    const double lp = of(lp_l, 0), b = s * (double)q.beta;
     const double ref = FORM == DPPO_KL_K3 ? (double)in.ref - lp : 0.0;
-    const double ex = FORM == DPPO_KL_K3 && lane == 1 ? expm1(ref) : exp(lp - (double)mu);
+    const double ex = FORM == DPPO_KL_K3 && lane == 1 ? expm1(ref) : exp(lane == 0 ? lp - (double)mu : (lane == 1 ? above_y : (lane == 2 ? above : (double)mu)));
     r = of(ex, 0);
+    mu_a = of(ex, 3);
+    const double fz = of(ex, 2);
     const double A = (double)adv, lo = 1.0 - (double)q.eps_low, hi = 1.0 + (double)q.eps_high;
     M = ((A > 0.0 && r > hi) || (A < 0.0 && r < lo)) ? 0 : 1;
     g = M ? s * r * A : 0.0;
     const double surrogate = M ? r * A : (A > 0.0 ? hi : lo) * A;
-    co.zr = (float)lse;
-    const double fz = 1.0 + ((double)co.zr - lse);       // e^(zr - lse)
+    co.zr = __shfl_sync(0xffffffffu, lse_l, 0);
     if (FORM == DPPO_KL_K3) {
       const double em = of(ex, 1), gk = g + b * em;
       kl = em - ref;
       co.A = (float)(gk * fz);
       co.fix = (float)(-gk * pi_o);
     } else {
-      // KL: sum over the other entries of probability * (difference of the log-probabilities, which is that of the logits less c), and the
-      // token's own term.  W is against mz - my.
-      const double c = lse - lse_y, shift = (double)mz - (double)my - c;
-      const double l_a = lp - ((y_a <= kLowest ? -INFINITY : (double)y_a) - lse_y);
-      co.yr = (float)lse_y;
+      // KL: sum over the other entries of probability * difference of the log-probabilities, and the token's own term.  W is against mz - my;
+      // shift is the difference of the log-probabilities that logits of mz and my would have.
+      const double top_l = d_top - log_total, shift = of(top_l, 0) - of(top_l, 1), l_a = lp - of(lp_l, 1);
+      co.yr = __shfl_sync(0xffffffffu, lse_l, 1);
       if (FORM == DPPO_KL_PI_REF) {
         kl = (pi_o > 0.0 ? pi_o * (W / S + shift) : 0.0) + (pi_a > 0.0 ? pi_a * l_a : 0.0);
         co.B = (float)(b * fz);
-        co.A = (float)(fz * (g + b * ((double)co.zr - (double)co.yr - c - kl)));
+        co.A = (float)(fz * (g + b * (above - above_y - kl)));
         co.fix = (float)(-g * pi_o + (pi_a > 0.0 ? b * pi_a * (l_a - kl) : 0.0));
       } else {
         kl = (rho_o > 0.0 ? rho_o * (W / Sy - shift) : 0.0) - (rho_a > 0.0 ? rho_a * l_a : 0.0);
         co.A = (float)(fz * (g + b));
-        co.B = (float)(b * (1.0 + ((double)co.yr - lse_y)));
+        co.B = (float)(b * of(ex, 1));
         co.fix = (float)(-g * pi_o + b * (pi_a - rho_a));
       }
     }
@@ -191,7 +194,7 @@ __device__ __forceinline__ Coef finish_row(const PolicyParams& q, int64_t t, con
     p.mask[t] = (uint8_t)M;
     p.row_loss[t] = (float)row_loss;
     p.row_r[t] = (float)r;
-    p.row_absdiff[t] = ok ? (float)fabs(exp((double)mu) - pi_a) : 0.f;
+    p.row_absdiff[t] = ok ? (float)fabs(mu_a - pi_a) : 0.f;
     if (!ok) atomicOr(p.status, DPPO_STATUS_NONFINITE_ROW);
   }
   co.mode = !ok ? kZeros : (w.rare != 0.f ? kCareful : kOrdinary);

@@ -91,6 +91,9 @@ template <> __device__ __forceinline__ void less_pairs<float>(const uint4& v, fl
   d[0] = __fadd2_rn(make_float2(__uint_as_float(v.x), __uint_as_float(v.y)), nm);
   d[1] = __fadd2_rn(make_float2(__uint_as_float(v.z), __uint_as_float(v.w)), nm);
 }
+// exp(d) for |d| < kNearZero, to 2^-41: for what a log-sum-exp loses when it is rounded to fp32, which is that little unless it is above 2^17
+constexpr double kNearZero = 0.0078125;
+__device__ __forceinline__ double exp_series(double d) { return 1.0 + d * (1.0 + d * (1.0 / 2 + d * (1.0 / 6 + d * (1.0 / 24)))); }
 __device__ __forceinline__ float warp_max_nan(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xffffffffu, v, o));
