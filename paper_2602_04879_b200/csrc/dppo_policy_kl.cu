@@ -49,15 +49,14 @@ constexpr int kMaxTeams = 2;
 constexpr int kThreads = 512, kWarps = kThreads / 32;      // of the kernel for any layout
 constexpr int kUnroll = 2;
 
-// what a warp knows of its part of a row
-struct Part { float mz, S, my, Sy, W, rare; };     // reference and sum of exp of z, the same of y, sum of exp times the difference; entries that are not ordinary
+// what a thread knows of its part of a row
+struct Part { float mz, S, my, Sy, W; };   // reference and sum of exp of z, the same of y, sum of exp times the difference
 // The same of a warp and of all of them.  From here on in 64 bits: the KL is what two large numbers leave, some 20 times smaller than they are.
-struct Sums { float mz, my, rare, pad; double S, Sy, W; };
+struct Sums { float mz, my; double S, Sy, W; };
 
 // Coefficients of the row's gradient: dz_j = e^(z_j - zr) (B ((z_j - zr) - (y_j - yr)) + A) for KL(pi || rho), e^(z_j - zr) A - B e^(y_j - yr) for
 // KL(rho || pi), A e^(z_j - zr) for k3, and its value at the token.  zr and yr are the two log-sum-exp, rounded.
-struct Coef { float zr, yr, A, B, fix; int mode; };
-enum { kZeros, kOrdinary, kCareful };      // careful: entries of probability zero may have differences that are infinite or no numbers
+struct Coef { float zr, yr, A, B, fix; int some; };        // some: 0 for a row of zeros
 
 // exp(z - m) of a vector's pairs; `arg` receives z - m
 template <typename T> __device__ __forceinline__ void exp_pairs(const uint4& z, float m, float2* arg, float2* e) {
@@ -197,7 +196,7 @@ __device__ __forceinline__ Coef finish_row(const PolicyParams& q, int64_t t, con
     p.row_absdiff[t] = ok ? (float)fabs(mu_a - pi_a) : 0.f;
     if (!ok) atomicOr(p.status, DPPO_STATUS_NONFINITE_ROW);
   }
-  co.mode = !ok ? kZeros : (w.rare != 0.f ? kCareful : kOrdinary);
+  co.some = ok;
   return co;
 }
 
@@ -211,7 +210,6 @@ __device__ __forceinline__ void masked_row(const RowParams& p, int64_t t, int a)
 // Adds NV vectors of z (and y) to a thread's sums: any entries, the references moved up to the maxima.
 template <typename InT, int FORM, int NV>
 __device__ __forceinline__ void add_careful(Part& w, uint4* zv, uint4* yv) {
-  w.rare = 1.f;
   constexpr bool TWO = FORM != DPPO_KL_K3;
   constexpr int N = Vec<InT>::N;
   RawMax<InT> mz, my;
@@ -341,32 +339,32 @@ __device__ __forceinline__ Sums merge_lanes(const Sums& w) {
     r.Sy = warp_sum(fy != 0.0 ? fy * w.Sy : 0.0);
     r.W = warp_sum(FORM == DPPO_KL_PI_REF ? (fz != 0.0 ? fz * fma(w.S, (double)off, w.W) : 0.0) : (fy != 0.0 ? fy * fma(-w.Sy, (double)off, w.W) : 0.0));
   }
-  r.rare = __any_sync(0xffffffffu, w.rare != 0.f) ? 1.f : 0.f;
   return r;
 }
 template <int FORM>
 __device__ __forceinline__ Sums merge_lanes(const Part& w) {
-  return merge_lanes<FORM>(Sums{w.mz, w.my, w.rare, 0.f, (double)w.S, (double)w.Sy, (double)w.W});
+  return merge_lanes<FORM>(Sums{w.mz, w.my, (double)w.S, (double)w.Sy, (double)w.W});
 }
 
-// The gradient of one vector.
-template <typename InT, int FORM, bool CAREFUL>
+// The gradient of one vector.  (Two tensors: an entry of probability zero may lie infinitely far from its other logit; the token's own entry, which the
+// sums leave out as such a one, makes no difference here.)
+template <typename InT, int FORM>
 __device__ __forceinline__ void grad_vector(const Coef& co, const uint4& zv, const uint4& yv, float* out) {
   constexpr bool TWO = FORM != DPPO_KL_K3;
   constexpr int N = Vec<InT>::N;
   const float2 A2 = make_float2(co.A, co.A), B2 = make_float2(co.B, co.B), nB = make_float2(-co.B, -co.B), neg = make_float2(-1.f, -1.f);
   float2 az[N / 2], ez[N / 2];
-  exp_pairs<InT>(TWO && CAREFUL ? clamp_raw<InT>(zv) : zv, co.zr, az, ez);
+  exp_pairs<InT>(TWO ? clamp_raw<InT>(zv) : zv, co.zr, az, ez);
   if (TWO) {
-    const uint4 yc = CAREFUL ? clamp_raw<InT>(yv) : yv;
+    const uint4 yc = clamp_raw<InT>(yv);
     float2 ay[N / 2], ey[N / 2];
     if (FORM == DPPO_KL_REF_PI) exp_pairs<InT>(yc, co.yr, ay, ey); else less_pairs<InT>(yc, co.yr, ay);
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) {
       if (FORM == DPPO_KL_PI_REF) {
         const float2 d = __ffma2_rn(ay[i], neg, az[i]);
-        // careful: (e B) first, so that an entry of probability zero stays zero however large its difference is
-        ez[i] = CAREFUL ? __ffma2_rn(__fmul2_rn(ez[i], B2), d, __fmul2_rn(ez[i], A2)) : __fmul2_rn(ez[i], __ffma2_rn(d, B2, A2));
+        // (e B) first, so that an entry of probability zero stays zero however large its difference is
+        ez[i] = __ffma2_rn(__fmul2_rn(ez[i], B2), d, __fmul2_rn(ez[i], A2));
       } else {
         ez[i] = __ffma2_rn(ey[i], nB, __fmul2_rn(ez[i], A2));
       }
@@ -521,7 +519,7 @@ __global__ void __launch_bounds__(kRingThreads<FORM != DPPO_KL_K3>, 1) policy_kl
       if (a >= 0) {
         const Geom g = geom_of<InT>(p, t);
         const int av = (a + g.head) / N, ai = (a + g.head) % N;        // the token's vector, and its place there
-        Part w{kLowest, 0.f, kLowest, 0.f, 0.f, 0.f};
+        Part w{kLowest, 0.f, kLowest, 0.f, 0.f};
         for (int c = rank; c < C; c += CL) {
           const bool mine = TEAMS == 1 || turn == team;
           turn = turn + 1 == TEAMS ? 0 : turn + 1;
@@ -601,9 +599,9 @@ __global__ void __launch_bounds__(kRingThreads<FORM != DPPO_KL_K3>, 1) policy_kl
         const bool have = mbar_wait_warp(coef_full + 8u * b, u & 1u, wc);
         Coef co = misc->coef[b];
         // (a vote on what was read, whatever its answer: the arrival is not to be moved up before the loads)
-        if ((!__any_sync(0xffffffffu, co.zr + co.yr + co.A + co.B + co.fix == 1.f && co.mode == kCareful) || p.V > 0) && lane == 0 && have)
+        if ((!__any_sync(0xffffffffu, co.zr + co.yr + co.A + co.B + co.fix == 1.f && co.some) || p.V > 0) && lane == 0 && have)
           mbar_arrive(coef_empty + 8u * b);
-        if (!have) co.mode = kZeros;
+        if (!have) co.some = 0;
         ++n;
         const int av = (a + head) / N;
         OutT* image = rd.row - head;       // where vector 0 goes, whole or not
@@ -618,22 +616,22 @@ __global__ void __launch_bounds__(kRingThreads<FORM != DPPO_KL_K3>, 1) policy_kl
               zv[k] = lds128(sz + (uint32_t)k * (16u * kTeam));
               if (TWO) yv[k] = lds128(sz + CHUNK + (uint32_t)k * (16u * kTeam));
             }
-            if (co.mode == kOrdinary && c * VECS >= rd.lo && (c + 1) * VECS <= rd.hi) {
+            if (co.some && c * VECS >= rd.lo && (c + 1) * VECS <= rd.hi) {
 #pragma unroll
               for (int k = 0; k < PER; ++k) {
                 float out[N];
-                grad_vector<InT, FORM, false>(co, zv[k], TWO ? yv[k] : zv[k], out);
+                grad_vector<InT, FORM>(co, zv[k], TWO ? yv[k] : zv[k], out);
                 Store<OutT, N>::run(image + (int64_t)(v0 + k * kTeam) * N, 0u, out);
               }
             } else {
 #pragma unroll
               for (int k = 0; k < PER; ++k) {
                 float out[N] = {};
-                if (co.mode != kZeros) grad_vector<InT, FORM, true>(co, zv[k], TWO ? yv[k] : zv[k], out);
+                if (co.some) grad_vector<InT, FORM>(co, zv[k], TWO ? yv[k] : zv[k], out);
                 if (v0 + k * kTeam < rd.nvec) store_vec<OutT, N>(rd, v0 + k * kTeam, out);
               }
             }
-            if (co.mode != kZeros && av >= c * VECS && av < (c + 1) * VECS && (av - v0) % kTeam == 0) rd.row[a] = from_f32<OutT>(co.fix);
+            if (co.some && av >= c * VECS && av < (c + 1) * VECS && (av - v0) % kTeam == 0) rd.row[a] = from_f32<OutT>(co.fix);
           }
           __syncwarp();
           if (lane == 0) mbar_arrive(gempty + 8u * pos.slot);
@@ -659,7 +657,7 @@ __global__ void __launch_bounds__(kRingThreads<FORM != DPPO_KL_K3>, 1) policy_kl
         const uint32_t b = (n - 1) % kHand, u = (n - 1) / kHand;
         const RowIn in = row_in<InT, FORM>(q, t, a);
         bool have = mbar_wait_warp(part_full + 8u * b, u & 1u, wc);
-        const Sums none{kLowest, kLowest, 0.f, 0.f, 0.0, 0.0, 0.0};
+        const Sums none{kLowest, kLowest, 0.0, 0.0, 0.0};
         Sums w = have && lane < TEAMS * kTeamWarps ? misc->part[b][lane] : none;
         w = merge_lanes<FORM>(w);
         if (lane == 0 && have) mbar_arrive(part_empty + 8u * b);           // (behind the exchange between the lanes: all have what they read)
@@ -670,10 +668,9 @@ __global__ void __launch_bounds__(kRingThreads<FORM != DPPO_KL_K3>, 1) policy_kl
           if (have && lane < CL) {
             const uint32_t dst = map_to_cta(smem_u32(&misc->x_part[b][rank]), (uint32_t)lane);
             st_cluster_f32x2(dst, w.mz, w.my);
-            st_cluster_f32x2(dst + 8, w.rare, 0.f);
-            st_cluster_f64(dst + 16, w.S);
-            st_cluster_f64(dst + 24, w.Sy);
-            st_cluster_f64(dst + 32, w.W);
+            st_cluster_f64(dst + 8, w.S);
+            st_cluster_f64(dst + 16, w.Sy);
+            st_cluster_f64(dst + 24, w.W);
             bar_arrive_cluster(map_to_cta(xf, (uint32_t)lane));
           }
           if (have) have = __all_sync(0xffffffffu, mbar_wait_cluster(xf, u & 1u, wc));
@@ -724,7 +721,7 @@ __global__ void __launch_bounds__(kThreads) policy_kl_kernel(const __grid_consta
     const RowIn in = row_in<InT, FORM>(q, t, a);
     const int av = (int)(((uint32_t)a + head) / N), ai = (int)(((uint32_t)a + head) % N);
     uint4 zv[kUnroll], yv[TWO ? kUnroll : 1];
-    Part w{kLowest, 0.f, kLowest, 0.f, 0.f, 0.f};
+    Part w{kLowest, 0.f, kLowest, 0.f, 0.f};
     for (int v0 = tid; v0 - tid < rz.nvec; v0 += kUnroll * kThreads) {
       load_vecs<kUnroll>(zv, rz, v0, kThreads, rz.nvec);
       if (TWO) load_vecs<kUnroll>(yv, ry, v0, kThreads, rz.nvec);
@@ -744,13 +741,13 @@ __global__ void __launch_bounds__(kThreads) policy_kl_kernel(const __grid_consta
     if (lane == 0) parts[warp] = sums;
     __syncthreads();
     if (warp == 0) {
-      sums = merge_lanes<FORM>(lane < kWarps ? parts[lane] : Sums{kLowest, kLowest, 0.f, 0.f, 0.0, 0.0, 0.0});
+      sums = merge_lanes<FORM>(lane < kWarps ? parts[lane] : Sums{kLowest, kLowest, 0.0, 0.0, 0.0});
       const Coef co = finish_row<FORM>(q, t, in, sums, lane, q.scale > 0.0 ? q.scale : p.hdr->scale, true);
       if (lane == 0) s_coef = co;
     }
     __syncthreads();
     const Coef co = s_coef;
-    if (co.mode == kZeros) {
+    if (!co.some) {
       zero_row<OutT, N>(rd, 0, 1, kThreads);
       continue;
     }
@@ -762,7 +759,7 @@ __global__ void __launch_bounds__(kThreads) policy_kl_kernel(const __grid_consta
         const int v = v0 + k * kThreads;
         if (v >= rz.nvec) break;
         float out[N];
-        grad_vector<InT, FORM, true>(co, zv[k], TWO ? yv[k] : zv[k], out);
+        grad_vector<InT, FORM>(co, zv[k], TWO ? yv[k] : zv[k], out);
         store_vec<OutT, N>(rd, v, out);
       }
     }
