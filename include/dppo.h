@@ -459,7 +459,7 @@ int dppo_token_logp_bwd(const void* logits, int64_t T, int64_t V, int64_t logits
  *                 overlap on the GPU need one each.
  * Rows whose KL or loss term is infinite (pi has mass where rho has none, or the reverse for KL(rho || pi)) are dropped with
  * DPPO_STATUS_NONFINITE_ROW, as rows with non-finite logits in either tensor are.  A KL of 1e30 or more counts as infinite, and one with
- * terms whose two log-probabilities are that far apart may.
+ * terms whose two log-probabilities are that far apart may; so does a loss term, or a derivative by a logit, that is infinite in fp32.
  */
 int dppo_policy_kl_fwd_bwd(const void* logits, int64_t T, int64_t V, int64_t logits_row_stride, int logits_dtype,
                            const void* ref_logits, int64_t ref_row_stride, const float* ref_logp,

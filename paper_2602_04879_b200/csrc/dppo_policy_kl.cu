@@ -185,7 +185,8 @@ __device__ __forceinline__ Coef finish_row(const PolicyParams& q, int64_t t, con
       }
     }
     row_loss = s * ((double)q.beta * kl - surrogate);
-    ok = fabs(kl) < 1e30 && isfinite(row_loss) && isfinite(g);
+    // (in fp32, which is what the row's numbers are handed on in: an infinite coefficient times nothing would be no number)
+    ok = fabs(kl) < 1e30 && isfinite((float)row_loss) && isfinite(co.A) && isfinite(co.B) && isfinite(co.fix);
   }
   if (!ok) { kl = r = row_loss = 0.0; M = 0; }
   if (write && lane == 0) {
