@@ -226,10 +226,11 @@ struct MatvecParams {
 // Two ways to the same sums:
 //   bf16   A word of 8 codes c0 .. c7 gives the pairs (c0, c4), (c1, c5), (c2, c6), (c3, c7): a mask and an or put a code into the low mantissa bits of
 //          the bf16 number 128, and subtracting 136 leaves code - 8, exactly.  11 instructions a word, chunks of 128 codes.
-//   int8   (up to 4 rows of x) The codes stay whole numbers: two masks and a shift give a word's 8 bytes.  x is written as three signed 8-bit digits in
-//          units of 2^-22 of (a power of two above) the largest entry of its group, a row of the operand each; the int32 products are exact, and
-//          8 times the sum of the digits is taken off, exactly.  What is lost of x is below 2^-23 of the group's largest entry: less than
-//          fp32 sums lose.
+//   int8   (up to 4 rows of x) The codes stay whole numbers: two masks and a shift give a word's 8 bytes.  x is written as four signed 8-bit digits in
+//          units of 2^-29 of the power of two at the largest entry of its group, a row of the operand each; the int32 products are exact, and
+//          8 times the sum of the digits is taken off, exactly.  That holds entries down to 2^-22 of the largest with all of their 8 bits.  A group
+//          with smaller ones, which may be all of its sum where the large one's weight is zero, is summed by the products' threads from x and
+//          the codes as they stand, in fp32.  (Of groups of standard normal x one in 20000 to 80000.)
 //
 // What bounds it, 151936 x 2048 in groups of 128 (166 MB; 25 us at the measured copy rate), calls back to back:
 //   1 row     31 us.  A launch, x and the first weights take 5 us; then 4 warps convert, and 8 take the products of, 256 codes of 115 rows in some 650
@@ -246,7 +247,7 @@ namespace mv {
 
 constexpr int LANES = 128;                 // rows of a tile at most
 constexpr int STAGE_BYTES = LANES * 128;   // 256 codes of each row
-constexpr int DIGITS = 3;
+constexpr int DIGITS = 4;
 
 struct Params {
   const __nv_bfloat16* x;
@@ -260,14 +261,16 @@ struct Params {
   int rows, stages, seg, nseg, groups;     // rows of a tile; seg: codes of K that x lies in shared memory for (a multiple of 256), nseg of them to a CTA
   int pairs;                               // blocks of 256 codes of a CTA
   int scales_together;                     // a chunk's scales lie on a boundary of their size
+  const unsigned char* q;                  // the codes once more, for groups that are summed without the tensor cores
+  int64_t ldq;
   int32_t* status;
   unsigned long long wait_ns;
   int inject;
 };
 
-// NT: columns of an MMA (bf16: rows of x; int8: four to a row of x, of which DIGITS count)
+// NT: columns of an MMA (bf16: rows of x; int8: DIGITS to a row of x)
 template <int NT, int G, bool I8> struct Shape {
-  static constexpr int XROWS = I8 ? 4 : NT;                            // rows of x
+  static constexpr int XROWS = I8 ? NT / DIGITS : NT;                            // rows of x
   static constexpr int CHUNK = I8 ? 256 : 128, PER = 256 / CHUNK;      // codes that a thread converts at a time; chunks of a stage
   static constexpr int STEP = I8 ? 32 : 16;                            // codes of an MMA
   static constexpr int XBYTES = I8 ? NT : 2 * NT;                      // of shared memory for a code
@@ -407,10 +410,11 @@ __device__ __forceinline__ void load_x(const Params& p, unsigned char* xs, int m
 }
 
 // int8: the same for XROWS rows as digits (row 4 m + digit of the operand) in blocks of 128 codes, and for each group and row of x what
-// the products need: 2^22 + 2^23 - 8 times the sum of each digit (see the products), and the group's unit.  A warp per row and group.  An
-// entry that is no number, or infinite, makes the unit NaN.
+// the products need: -8 times the sum of the lower two digits (the second 256-fold) and of the upper two, and the group's unit.  A warp per row and
+// group.  A group with an entry that is no whole number of units has zeros for digits and a negative unit, and is announced.  An entry that is no number,
+// or infinite, makes the unit NaN.
 template <int NT, int XROWS, int G, int WARPS>
-__device__ __forceinline__ void load_x_digits(const Params& p, unsigned char* xs, int4* table, int m0, int k0, int warp, int lane) {
+__device__ __forceinline__ void load_x_digits(const Params& p, unsigned char* xs, int4* table, int* odd, int m0, int k0, int warp, int lane) {
   constexpr int AT_ONCE = 4;
   const int rows = min(XROWS, p.M - m0), all = p.seg / G * rows;           // (columns of rows that there are not are never read)
   for (int u0 = warp; u0 < all; u0 += AT_ONCE * WARPS) {
@@ -433,17 +437,25 @@ __device__ __forceinline__ void load_x_digits(const Params& p, unsigned char* xs
       for (int j = 0; j < G / 32; ++j) top = max_nan(top, fabsf(v[a][j]));
       top = warp_max_nan(top);
       const bool bad = !(top <= 3.4028234e38f);
-      // unit 2^(e - 21) for a largest entry in [2^e, 2^(e + 1)); tiny groups in units of 2^-121
-      const int e = max((int)(__float_as_uint(top) >> 23) - 127, -100);
-      const float up = __uint_as_float((uint32_t)(127 + 21 - e) << 23), unit = bad ? NAN : __uint_as_float((uint32_t)(127 + e - 21) << 23);
+      // unit 2^(e - 29) for a largest entry in [2^e, 2^(e + 1)), not below 2^-133, of which every bf16 number is a multiple; 1 / unit in two steps, as it
+      // may be beyond fp32
+      const int e = max((int)(__float_as_uint(top) >> 23) - 127, -104);
+      const float up = __uint_as_float((uint32_t)(127 + 21 - e) << 23);
+      bool whole = true;
+#pragma unroll
+      for (int j = 0; j < G / 32; ++j) {
+        v[a][j] = v[a][j] * up * 256.f;
+        whole = whole && rintf(v[a][j]) == v[a][j];
+      }
+      whole = __all_sync(0xffffffffu, whole);
       int sum[DIGITS] = {};
 #pragma unroll
       for (int j = 0; j < G / 32; ++j) {
-        int X = bad ? 0 : __float2int_rn(v[a][j] * up);
+        int X = whole ? __float2int_rn(v[a][j]) : 0;
         const int k = kg + 32 * j + lane, byte = (k & 127 & ~7) + ((k & 1) * 4 + ((k & 7) >> 1));
 #pragma unroll
         for (int d = 0; d < DIGITS; ++d) {
-          const int digit = d == DIGITS - 1 ? X : ((X + 128) & 255) - 128, row = 4 * m + d;
+          const int digit = d == DIGITS - 1 ? X : ((X + 128) & 255) - 128, row = DIGITS * m + d;
           X = (X - digit) >> 8;
           sum[d] += digit;
           xs[k / 128 * (NT * 128) + row * 128 + (byte ^ ((row & 7) << 4))] = (unsigned char)digit;
@@ -451,10 +463,29 @@ __device__ __forceinline__ void load_x_digits(const Params& p, unsigned char* xs
       }
 #pragma unroll
       for (int d = 0; d < DIGITS; ++d) sum[d] = __reduce_add_sync(0xffffffffu, sum[d]);
-      if (lane == 0) table[gi * XROWS + m] = make_int4(0x4B400000 - 8 * sum[0], 0x4B400000 - 8 * sum[1], 0x4B400000 - 8 * sum[2], (int)__float_as_uint(unit));
+      const uint32_t unit = e >= -97 ? (uint32_t)(127 + e - 29) << 23 : 1u << (e + 120);
+      if (lane == 0) {
+        table[gi * XROWS + m] = make_int4(-8 * (sum[0] + 256 * sum[1]), -8 * (sum[2] + 256 * sum[3]), (int)(bad ? 0x7fc00000u : (whole ? unit : unit | 0x80000000u)), 0);
+        if (!whole && !bad) *odd = 1;
+      }
     }
   }
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+}
+
+// The sum of a group as it stands: n entries of x, their codes from q on, on a 16-byte boundary.
+template <int G> __device__ __noinline__ float group_sum(const __nv_bfloat16* x, const unsigned char* q, int n) {
+  float s = 0.f;
+  if (n >= G) {
+    uint4 w[G / 32];
+#pragma unroll
+    for (int j = 0; j < G / 32; ++j) w[j] = *reinterpret_cast<const uint4*>(q + 16 * j);
+#pragma unroll
+    for (int j = 0; j < G; ++j) s = fmaf(__bfloat162float(x[j]), (float)((int)(word_of(w[j / 32], j / 8 % 4) >> (4 * (j % 8)) & 15u) - 8), s);
+  } else {
+    for (int j = 0; j < n; ++j) s = fmaf(__bfloat162float(x[j]), (float)((int)(q[j / 2] >> (4 * (j % 2)) & 15u) - 8), s);
+  }
+  return s;
 }
 
 struct Bars {
@@ -465,6 +496,7 @@ struct Bars {
   unsigned long long sum_full[2], sum_free[2];       // pairs of CTAs, by whose turn it is: the other's sums are here; read by the other
   uint32_t tmem;
   int abort_flag;
+  int odd;                                 // int8: x has a group that digits do not hold
 };
 
 template <int NT, int G, int CL, bool I8>
@@ -491,6 +523,7 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
     for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&bars->turn[i]), 4 * S::E);
     for (int i = 0; i < TURNS; ++i) { mbar_init(smem_u32(&bars->sum_full[i]), 1); mbar_init(smem_u32(&bars->sum_free[i]), 4 * S::E); }
     bars->abort_flag = 0;
+    bars->odd = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -582,7 +615,7 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
           if (lane == 0) mbar_arrive(x_free);
           if (!mbar_wait_warp(x_free, n_x & 1u, wc)) { ok = false; break; }
           const int k0 = (pair0 + seg * (p.seg / 256)) * 256;
-          if (I8) load_x_digits<NT, XROWS, G, L * 4>(p, xs, table, block * XROWS, k0, warp - 1 - L, lane);
+          if (I8) load_x_digits<NT, XROWS, G, L * 4>(p, xs, table, &bars->odd, block * XROWS, k0, warp - 1 - L, lane);
           else load_x<NT, L * 4>(p, xs, block * XROWS, k0, warp - 1 - L, lane);
           __syncwarp();
           if (lane == 0) mbar_arrive(x_full);
@@ -725,11 +758,10 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
               asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
               if (I8) {
                 float* a = reinterpret_cast<float*>(acc);
-                // v - 8 (sum of the digits) is below 2^22 in magnitude: added to the bits of 1.5 2^23 it gives that number plus it
                 auto add = [&](const uint32_t* v, int m, float s1, const int4& t) {
-                  const float d0 = __int_as_float((int)v[0] + t.x) - 12582912.f, d1 = __int_as_float((int)v[1] + t.y) - 12582912.f;
-                  const float d2 = __int_as_float((int)v[2] + t.z) - 12582912.f;
-                  a[m] = fmaf(s1 * __int_as_float(t.w), fmaf(d2, 65536.f, fmaf(d1, 256.f, d0)), a[m]);
+                  // the lower and the upper half of the sum: below 2^25 in magnitude; times a power of two, in fp32's range wherever the sum is: exact
+                  const float low = (float)((int)v[0] + 256 * (int)v[1] + t.x), high = (float)((int)v[2] + 256 * (int)v[3] + t.y);
+                  a[m] = fmaf(s1, fmaf(high, 65536.f, low) * fabsf(__int_as_float(t.z)), a[m]);
                 };
                 if (p.M == 1) {            // a single row: its digits only
                   uint32_t v[NG][4];
@@ -782,6 +814,21 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
         }
       }
       if (!ok) break;
+      if (I8 && bars->odd) {               // the groups that digits do not hold (here, so that the loop above is rid of them: 4 rows 41 us, with them 45)
+        float* a = reinterpret_cast<float*>(acc);
+        for (int base = 0; base < per_tile * NG * XROWS; base += 32) {
+          const int at = base + lane;
+          const bool such = at < per_tile * NG * XROWS && at / (NG * XROWS) % SPLIT == begin && m0 + at % XROWS < p.M && table[at].z < 0;
+          for (uint32_t left = __ballot_sync(0xffffffffu, such); left; left &= left - 1u) {
+            const int i = base + __ffs((int)left) - 1, gi = i / XROWS, m = i % XROWS, k = pair0 * 256 + gi * G;
+            if (!live) continue;
+            const float sum = __bfloat162float(p.scale[(int64_t)n * p.lds + g0 + gi]) *
+                              group_sum<G>(p.x + (int64_t)(m0 + m) * p.ldx + k, p.q + (int64_t)n * p.ldq + k / 2, p.K - k);
+#pragma unroll
+            for (int r = 0; r < XROWS; ++r) a[r] += r == m ? sum : 0.f;
+          }
+        }
+      }
       if (TURNS > 1) {
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bars->turn[turn ^ 1]));
@@ -908,6 +955,7 @@ cudaError_t launch_cl(Params p, const unsigned char* q, int64_t ldq, int sms, in
   constexpr int FIXED = Room<NT, G, CL, I8>::FIXED, X256 = Room<NT, G, CL, I8>::X256;
   const int room = smem_most - FIXED, total = (p.K + 255) / 256;
   p.pairs = (total + CL - 1) / CL;
+  p.q = q; p.ldq = ldq;
   p.scales_together = (uintptr_t)p.scale % (2 * S::NG) == 0 && (p.N == 1 || p.lds % S::NG == 0);
   // x for all of this CTA's K where at least four stages are left besides it, else as much as leaves that many
   const int most = x_blocks<NT, G, CL, I8>(smem_most);
