@@ -856,7 +856,7 @@ extern "C" int dppo_policy_kl_fwd_bwd(const void* logits, int64_t T, int64_t V, 
   if (logits_dtype != DPPO_F32 && logits_dtype != DPPO_BF16) return DPPO_ERR_DTYPE;
   if (o.dlogits_dtype != DPPO_DLOGITS_SAME && o.dlogits_dtype != DPPO_DLOGITS_F32) return DPPO_ERR_DTYPE;
   if (kl_form < DPPO_KL_PI_REF || kl_form > DPPO_KL_K3) return DPPO_ERR_VARIANT;
-  if (!(kl_coef >= 0.f) || !isfinite(kl_coef) || !(eps_low >= 0.f) || !(eps_high >= 0.f)) return DPPO_ERR_UNSUPPORTED;
+  if (!(kl_coef >= 0.f) || !isfinite(kl_coef) || !(eps_low >= 0.f) || !(eps_high >= 0.f) || o.wait_limit_us < 0) return DPPO_ERR_UNSUPPORTED;
   const bool two = kl_form != DPPO_KL_K3;
   if (!loss || !status) return DPPO_ERR_NULL;
   if (T > 0 && (!logits || !sampled_ids || !mu_logp || !advantages || !kl || !mask || !dlogits || (two ? !ref_logits : !ref_logp))) return DPPO_ERR_NULL;
