@@ -27,6 +27,8 @@
 //
 // The token's own entry is left out of the sums and added in 64 bits, so that 1 - pi(a) keeps its relative accuracy.  Differences enter the
 // sums as (z - max z) - (y - max y): the KL, a small difference of large sums, then does not depend on offsets between z and y.
+#include <atomic>
+
 #include "dppo_rowvec.cuh"
 
 namespace dppo {
@@ -805,9 +807,9 @@ cudaError_t launch_form(const PolicyParams& q, bool ring, cudaStream_t st) {
   int64_t clusters = sms;
   if (CL > 1) {
     // as many clusters as the device runs at a time (asked once per device and size)
-    static int known[64][4] = {};
+    static std::atomic<int> known[64][4] = {};         // (calls may come from several threads)
     const int li = CL == 2 ? 1 : (CL == 4 ? 2 : 3);
-    int nc = dev >= 0 && dev < 64 ? known[dev][li] : 0;
+    int nc = dev >= 0 && dev < 64 ? known[dev][li].load() : 0;
     if (nc <= 0) {
       attr[0].val.clusterDim.x = (unsigned)CL;
       cfg.numAttrs = 1;
@@ -866,7 +868,9 @@ extern "C" int dppo_policy_kl_fwd_bwd(const void* logits, int64_t T, int64_t V, 
   if ((uintptr_t)sampled_ids % 4 || (uintptr_t)mu_logp % 4 || (uintptr_t)advantages % 4 || (uintptr_t)ref_logp % 4 || (uintptr_t)loss % 4 ||
       (uintptr_t)kl % 4 || (uintptr_t)stats % 4 || (uintptr_t)status % 4) return DPPO_ERR_ALIGN;
   if (T > 0) {
-    // the gradient in place of the logits is fine (a cluster holds its row before it writes); any other overlap is not
+    // The gradient in place of the logits is fine: a row's sums are complete before its coefficients are, a slot's gradient is written by the CTA that
+    // has just read the slot for the second time, and of a 16-byte vector that two rows share each takes and writes its own entries.  Any other
+    // overlap is not.
     const size_t nz = ((size_t)(T - 1) * logits_row_stride + V) * esize(logits_dtype), nd = ((size_t)(T - 1) * dlogits_row_stride + V) * esize(out_dtype);
     const bool in_place = dlogits == logits && out_dtype == logits_dtype && (T == 1 || dlogits_row_stride == logits_row_stride);
     if (!in_place && overlap(logits, nz, dlogits, nd)) return DPPO_ERR_ALIAS;

@@ -26,3 +26,30 @@ def test_rows_whose_term_leaves_fp32_are_dropped(dtype, V, form):
     k["mu"][3] = mu[3] - 3.0                 # the same term and gradient, with a ratio that the tolerances can go by
     k["adv"][5] = 0.0
     check_policy(k, o, form, valid=np.array([1, 0, 1, 1, 1, 0], bool), scale=1.0 / 6)
+
+
+def test_calls_from_several_threads_share_nothing():
+    """Few rows, shared by clusters of every size: the first calls of each shape ask the device how many of them it runs."""
+    import threading
+    cases = [policy_case(T, V, BF, seed=T + V, masked=False) for T, V in ((3, 9000), (30, 20488), (70, 40000), (2, 151936))]
+    wrong = []
+
+    def work(i):
+        st = torch.cuda.Stream("cuda:0")
+        try:
+            with torch.cuda.stream(st):
+                first = run_policy(cases[i], "pi_ref", mask=False)
+                for _ in range(30):
+                    o = run_policy(cases[i], "pi_ref", mask=False)
+                    if not all(torch.equal(o[n], first[n]) for n in ("loss", "kl", "dlogits")):
+                        wrong.append((i, "result"))
+                check_policy(cases[i], first, "pi_ref")
+        except Exception as e:             # noqa: BLE001 (reported below)
+            wrong.append((i, repr(e)[:300]))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(cases))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong, wrong[:3]
