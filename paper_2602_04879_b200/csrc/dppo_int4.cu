@@ -230,7 +230,8 @@ struct MatvecParams {
 //          units of 2^-29 of the power of two at the largest entry of its group, a row of the operand each; the int32 products are exact, and
 //          8 times the sum of the digits is taken off, exactly.  That holds entries down to 2^-22 of the largest with all of their 8 bits.  A group
 //          with smaller ones, which may be all of its sum where the large one's weight is zero, is summed by the products' threads from x and
-//          the codes as they stand, in fp32.  (Of groups of standard normal x one in 20000 to 80000.)
+//          the codes as they stand, in fp32.  (Of groups of standard normal x one in 20000 to 80000.  151936 x 2048, one row: 31 us, with one
+//          such group of the 16 49 us, with nothing else 191 us.)
 //
 // What bounds it, 151936 x 2048 in groups of 128 (166 MB; 25 us at the measured copy rate), calls back to back:
 //   1 row     31 us.  A launch, x and the first weights take 5 us; then 4 warps convert, and 8 take the products of, 256 codes of 115 rows in some 650
@@ -239,8 +240,9 @@ struct MatvecParams {
 //             16 words x 11 instructions of conversion, and the products' warps some 100 each around their sums.  The tensor cores are not the
 //             bound: an MMA takes 47 cycles with up to 96 columns, of bf16 (K = 16) as of int8 (K = 32): 374 cycles a chunk for bf16, 187 for int8, of
 //             the 760 that it takes.
+// Up to four rows, groups of 128: 31, 35, 41 us for 1, 2, 4 rows; groups of 32: 44 us for one row, 90 for four.
 // Tried and left: the chunks' products in rotation over two or three parts for bf16 (32 rows 64 -> 72 us: more warps for the same issue slots), three or
-// four lines for int8 (31 -> 33 us), int8 for 8 and 16 rows (see launch_rows).
+// four lines for int8 (31 -> 33 us), int8 for 8 and 16 rows (see launch_rows), groups that digits do not hold within the loop over chunks.
 //
 // x is laid out in the order that the conversion makes of k.
 namespace mv {
@@ -683,7 +685,7 @@ __global__ void __launch_bounds__(Shape<NT, G, I8>::THREADS, 1) matvec_int4_kern
     };
     // (a register each, and the loads by predicate: nothing here may wait for them)
     uint32_t sc[AHEAD][NG];
-    // int8, four or eight groups to a chunk: all at once where they lie so (two to a register then; groups of 32, one row: 64 -> 56 us).
+    // int8, four or eight groups to a chunk: all at once where they lie so (two to a register then; groups of 32, one row: 64 -> 56 us when x had three digits, 43 us now).
     constexpr bool MANY = I8 && NG >= 4;
     const bool together = MANY && p.scales_together;
     auto fetch = [&](const unsigned short* row, int c, uint32_t* to) {
@@ -1007,8 +1009,8 @@ cudaError_t launch(const Params& p, const unsigned char* q, int64_t ldq, int sms
 }
 
 // Rows of x that one pass over the weights serves.  (Of 64 rows and groups of 32 the products would not fit tensor memory.)  Up to four rows as integers: a
-// tile's int8 MMAs take half as long and its conversion a third of the instructions; above that the products take more than is saved (8 rows
-// 69 us against 54, 16 rows 135 against 55, at 151936 x 2048).
+// tile's int8 MMAs take half as long and its conversion a third of the instructions; above that the products take more than is saved (with
+// three digits 8 rows 69 us against 54, 16 rows 135 against 55, at 151936 x 2048).
 template <int G>
 cudaError_t launch_rows(const Params& p, const unsigned char* q, int64_t ldq, int sms, int smem_most, cudaStream_t st) {
   if (p.M <= 4) return launch<16, G, true>(p, q, ldq, sms, smem_most, st);

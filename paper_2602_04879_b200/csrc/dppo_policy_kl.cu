@@ -21,9 +21,9 @@
 // All waits are bounded.
 // policy_kl_kernel, any layout: a CTA per row, one role after the other.
 //
-// 4096 x 151936 bf16: k3 455 us, 85 % of the measured copy rate over one read and one write of the logits; the KL from logits 868 us, 67 % over two reads
-// and a write.  The ring alone, without any arithmetic, takes 722 to 774 us of the latter; 63 % of the issue slots are busy.  Rows held in
-// registers of a cluster between the two uses (850 and 1976 us), or handed out by a queue to whichever SM is free, were slower.
+// 4096 x 151936 bf16, back to back: k3 443 us, 87 % of the measured copy rate over one read and one write of the logits; KL(pi || rho) 827 us, 70 % over two
+// reads and a write, KL(rho || pi) 887 us.  The ring alone, without any arithmetic, takes 722 to 774 us of the latter; 62 % of the issue slots are busy.
+// Rows held in registers of a cluster between the two uses (850 and 1976 us), or handed out by a queue to whichever SM is free, were slower.
 //
 // The token's own entry is left out of the sums and added in 64 bits, so that 1 - pi(a) keeps its relative accuracy.  Differences enter the
 // sums as (z - max z) - (y - max y): the KL, a small difference of large sums, then does not depend on offsets between z and y.
@@ -42,7 +42,7 @@ constexpr int kAhead = 11;                 // slots by which the sums may lead t
 constexpr int kHand = kScalarWarps;        // rows on their way from the sums to the gradient
 constexpr int kMaxCluster = 8;
 // teams that take the sums' slots in turn: the two exponentials an entry of two tensors keep one team busy too long (8 KB of each tensor,
-// 4096 x 151936 bf16: 921 us with one, 868 with two)
+// 4096 x 151936 bf16, KL(pi || rho): 909 us with one, 837 with two)
 template <bool TWO> constexpr int kSumTeams = TWO ? 2 : 1;
 template <bool TWO> constexpr int kRingThreads = (kSumTeams<TWO> + 1) * kTeam + 32 * kScalarWarps + 64;
 template <bool TWO> constexpr int kChunk = TWO ? kSlot / 2 : kSlot;    // bytes of a tensor in a slot
